@@ -308,6 +308,75 @@ int compact_prefix_stack_forward(compact_ctx* ctx, int32_t n_layers, const compa
                                  int32_t n_steps, const void* d_x_decode, compact_kv* shared, compact_kv* tails,
                                  void* d_y_decode, void* d_workspace, size_t ws_bytes, void* hip_stream);
 
+/* ---- paged cache in 8 bits -------------------------------------------------
+ * For a server whose requests arrive, grow and finish (the continuous batch that the paper's server keeps, Sec. IV-B): the
+ * cached rows of a request live in pages of page_rows rows that its row of the block table names, K and V are held in 8 bits,
+ * and every length stays on the device: a step is planned by the GPU from the requests' lengths, no call below reads
+ * a device value on the host, uploads anything or allocates, and all of them may be captured in a HIP graph.
+ *
+ * Codes are E4M3 (OCP 8-bit floating point: no infinities, 0x7F / 0xFF = NaN), scales E8M0: a code c of a page and
+ * KV head stands for c * 2^(scale - 127).  The scale of a page and head is the least power of two (>= 2^-126) that brings the
+ * largest finite value written to it to at most 448; where a later row raises it, the page's codes are rounded to the new
+ * scale once more.  The first row of a page starts it anew, whatever the page held before.
+ * Page sizes: page_rows in {16, 32, 64, 128}.  Both storage types; d_k and d_v must be 16-byte aligned.                    */
+typedef struct compact_paged_kv {
+    void*    d_k;          /* uint8 [n_pages][Hkv][page_rows][hd], after rotary embedding */
+    void*    d_v;          /* uint8 [n_pages][Hkv][hd][page_rows] (transposed: cached rows contiguous) */
+    void*    d_k_scale;    /* uint8 [n_pages][Hkv] */
+    void*    d_v_scale;    /* uint8 [n_pages][Hkv] */
+    int32_t* d_table;      /* [n_requests][max_pages]: row r of request i is in page d_table[i][r / page_rows] */
+    int32_t  n_pages;
+    int32_t  page_rows;
+    int32_t  max_pages;    /* pages of a request at most */
+    int32_t  n_requests;   /* rows of the table, at most 4096 */
+} compact_paged_kv;
+
+/* What compact_paged_plan reads and writes; all device arrays.  No output may be an input (d_free and the table are both):
+ * a program keeps d_len / d_len_out and d_n_free / d_n_free_out in pairs and swaps them.                                  */
+typedef struct compact_paged_step {
+    const int32_t* d_n_new;      /* [N] rows that request i adds: > 0 prompt rows or 1 to decode, 0 rests, < 0 has finished */
+    const int32_t* d_len;        /* [N] rows cached before the step */
+    const int32_t* d_n_free;     /* [1] pages on the stack d_free */
+    int32_t*       d_free;       /* [n_pages] stack of free pages, the last one is taken first */
+    int32_t*       d_n_free_out; /* [1] */
+    int32_t*       d_n_refused;  /* [1] requests whose rows did not fit */
+    int32_t*       d_len_out;    /* [N] rows cached after the step */
+    int32_t*       d_kv_len;     /* [N] the same for requests that add rows in this step, 0 for all others */
+    int32_t*       d_cu;         /* [N + 1] first packed row of every request (2^31 - 1 where it is more) */
+    int64_t*       d_slot;       /* [max_rows] page * page_rows + row in the page; -1 = nowhere */
+    float*         d_rot;        /* [max_rows][hd / 2][2] cos and sin of the row's rotary angles */
+    int32_t        max_rows;     /* rows of the packed batch; those past d_cu[N] get slot -1 and position 0 */
+} compact_paged_step;
+
+/* Plans one step: block table, slot map and rotary table from the lengths, in one launch.  Finished requests (d_n_new < 0)
+ * give their pages back first, pushed on the stack in the order of requests and table columns; then every request that
+ * adds rows takes what it lacks, in the order of requests, the first missing page from the top of the stack.  A request is
+ * refused as a whole -- its length stays, its rows get slot -1, its d_kv_len is 0 -- when its rows end beyond max_rows or max_pages, or
+ * when its pages and those of the requests before it (granted or not) are more than there are.  Table columns that the step does not fill
+ * and stack entries above the old and the new top are left as they are.  COMPACT_ESHAPE beyond 4096 requests. */
+int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, const compact_paged_step* step, void* hip_stream);
+
+/* Rows of a packed qkv [n_rows, Dq + 2 Dkv]: q rotated to d_q [n_rows, Dq], k rotated and v into the pages at d_slot (slots
+ * < 0 or past the last page: nowhere), d_rot as compact_paged_plan writes it.  The rows of a page that one call
+ * writes must be consecutive rows with consecutive slots; rows of the page below the first of them count as written before.
+ * A row whose k (rotated) or v in a KV head holds an infinity or NaN makes every attention output of that head that sees
+ * it NaN and no other: its K codes are NaN, those of its V that are not finite are 0.                                     */
+int compact_rope_paged_write(compact_ctx* ctx, int32_t n_rows, const void* d_qkv, const compact_paged_kv* kv,
+                             const int64_t* d_slot, const float* d_rot, void* d_q, void* hip_stream);
+
+/* Attention of the rows of a step over the pages.  Request i has query rows d_cu[i] .. d_cu[i+1]-1 (n of them, n_rows in
+ * all), the last rows of its d_kv_len[i] cached ones: row j sees cached rows 0 .. d_kv_len[i] - n + j, and gives zeros
+ * where that is none.  One row per request is a decode step, more a prompt or a chunk of one; both may share a call.
+ * max_new and max_kv_len bound n and d_kv_len (rows of requests with more are not computed rightly; nothing outside the
+ * buffers is touched).  q rows are q_stride elements apart (>= Dq, a multiple of 8), o is [n_rows, Dq]; both 16-byte aligned.
+ * Rows that belong to no request are left as they are.  How a request's keys are split depends on its own lengths
+ * alone: its results do not depend on the other requests.  The workspace must hold compact_paged_workspace_bytes(...). */
+int compact_paged_workspace_bytes(const compact_ctx* ctx, int32_t n_requests, int32_t n_rows, int32_t max_new,
+                                  int32_t max_kv_len, size_t* bytes);
+int compact_attn_paged(compact_ctx* ctx, const compact_paged_kv* kv, int32_t n_rows, const int32_t* d_cu,
+                       const int32_t* d_kv_len, int32_t max_new, int32_t max_kv_len, const void* d_q, int64_t q_stride,
+                       void* d_o, void* d_workspace, size_t ws_bytes, void* hip_stream);
+
 /* ---- per-kernel timing ----------------------------------------------------
  * When enabled, every launch of the selected kernel class is bracketed by HIP
  * events on the launch stream.  compact_profile_read synchronises those

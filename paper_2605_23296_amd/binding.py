@@ -28,6 +28,7 @@ EXPORTS = [
     "compact_stack_workspace_bytes", "compact_stack_forward", "compact_prefill_extend", "compact_mxfp4_dequant",
     "compact_mixed_workspace_bytes", "compact_mixed_forward",
     "compact_prefix_stack_workspace_bytes", "compact_prefix_stack_forward",
+    "compact_paged_plan", "compact_rope_paged_write", "compact_paged_workspace_bytes", "compact_attn_paged",
 ]
 
 
@@ -52,6 +53,16 @@ class KV(C.Structure):
 
 class RouteOut(C.Structure):
     _fields_ = [("d_expert_idx", C.c_void_p), ("d_gate", C.c_void_p)]
+
+
+class PagedKVStruct(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p), ("d_table", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_rows", C.c_int32), ("max_pages", C.c_int32), ("n_requests", C.c_int32)]
+
+
+class PagedStepStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_n_new", "d_len", "d_n_free", "d_free", "d_n_free_out", "d_n_refused", "d_len_out",
+                                          "d_kv_len", "d_cu", "d_slot", "d_rot")] + [("max_rows", C.c_int32)]
 
 
 class CompactError(RuntimeError):
@@ -104,6 +115,10 @@ def lib():
     L.compact_mxfp4_dequant.argtypes = [vp, vp, vp, i64, i32, vp, vp]
     L.compact_stack_workspace_bytes.argtypes = [vp, i64, i32, i32, P(sz)]
     L.compact_stack_forward.argtypes = [vp, i32, P(Weights), i32, P(i32), vp, i32, vp, P(KV), vp, vp, vp, sz, vp]
+    L.compact_paged_plan.argtypes = [vp, P(PagedKVStruct), P(PagedStepStruct), vp]
+    L.compact_rope_paged_write.argtypes = [vp, i32, vp, P(PagedKVStruct), vp, vp, vp, vp]
+    L.compact_paged_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, P(sz)]
+    L.compact_attn_paged.argtypes = [vp, P(PagedKVStruct), i32, vp, vp, i32, i32, vp, i64, vp, vp, sz, vp]
     for name in EXPORTS:
         fn = getattr(L, name)
         if name not in ("compact_destroy", "compact_last_error"):
@@ -170,6 +185,72 @@ class KVCache:
         L, Hkv, hd = self.h_len[b], self.layer.n_kv_heads, self.layer.head_dim
         slab = self.v[self.offs[b]:self.offs[b] + self.caps[b] * Hkv * hd].view(Hkv, hd, self.caps[b])
         return slab[:, :, :L].permute(2, 0, 1)
+
+
+class PagedKV:
+    """Pages in 8 bits and their block table (compact_paged_kv): k uint8 [n_pages, Hkv, page_rows, hd], v uint8 [n_pages, Hkv,
+    hd, page_rows], k_scale and v_scale uint8 [n_pages, Hkv], table int32 [n_requests, max_pages].  n_pages and page_rows
+    are taken from k unless given (a plan needs the table alone)."""
+
+    def __init__(self, layer, k, v, k_scale, v_scale, table, n_pages=None, page_rows=None):
+        self.layer, self.k, self.v, self.k_scale, self.v_scale, self.table = layer, k, v, k_scale, v_scale, table
+        self.n_pages = k.shape[0] if n_pages is None else n_pages
+        self.page_rows = k.shape[2] if page_rows is None else page_rows
+        self.n_requests, self.max_pages = table.shape
+        if k.numel():
+            pages, rows = (self.n_pages, layer.n_kv_heads), (self.page_rows, layer.head_dim)
+            assert tuple(k.shape) == pages + rows and tuple(v.shape) == pages + rows[::-1], (k.shape, v.shape)
+            assert tuple(k_scale.shape) == pages and tuple(v_scale.shape) == pages, (k_scale.shape, v_scale.shape)
+        assert all(x.dtype == torch.uint8 and x.is_contiguous() for x in (k, v, k_scale, v_scale))
+        assert table.dtype == torch.int32 and table.is_contiguous()
+        self.c = PagedKVStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), self.n_pages,
+                               self.page_rows, self.max_pages, self.n_requests)
+
+    @classmethod
+    def allocate(cls, layer, n_requests, max_pages, n_pages, page_rows, device):
+        def pool(*shape):
+            return torch.empty((n_pages, layer.n_kv_heads) + shape, dtype=torch.uint8, device=device)
+        table = torch.full((n_requests, max_pages), -1, dtype=torch.int32, device=device)
+        return cls(layer, pool(page_rows, layer.head_dim), pool(layer.head_dim, page_rows), pool(), pool(), table)
+
+    def rows(self, request, length):
+        """Cached rows of a request as fp32 [length, Hkv, hd] (K, V): the values that the codes stand for."""
+        pages = self.table[request, :-(-length // self.page_rows)].long()
+
+        def values(codes, scale):
+            return codes[pages].view(torch.float8_e4m3fn).float() * scale[pages].view(torch.float8_e8m0fnu).float()[..., None, None]
+
+        def flat(x):   # [pages, Hkv, page_rows, hd]
+            return x.transpose(1, 2).reshape(-1, *x.shape[1:2], x.shape[3])[:length]
+        return flat(values(self.k, self.k_scale)), flat(values(self.v, self.v_scale).transpose(2, 3))
+
+
+class PagedStep:
+    """Device arrays of a step's plan (compact_paged_step).  Arrays not given are allocated: all pages free, no rows cached."""
+
+    def __init__(self, layer, n_requests, max_rows, device, n_pages=None, n_new=None, len=None, free=None, n_free=None):
+        def ints(n, given=None):
+            return torch.zeros(n, dtype=torch.int32, device=device) if given is None else given
+        self.n_new, self.len = ints(n_requests, n_new), ints(n_requests, len)
+        # the last entry of the stack is taken first: page 0
+        self.free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device) if free is None else free
+        self.n_free = ints(1, n_free) if n_free is not None else torch.tensor([self.free.numel()], dtype=torch.int32, device=device)
+        self.n_free_out, self.n_refused = ints(1), ints(1)
+        self.len_out, self.kv_len, self.cu = ints(n_requests), ints(n_requests), ints(n_requests + 1)
+        self.slot = torch.empty(max_rows, dtype=torch.int64, device=device)
+        self.rot = torch.empty((max_rows, layer.head_dim // 2, 2), dtype=torch.float32, device=device)
+        self.n_requests, self.max_rows = n_requests, max_rows
+        assert self.n_new.numel() == n_requests and self.len.numel() == n_requests
+        assert all(x.dtype == torch.int32 for x in (self.n_new, self.len, self.free, self.n_free))
+
+    def struct(self):
+        return PagedStepStruct(*[x.data_ptr() for x in (self.n_new, self.len, self.n_free, self.free, self.n_free_out, self.n_refused,
+                                                        self.len_out, self.kv_len, self.cu, self.slot, self.rot)], self.max_rows)
+
+    def advance(self):
+        """After a step: its lengths and its stack are the next one's."""
+        self.len, self.len_out = self.len_out, self.len
+        self.n_free, self.n_free_out = self.n_free_out, self.n_free
 
 
 class Layer:
@@ -324,6 +405,33 @@ class Layer:
         wsp, wsn = self._ws()
         self.check(self.L.compact_attn_decode_prefix(self.ctx, tails.N, _ptr(q), C.byref(shared.c), _i32arr(prefix_len),
                                                      C.byref(tails.c), _ptr(o), wsp, wsn, _stream()))
+
+    # -- paged cache in 8 bits ------------------------------------------------------
+    def compact_paged_plan(self, kv, step):
+        assert step.n_requests == kv.n_requests and step.free.numel() >= kv.n_pages
+        self.check(self.L.compact_paged_plan(self.ctx, C.byref(kv.c), C.byref(step.struct()), _stream()))
+
+    def compact_rope_paged_write(self, qkv, kv, slot, rot, q):
+        """qkv [rows, Dq + 2 Dkv] -> q [rows, Dq] (rotated), k and v into kv's pages at slot [rows]."""
+        self.check(self.L.compact_rope_paged_write(self.ctx, qkv.shape[0], _ptr(qkv), C.byref(kv.c), _ptr(slot), _ptr(rot), _ptr(q), _stream()))
+
+    def paged_workspace_bytes(self, n_requests, n_rows, max_new, max_kv_len):
+        n = C.c_size_t()
+        self.check(self.L.compact_paged_workspace_bytes(self.ctx, n_requests, n_rows, max_new, max_kv_len, C.byref(n)))
+        return n.value
+
+    def ensure_paged_workspace(self, n_requests, n_rows, max_new, max_kv_len, device):
+        need = self.paged_workspace_bytes(n_requests, n_rows, max_new, max_kv_len)
+        if self.ws is None or self.ws.numel() < need:
+            self.ws = torch.empty(need, dtype=torch.uint8, device=device)
+        return self.ws
+
+    def compact_attn_paged(self, q, kv, cu, kv_len, max_new, max_kv_len, o):
+        """q [rows, >= Dq] (its rows may be apart), o [rows, Dq]."""
+        assert q.stride(1) == 1
+        wsp, wsn = self._ws()
+        self.check(self.L.compact_attn_paged(self.ctx, C.byref(kv.c), q.shape[0], _ptr(cu), _ptr(kv_len), max_new, max_kv_len,
+                                             C.c_void_p(q.data_ptr()), q.stride(0), _ptr(o), wsp, wsn, _stream()))
 
     # -- profiling --------------------------------------------------------------
     def compact_profile_select(self, klass):

@@ -1,0 +1,62 @@
+// Attention over the paged cache: what its kernels share.
+#pragma once
+#include "paged.h"
+
+#define LOG2E 1.4426950408889634f
+
+#define FEW_COLS 16      // query columns (rows x heads of a KV group) of a request that the streaming kernel takes: one MFMA tile
+#define FEW_CHUNK 256    // cached rows of one of its work items
+#define TILE_COLS 128    // query columns of a tile of the other kernel
+#define TILE_KEYS 64     // cached rows of a step of it
+#define TILE_SPLIT 512   // a request of t tiles has its keys cut into pieces of 512 t to 1024 t rows
+
+struct PagedAttnArgs {
+    PagedView kv;
+    const int32_t *cu, *kv_len;
+    int n_rows, max_new, max_kv;   // the call's bounds (max_kv: no more than the table holds)
+    const void* q;
+    void* o;
+    int64_t q_stride;
+    int Hq, Hkv;
+    float scale_log2;
+    // records of requests whose keys are split: [request][row][query head][piece], HD values each, and behind all of them (max, sum)
+    float* rec;
+    int64_t rec_stride;       // row-pieces of a request
+    int64_t n_rec;            // records in all
+    int32_t* sched;           // tile kernel: [8] units taken per XCD, then [N + 1] units before request i
+};
+
+struct PagedReq {
+    int row0, n, kv;   // first packed row, rows, cached rows (whatever the arrays hold: inside the buffers)
+};
+__device__ __forceinline__ PagedReq paged_req(const PagedAttnArgs& a, int i) {
+    PagedReq r;
+    r.row0 = min(max(a.cu[i], 0), a.n_rows);
+    r.n = min(min(max(a.cu[i + 1], r.row0), a.n_rows) - r.row0, a.max_new);
+    r.kv = min(max(a.kv_len[i], 0), a.max_kv);
+    return r;
+}
+__device__ __forceinline__ bool is_few(int n, int group) { return n <= FEW_COLS && n * group <= FEW_COLS; }
+// pieces of a request's keys (at least one, so that a request without keys has somebody to write its zeros)
+__device__ __forceinline__ int few_pieces(int kv) { return max((kv + FEW_CHUNK - 1) / FEW_CHUNK, 1); }
+__device__ __forceinline__ int n_tiles(int n, int group) { return (int)(((int64_t)n * group + TILE_COLS - 1) / TILE_COLS); }
+__device__ __forceinline__ int tile_pieces(int tiles, int kv) { return max(kv / TILE_SPLIT / tiles, 1); }
+// rows of a piece: the last piece may hold fewer
+__device__ __forceinline__ int tile_piece_rows(int pieces, int kv) {
+    return ((kv + pieces - 1) / pieces + TILE_KEYS - 1) / TILE_KEYS * TILE_KEYS;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// x as the sum of NP bf16 values: rounded once (NP = 1), or all 24 bits of it (NP = 3)
+template <int NP>
+__device__ __forceinline__ void split_bf16(float x, bf16 (&p)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        p[i] = (bf16)x;
+        x -= (float)p[i];
+    }
+}
+
+// attn_paged_tiles.hip
+int launch_attn_paged_tiles(compact_ctx* ctx, const PagedAttnArgs& a, hipStream_t s);
