@@ -58,5 +58,10 @@ __device__ __forceinline__ void split_bf16(float x, bf16 (&p)[NP]) {
     }
 }
 
+__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) { *reinterpret_cast<floatx4*>(p) = floatx4{a, b, c, d}; }
+__device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d) {
+    *reinterpret_cast<bf16x4*>(p) = bf16x4{(bf16)a, (bf16)b, (bf16)c, (bf16)d};
+}
+
 // attn_paged_tiles.hip
 int launch_attn_paged_tiles(compact_ctx* ctx, const PagedAttnArgs& a, hipStream_t s);
