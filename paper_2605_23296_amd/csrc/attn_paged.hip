@@ -77,11 +77,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void attn_paged_few_kernel(const Pa
             }
             int all;
             const int upto = block_prefix(units, red, all);
-            if (i < N) a.sched[8 + i + 1] = before + upto;
+            if (i < N) a.sched[SCHED_UNITS + i + 1] = before + upto;
             before += all;
         }
-        if (t == 0) a.sched[8] = 0;
-        if (t < 8) a.sched[t] = 0;
+        if (t == 0) a.sched[SCHED_UNITS] = 0;
+        if (t < 8) a.sched[t * SCHED_PITCH] = 0;
         __syncthreads();
     }
 
@@ -282,43 +282,76 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void attn_paged_few_kernel(const Pa
 }
 
 // ---------------------------------------------------------------------------
-// Joins the pieces of one (row, query head): one wavefront each.  HD / 4 lanes span a record.
+// Joins the pieces of the (row, query head) pairs of split requests: WAVES wavefronts each, HD / 4 lanes span a record, and a
+// lane sends for MERGE_FLIGHT records before it uses one.  Four wavefronts where a request can have more than MERGE_SHORT pieces,
+// one up to there.
 // ---------------------------------------------------------------------------
-template <int HD, typename T>
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnArgs a, int rows_per_req) {
-    constexpr int TPR = HD / 4, NS = 64 / TPR;   // lanes per record, records side by side
-    const int lane = threadIdx.x & 63, G = a.Hq / a.Hkv;
-    const int64_t id = (int64_t)blockIdx.x * 4 + wave_index();
-    const int head = (int)(id % a.Hq), row = (int)(id / a.Hq % rows_per_req), req = (int)(id / a.Hq / rows_per_req);
-    if (req >= a.kv.n_requests) return;
+#define MERGE_FLIGHT 8
+#define MERGE_SHORT 16
+template <int HD, int WAVES, typename T>
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnArgs a, int rows_per_req, int heads_per_wg) {
+    constexpr int TPR = HD / 4, NS = 64 / TPR, STEP = NS * WAVES;   // lanes per record, records side by side
+    constexpr int PAIRS = 4 / WAVES;                                  // pairs that a workgroup has in hand at a time
+    __shared__ floatx4 part[WAVES == 1 ? 1 : WAVES * TPR];
+    const int lane = threadIdx.x & 63, wave = wave_index(), G = a.Hq / a.Hkv;
+    const int per_row = (a.Hq + heads_per_wg - 1) / heads_per_wg;
+    const int id = blockIdx.x / per_row, h_lo = blockIdx.x % per_row * heads_per_wg;
+    const int row = id % rows_per_req, req = id / rows_per_req;
     const PagedReq rq = paged_req(a, req);
     if (row >= rq.n) return;
     const int pieces = is_few(rq.n, G) ? few_pieces(rq.kv) : tile_pieces(n_tiles(rq.n, G), rq.kv);
     if (pieces == 1) return;   // written by the kernel before
-    const int64_t rec = ((int64_t)req * a.rec_stride + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces;
-    const float* val = a.rec + rec * HD;
-    const float2* ml = reinterpret_cast<const float2*>(a.rec + a.n_rec * HD) + rec;
-    float m = -3e38f, l = 0.f;
-    for (int i = lane; i < pieces; i += 64) m = fmaxf(m, ml[i].x);
-    m = wave_max(m);
-    for (int i = lane; i < pieces; i += 64) l += exp2_fast(ml[i].x - m) * ml[i].y;
-    l = wave_sum(l);
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i = lane / TPR; i < pieces; i += NS) {
-        const float w = exp2_fast(ml[i].x - m);
-        const floatx4 v = *reinterpret_cast<const floatx4*>(val + (size_t)i * HD + lane % TPR * 4);
+    const int sub = WAVES == 1 ? lane / TPR : wave * NS + lane / TPR, e4 = lane % TPR;
+    for (int head = h_lo + wave / WAVES; head < min(h_lo + heads_per_wg, a.Hq); head += PAIRS) {
+        const int64_t rec = ((int64_t)req * a.rec_stride + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces;
+        const floatx4* val = reinterpret_cast<const floatx4*>(a.rec + rec * HD) + e4;
+        const float2* ml = reinterpret_cast<const float2*>(a.rec + a.n_rec * HD) + rec;
+        floatx4 v[MERGE_FLIGHT];
+        float2 w[MERGE_FLIGHT];
+        auto load = [&](int i0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += w * v[e];
-    }
+            for (int u = 0; u < MERGE_FLIGHT; ++u) {
+                const int i = min(i0 + u * STEP + sub, pieces - 1);
+                v[u] = val[(size_t)i * TPR];
+                w[u] = ml[i];
+            }
+        };
+        load(0);
+        float m = -3e38f, l = 0.f;
+        for (int i = lane; i < pieces; i += 64) m = fmaxf(m, ml[i].x);
+        m = wave_max(m);
+        for (int i = lane; i < pieces; i += 64) l += exp2_fast(ml[i].x - m) * ml[i].y;
+        l = wave_sum(l);
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = 0;;) {
 #pragma unroll
-    for (int ofs = TPR; ofs < 64; ofs <<= 1)
+            for (int u = 0; u < MERGE_FLIGHT; ++u) {
+                const float f = i0 + u * STEP + sub < pieces ? exp2_fast(w[u].x - m) : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], ofs, 64);
-    if (lane < TPR) {
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        T* op = (T*)a.o + ((size_t)(rq.row0 + row) * a.Hq + head) * HD + lane * 4;
+                for (int e = 0; e < 4; ++e) acc[e] += f != 0.f ? f * v[u][e] : 0.f;
+            }
+            i0 += MERGE_FLIGHT * STEP;
+            if (i0 >= pieces) break;
+            load(i0);
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) op[e] = from_f32<T>(acc[e] * inv);
+        for (int ofs = TPR; ofs < 64; ofs <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], ofs, 64);
+        if (WAVES > 1) {
+            __syncthreads();
+            if (lane < TPR) part[wave * TPR + lane] = acc;
+            __syncthreads();
+            if (wave > 0) continue;
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += part[i * TPR + e4][e];
+        }
+        if (lane < TPR) {
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            put4((T*)a.o + ((size_t)(rq.row0 + row) * a.Hq + head) * HD + lane * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        }
     }
 }
 
@@ -346,7 +379,7 @@ static int64_t record_stride(const compact_layer_cfg& c, int max_new, int max_kv
 
 static size_t paged_workspace(const compact_layer_cfg& c, int n_requests, int max_new, int max_kv) {
     const size_t rec = (size_t)n_requests * record_stride(c, max_new, max_kv) * c.n_q_heads;
-    return align_up(sizeof(int32_t) * (8 + PAGED_MAX_REQUESTS + 1), 256) + rec * (c.head_dim + 2) * 4;
+    return align_up(SCHED_BYTES, 256) + rec * (c.head_dim + 2) * 4;
 }
 
 static int check_bounds(compact_ctx* ctx, int n_requests, int n_rows, int max_new, int max_kv_len) {
@@ -385,9 +418,15 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     const int G = c.n_q_heads / c.n_kv_heads;
     const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * (a.max_kv / TILE_SPLIT / 2) / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
-    const int64_t wgs = (rows * c.n_q_heads * a.kv.n_requests + 3) / 4;
+    const int most_pieces = std::max((a.max_kv - 1) / FEW_CHUNK + 1, tiles ? a.max_kv / TILE_SPLIT : 0);
+    const int pairs = most_pieces > MERGE_SHORT ? 1 : 4;   // side by side in a workgroup
+    // (workgroups of rows that are not split leave at once: no more than some thousand of them)
+    int heads = pairs;
+    while (heads < c.n_q_heads && rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads) > 4096) heads *= 2;
+    const int64_t wgs = rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads);
     if (wgs >= INT32_MAX / 256) return set_err(ctx, COMPACT_ESHAPE, "too many rows of split requests for one call");
-    attn_paged_merge_kernel<HD, T><<<(unsigned)wgs, 256, 0, s>>>(a, (int)rows);
+    auto merge = pairs == 1 ? attn_paged_merge_kernel<HD, 4, T> : attn_paged_merge_kernel<HD, 1, T>;
+    merge<<<(unsigned)wgs, 256, 0, s>>>(a, (int)rows, heads);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }
@@ -422,7 +461,7 @@ extern "C" int compact_attn_paged(compact_ctx* ctx, const compact_paged_kv* kv, 
     a.rec_stride = record_stride(c, max_new, a.max_kv);
     a.n_rec = (int64_t)kv->n_requests * a.rec_stride * c.n_q_heads;
     a.sched = (int32_t*)d_workspace;
-    a.rec = (float*)((char*)d_workspace + align_up(sizeof(int32_t) * (8 + PAGED_MAX_REQUESTS + 1), 256));
+    a.rec = (float*)((char*)d_workspace + align_up(SCHED_BYTES, 256));
     const bool b = c.dtype == COMPACT_BF16;
     auto launch = c.head_dim == 128 ? (b ? launch_attn_paged<128, 1, bf16> : launch_attn_paged<128, 3, float>)
                                     : (b ? launch_attn_paged<64, 1, bf16> : launch_attn_paged<64, 3, float>);
