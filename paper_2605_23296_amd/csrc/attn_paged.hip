@@ -8,20 +8,7 @@
 #define FEW_WAVES 4
 #define FEW_PLD (FEW_CHUNK + 8)   // bf16 per column of the probability tile (padded against bank conflicts)
 
-// sum over the workgroup's threads, the same for all; `red`: one int per wavefront
-__device__ __forceinline__ int block_total(int v, int* red) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    int t = 0;
-#pragma unroll
-    for (int i = 0; i < FEW_WAVES; ++i) t += red[i];
-    return t;
-}
-
-// inclusive sum over the workgroup's threads
+// inclusive sum over the workgroup's threads; `red`: one int per wavefront
 __device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
@@ -46,20 +33,42 @@ __device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
 // cached rows); a persistent workgroup of four wavefronts takes a contiguous share of them.  Scores S^T = K Q^T by
 // v_mfma_f32_16x16x32_bf16, 64 cached rows per wavefront; the codes go straight from memory into MFMA operands (exact in
 // bf16); probabilities through LDS; output O^T = V^T P^T, HD / 4 elements per wavefront.
+// The loads run ahead of the items: the next item's K codes are sent for as soon as the scores of this one have used its own, its V
+// codes behind the output, its pages' numbers and scales an item earlier still.  For the compiler to wait for no more
+// than it needs (it counts outstanding loads), every load of the loop is issued unconditionally, with an address that is
+// read anyway where there is no next item, and the stores stand right before the V loads.  Records are held back in LDS until the
+// buffer is full or the share is done: a store in the load stream stalls it out of proportion.
 // NP: bf16 parts of a query and of a probability (3 for fp32 storage: all 24 bits).
 // ---------------------------------------------------------------------------
+#define FEW_REC_SLOTS 8
+__host__ __device__ constexpr int few_resident(int hd, int np) { return np > 1 ? 2 : hd == 128 ? 3 : 4; }   // workgroups per CU
+
+// barrier that waits for this wavefront's LDS operations only: loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));   // lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+}
+
 template <int HD, int NP, typename T, bool TILES>
-__global__ __launch_bounds__(FEW_WAVES * 64) void attn_paged_few_kernel(const PagedAttnArgs a) {
+__global__ __launch_bounds__(FEW_WAVES * 64, few_resident(HD, NP)) void attn_paged_few_kernel(const PagedAttnArgs a, int slot_cols, int rec_slots) {
     constexpr int KH = HD / 64;                // 16-byte pieces of a K row per lane
     constexpr int RT = HD / 16 / FEW_WAVES;    // 16-element tiles of O^T per wavefront
     constexpr int VS = FEW_CHUNK / 64;         // 16-byte pieces of a V row per lane
+    constexpr int RLD = HD + 4;                // floats of a held record: values, maximum, sum
     __shared__ __attribute__((aligned(16))) bf16 qs[NP][FEW_COLS * HD];
     __shared__ __attribute__((aligned(16))) bf16 ps[NP][FEW_COLS * FEW_PLD];
     __shared__ float s_max[FEW_WAVES][16], s_sum[FEW_WAVES][16];
-    __shared__ int red[FEW_WAVES], s_first[2];
+    __shared__ int red[FEW_WAVES];
+    extern __shared__ __attribute__((aligned(16))) float recbuf[];   // [slot][column][RLD]
+    __shared__ int64_t held_rec[FEW_REC_SLOTS];
+    __shared__ int held_pieces[FEW_REC_SLOTS], held_cols[FEW_REC_SLOTS];
     const int N = a.kv.n_requests, G = a.Hq / a.Hkv, Hkv = a.Hkv;
     const int t = threadIdx.x, lane = t & 63, wave = wave_index();
-    const int r = lane & 15, c = lane >> 4;
+    const int r = lane & 15, c = lane >> 4, r_row = r / G, r_head = r % G;
     const int shift = a.kv.page_shift, P = 1 << shift;
 
     // ---- the other kernel's schedule: units (tile, piece) before every request, nothing taken yet ----
@@ -85,103 +94,167 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void attn_paged_few_kernel(const Pa
         __syncthreads();
     }
 
-    // ---- this workgroup's share: items are numbered by request, KV head, chunk ----------------------
-    auto items_of = [&](int i) {
-        const PagedReq rq = paged_req(a, i);
-        return rq.n > 0 && is_few(rq.n, G) ? few_pieces(rq.kv) * Hkv : 0;
-    };
-    int mine = 0;
-    for (int i = t; i < N; i += FEW_WAVES * 64) mine += items_of(i);
-    const int total = block_total(mine, red);
-    int w = (int)((int64_t)blockIdx.x * total / gridDim.x);
-    const int w_end = (int)((int64_t)(blockIdx.x + 1) * total / gridDim.x);
-    if (w >= w_end) return;
-    {   // the request that item w belongs to: wavefront 0 walks over the requests, 64 at a time
-        if (wave == 0) {
-            int before = 0;
-            for (int i0 = 0; i0 < N; i0 += 64) {
-                const int n = i0 + lane < N ? items_of(i0 + lane) : 0;
-                int upto = n;
+    // ---- this workgroup's share: items are numbered by request, KV head, chunk.  Every wavefront goes over the requests by
+    // itself, 64 at a time: once for their number, again for the request of the first item (which stays in the registers of
+    // its lane's scan where there are no more than 64) ----------------------
+    auto items_of = [&](const PagedReq& rq) { return rq.n > 0 && is_few(rq.n, G) ? few_pieces(rq.kv) * Hkv : 0; };
+    PagedReq rq;
+    int n_items = 0, upto = 0;   // of the lane's request, and of all up to it
+    auto scan = [&](int i0) {
+        rq = paged_req(a, min(i0 + lane, N - 1));
+        n_items = i0 + lane < N ? items_of(rq) : 0;
+        upto = n_items;
 #pragma unroll
-                for (int ofs = 1; ofs < 64; ofs <<= 1) {
-                    const int u = __shfl_up(upto, ofs, 64);
-                    if (lane >= ofs) upto += u;
-                }
-                const uint64_t past = __ballot(before + upto > w);
-                if (past) {
-                    if (lane == __builtin_ctzll(past)) {
-                        s_first[0] = i0 + lane;
-                        s_first[1] = w - (before + upto - n);
-                    }
-                    break;
-                }
-                before += __shfl(upto, 63, 64);
-            }
+        for (int ofs = 1; ofs < 64; ofs <<= 1) {
+            const int u = __shfl_up(upto, ofs, 64);
+            if (lane >= ofs) upto += u;
         }
-        __syncthreads();
+    };
+    int total = 0;
+    for (int i0 = 0; i0 < N; i0 += 64) {
+        scan(i0);
+        total += __builtin_amdgcn_readlane(upto, 63);
     }
-    int req = __builtin_amdgcn_readfirstlane(s_first[0]), in_req = __builtin_amdgcn_readfirstlane(s_first[1]);
-    PagedReq rq = paged_req(a, req);
-    int pieces = few_pieces(rq.kv);
-    int q_req = -1, q_head = -1;
+    const int w = (int)((int64_t)blockIdx.x * total / gridDim.x);
+    int left = (int)((int64_t)(blockIdx.x + 1) * total / gridDim.x) - w;
+    if (left <= 0) return;
+    int first = 0, before = 0;   // the request of item w, 64 i0 + its lane
+    uint64_t past = 0;
+    for (;; first += 64) {
+        if (N > 64) scan(first);
+        past = __ballot(before + upto > w);
+        if (past) break;
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int at = __builtin_ctzll(past);
 
-    for (; w < w_end; ++w, ++in_req) {
-        while (in_req >= pieces * Hkv) {   // (w < w_end: there is a request with items left)
-            do {
-                ++req;
-                rq = paged_req(a, req);
-            } while (rq.n <= 0 || !is_few(rq.n, G));
-            pieces = few_pieces(rq.kv);
-            in_req = 0;
-        }
-        const int kvh = in_req / pieces, ch = in_req - kvh * pieces;
-        const int base = ch * FEW_CHUNK, n_keys = min(rq.kv - base, FEW_CHUNK), cols = rq.n * G;
+    // ---- items: a request's lengths come through the scalar cache, outside the counter of vector loads ----
+    typedef const __attribute__((address_space(4))) int32_t* IntPtr;
+    const IntPtr cu = (IntPtr)a.cu, kv_len = (IntPtr)a.kv_len;
+    struct Item {
+        int req, row0, n, kv, pieces, kvh, ch;
+    };
+    auto enter = [&](Item& it, int req) {
+        it.req = req;
+        it.row0 = min(max(cu[req], 0), a.n_rows);
+        it.n = min(min(max(cu[req + 1], it.row0), a.n_rows) - it.row0, a.max_new);
+        it.kv = min(max(kv_len[req], 0), a.max_kv);
+        it.pieces = few_pieces(it.kv);
+    };
+    auto next_item = [&](Item& it) {   // (only called while there is one)
+        if (++it.ch < it.pieces) return;
+        it.ch = 0;
+        if (++it.kvh < Hkv) return;
+        it.kvh = 0;
+        int req = it.req;
+        do {
+            enter(it, ++req);
+        } while (it.n <= 0 || !is_few(it.n, G));
+    };
+    Item cur, nxt;
+    cur.req = first + at;
+    cur.row0 = __builtin_amdgcn_readlane(rq.row0, at);
+    cur.n = __builtin_amdgcn_readlane(rq.n, at);
+    cur.kv = __builtin_amdgcn_readlane(rq.kv, at);
+    cur.pieces = few_pieces(cur.kv);
+    {
+        const int in_req = w - before - __builtin_amdgcn_readlane(upto - n_items, at);
+        cur.kvh = in_req / cur.pieces;
+        cur.ch = in_req - cur.kvh * cur.pieces;
+    }
 
-        // lane l < 16 (and l + 16 ..) holds the page and the scales of granule l of the chunk
-        const int gtok = max(min(base + r * PAGED_GRAN, rq.kv - 1), 0);
-        const int pid = min(max(a.kv.table[(size_t)req * a.kv.max_pages + (gtok >> shift)], 0), a.kv.n_pages - 1);
-        const size_t ph = (size_t)pid * Hkv + kvh;
-        const float ksc = e8m0(a.kv.ks[ph]), vsc = e8m0(a.kv.vs[ph]);
-
-        uintx4 kf[4][KH], vf[RT][VS];
+    // lane l holds the page of granule l % 16 of a chunk (granules past the cached rows: the last one's)
+    auto load_pid = [&](const Item& it) {
+        const int row = max(min(it.ch * FEW_CHUNK + r * PAGED_GRAN, it.kv - 1), 0);
+        return a.kv.table[(size_t)it.req * a.kv.max_pages + (row >> shift)];
+    };
+    auto in_range = [&](int pid) { return min(max(pid, 0), a.kv.n_pages - 1); };
+    uintx4 kf[4][KH], vf[RT][VS];
+    // keep = 0 (otherwise all ones): nothing to fetch; the same instructions go out, all lanes for the same few bytes (masks, no
+    // branch: both cases have to be one stream of instructions for the compiler's count of the loads)
+    auto load_k = [&](const Item& it, int pid, int keep) {
+        const int off = (r * HD + c * 16) & keep;
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt) {
-            const int g = wave * 4 + tt, page = __builtin_amdgcn_readlane(pid, g);
-            const uint8_t* kp = a.kv.k + ((((size_t)page * Hkv + kvh) << shift) + ((base + g * PAGED_GRAN) & (P - 1)) + r) * HD + c * 16;
+            const int g = wave * 4 + tt;
+            const unsigned page = __builtin_amdgcn_readlane(pid, g);
+            const uint8_t* kp = a.kv.k + ((((size_t)page * Hkv + it.kvh) << shift) + ((it.ch * FEW_CHUNK + g * PAGED_GRAN) & (P - 1))) * HD;
 #pragma unroll
-            for (int s = 0; s < KH; ++s) kf[tt][s] = *reinterpret_cast<const uintx4*>(kp + s * 64);
+            for (int s = 0; s < KH; ++s) kf[tt][s] = *reinterpret_cast<const uintx4*>(kp + (off + s * 64));
         }
+    };
+    auto load_v = [&](const Item& it, int pid, int keep) {
+        const int row = (wave * RT * 16 + r) & keep, next = (16 << shift) & keep;
 #pragma unroll
         for (int j = 0; j < VS; ++j) {
-            const int g = 4 * j + c, page = __shfl(pid, g, 64);
-            const uint8_t* vp = a.kv.v + ((((size_t)page * Hkv + kvh) * HD) << shift) + ((base + g * PAGED_GRAN) & (P - 1));
+            const int g = (4 * j + c) & keep;
+            const unsigned page = __shfl(pid, g, 64);
+            const uint8_t* vp = a.kv.v + ((((size_t)page * Hkv + it.kvh) * HD + row) << shift) + ((it.ch * FEW_CHUNK + g * PAGED_GRAN) & (P - 1));
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
-                vf[i][j] = *reinterpret_cast<const uintx4*>(vp + ((size_t)((wave * RT + i) * 16 + r) << shift));
+            for (int i = 0; i < RT; ++i) vf[i][j] = *reinterpret_cast<const uintx4*>(vp + i * next);
         }
-        if (req != q_req || kvh != q_head) {   // the group's query rows, column = row * G + head of the group
-            q_req = req;
-            q_head = kvh;
-            __syncthreads();
-            for (int i = t; i < FEW_COLS * HD / 8; i += FEW_WAVES * 64) {
-                const int col = i / (HD / 8), e = i % (HD / 8) * 8;
-                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (col < cols) load8((const T*)a.q + (size_t)(rq.row0 + col / G) * a.q_stride + (kvh * G + col % G) * HD + e, x);
+    };
+    // the item's query rows: columns row * G + head of the group, 8 elements per thread
+    struct alignas(16) Eight { T x[8]; };
+    Eight qreg;
+    const int q_col = min(t / (HD / 8), FEW_COLS - 1), q_e = t % (HD / 8) * 8, q_row = q_col / G, q_head = q_col % G;
+    static_assert(FEW_COLS * HD / 8 <= FEW_WAVES * 64, "a thread holds at most one piece of the query rows");
+    auto load_q = [&](const Item& it) {
+        const int row = it.row0 + min(q_row, it.n - 1);
+        qreg = *reinterpret_cast<const Eight*>((const T*)a.q + (size_t)row * a.q_stride + (it.kvh * G + q_head) * HD + q_e);
+    };
+
+    // (sent in the order that the loop sends them: the compiler waits for a load by the least number of later ones)
+    int pid = load_pid(cur);
+    nxt = cur;
+    if (left > 1) next_item(nxt);
+    int pid_n = load_pid(nxt);
+    pid = in_range(pid);
+    size_t ph = (size_t)pid * Hkv + cur.kvh;
+    unsigned ksb = a.kv.ks[ph], vsb = a.kv.vs[ph];
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(cur, pid, -1);
+    load_q(cur);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(cur, pid, -1);
+    __builtin_amdgcn_sched_barrier(0);
+    int q_req = -1, q_kvh = -1, n_held = 0;
+
+    for (;;) {
+        const bool has_next = left > 1;
+        const int keep = here(has_next ? -1 : 0);
+        const int base = cur.ch * FEW_CHUNK, n_keys = min(cur.kv - base, FEW_CHUNK), cols = cur.n * G;
+        // pages and scales of the next item; the page numbers of the one after it
+        pid = in_range(pid_n);
+        Item nn = nxt;
+        if (left > 2) next_item(nn);
+        pid_n = load_pid(nn);
+        ph = (size_t)pid * Hkv + nxt.kvh;
+        const unsigned ksb_n = a.kv.ks[ph], vsb_n = a.kv.vs[ph];
+
+        if (cur.req != q_req || cur.kvh != q_kvh) {
+            q_req = cur.req;
+            q_kvh = cur.kvh;
+            lds_barrier();   // (the rows before have been read)
+            if (t < FEW_COLS * HD / 8) {
+                bf16x8 part[NP];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     bf16 p[NP];
-                    split_bf16<NP>(x[j], p);
+                    split_bf16<NP>(q_col < cols ? to_f32(qreg.x[j]) : 0.f, p);
 #pragma unroll
-                    for (int u = 0; u < NP; ++u) qs[u][col * HD + e + j] = p[u];
+                    for (int u = 0; u < NP; ++u) part[u][j] = p[u];
                 }
+#pragma unroll
+                for (int u = 0; u < NP; ++u) *reinterpret_cast<bf16x8*>(&qs[u][q_col * HD + q_e]) = part[u];
             }
-            __syncthreads();
+            lds_barrier();
         }
 
         // ---- S^T = K Q^T: lane (r, c) of tile tt gets column r, rows wave * 64 + tt * 16 + 4c .. + 3 ----
         float sv[4][4];
         float mx = -INFINITY;
-        const int sees = min(rq.kv - rq.n + (r < cols ? r / G : 0) + 1 - base, n_keys);   // rows of the chunk that column r sees
+        const int sees = min(cur.kv - cur.n + (r < cols ? r_row : 0) + 1 - base, n_keys);   // rows of the chunk that column r sees
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt) {
             floatx4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -197,17 +270,20 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void attn_paged_few_kernel(const Pa
                     }
                 }
             const int g = wave * 4 + tt;
-            const float f = a.scale_log2 * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ksc), g));
+            const float f = a.scale_log2 * e8m0(__builtin_amdgcn_readlane(ksb, g));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 sv[tt][e] = g * PAGED_GRAN + 4 * c + e < sees ? acc[e] * f : -INFINITY;
                 mx = fmaxf(mx, sv[tt][e]);
             }
         }
+        // the K registers are free
+        load_k(nxt, pid, keep);
+        load_q(nxt);
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         if (c == 0) s_max[wave][r] = mx;
-        __syncthreads();
+        lds_barrier();
         float m = -3e38f;   // (finite where a column sees nothing: its probabilities are exp2(-inf) = 0)
 #pragma unroll
         for (int i = 0; i < FEW_WAVES; ++i) m = fmaxf(m, s_max[i][r]);
@@ -230,54 +306,87 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void attn_paged_few_kernel(const Pa
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
         if (c == 0) s_sum[wave][r] = l;
-        __syncthreads();
+        lds_barrier();
 
         // ---- O^T = V^T P^T: HD / 4 elements per wavefront over all rows of the chunk -----------------
         floatx4 oacc[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) oacc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (n_keys < FEW_CHUNK) {   // whatever lies behind the cached rows must not reach the MFMA
 #pragma unroll
-        for (int j = 0; j < VS; ++j) {
-            const float sc = __shfl(vsc, 4 * j + c, 64);
-            if (n_keys < FEW_CHUNK) {   // whatever lies behind the cached rows must not reach the MFMA
-                const int live = n_keys - (64 * j + 16 * c);
+            for (int j = 0; j < VS; ++j)
 #pragma unroll
                 for (int wd = 0; wd < 4; ++wd) {
-                    const unsigned keep = low_bytes(live - 4 * wd);
+                    const unsigned keep = low_bytes(n_keys - (64 * j + 16 * c) - 4 * wd);
 #pragma unroll
                     for (int i = 0; i < RT; ++i) vf[i][j][wd] &= keep;
                 }
-            }
+        }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int j = 0; j < VS; ++j) {
+            const float sc = e8m0(__shfl(vsb, 4 * j + c, 64));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 vb[RT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) vb[i] = codes8_to_bf16(vf[i][j][2 * h], vf[i][j][2 * h + 1], sc);
 #pragma unroll
                 for (int u = 0; u < NP; ++u) {
                     const bf16x8 pb = *reinterpret_cast<const bf16x8*>(&ps[u][r * FEW_PLD + 64 * j + 16 * c + 8 * h]);
 #pragma unroll
-                    for (int i = 0; i < RT; ++i)
-                        oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8_to_bf16(vf[i][j][2 * h], vf[i][j][2 * h + 1], sc), pb, oacc[i], 0, 0, 0);
+                    for (int i = 0; i < RT; ++i) oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb[i], pb, oacc[i], 0, 0, 0);
                 }
+            }
         }
         float lt = s_sum[0][r];
 #pragma unroll
         for (int i = 1; i < FEW_WAVES; ++i) lt += s_sum[i][r];
         // lane (r, c): column r, elements (wave * RT + i) * 16 + 4c .. + 3
-        if (r < cols) {
-            const int row = r / G, head = kvh * G + r % G;
-            if (pieces == 1) {
+        if (cur.pieces == 1) {
+            if (r < cols) {
                 const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-                T* op = (T*)a.o + ((size_t)(rq.row0 + row) * a.Hq + head) * HD + 4 * c;
+                T* op = (T*)a.o + ((size_t)(cur.row0 + r_row) * a.Hq + cur.kvh * G + r_head) * HD + 4 * c;
 #pragma unroll
-                for (int i = 0; i < RT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) op[(wave * RT + i) * 16 + e] = from_f32<T>(oacc[i][e] * inv);
-            } else {
-                const int64_t rec = ((int64_t)req * a.rec_stride + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces + ch;
-#pragma unroll
-                for (int i = 0; i < RT; ++i) *reinterpret_cast<floatx4*>(a.rec + rec * HD + (wave * RT + i) * 16 + 4 * c) = oacc[i];
-                if (wave == 0 && c == 0) *reinterpret_cast<float2*>(a.rec + a.n_rec * HD + rec * 2) = make_float2(m, lt);
+                for (int i = 0; i < RT; ++i) put4(op + (wave * RT + i) * 16, oacc[i][0] * inv, oacc[i][1] * inv, oacc[i][2] * inv, oacc[i][3] * inv);
             }
+        } else {
+            float* slot = recbuf + (size_t)n_held * slot_cols * RLD + r * RLD;
+            if (r < cols) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i) *reinterpret_cast<floatx4*>(slot + (wave * RT + i) * 16 + 4 * c) = oacc[i];
+                if (wave == 0 && c == 0) *reinterpret_cast<float2*>(slot + HD) = make_float2(m, lt);
+            }
+            if (t == 0) {
+                held_rec[n_held] = (int64_t)cur.req * a.rec_stride * a.Hq + (int64_t)cur.kvh * G * cur.pieces + cur.ch;
+                held_pieces[n_held] = cur.pieces;
+                held_cols[n_held] = cols;
+            }
+            ++n_held;
         }
+        if (n_held == rec_slots || (!has_next && n_held > 0)) {
+            lds_barrier();
+            for (int k = 0; k < n_held; ++k) {
+                const float* slot = recbuf + (size_t)k * slot_cols * RLD;
+                const int pieces = held_pieces[k], n = held_cols[k];
+                for (int i = t; i < n * (HD / 4); i += FEW_WAVES * 64) {
+                    const int col = i / (HD / 4), e = i % (HD / 4) * 4;
+                    const int64_t rec = held_rec[k] + (int64_t)(col / G) * pieces * a.Hq + (int64_t)(col % G) * pieces;
+                    *reinterpret_cast<floatx4*>(a.rec + rec * HD + e) = *reinterpret_cast<const floatx4*>(slot + col * RLD + e);
+                    if (e == 0) *reinterpret_cast<float2*>(a.rec + a.n_rec * HD + rec * 2) = *reinterpret_cast<const float2*>(slot + col * RLD + HD);
+                }
+            }
+            n_held = 0;
+            lds_barrier();
+        }
+        // the V registers are free
+        load_v(nxt, pid, keep);
+        asm volatile("" ::: "memory");   // (the loads stay on this side of the branch, see above)
+        if (!has_next) break;
+        cur = nxt;
+        nxt = nn;
+        ksb = ksb_n;
+        vsb = vsb_n;
+        --left;
     }
 }
 
@@ -404,18 +513,20 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     int n_cus = 0;
     TRY_RC(device_cu_count(ctx, &n_cus));
     const bool tiles = has_tiles(c, a.max_new);
+    const int G = c.n_q_heads / c.n_kv_heads;
     const int64_t most = (int64_t)((a.max_kv - 1) / FEW_CHUNK + 1) * c.n_kv_heads * a.kv.n_requests;   // work items
     if (most > INT32_MAX) return set_err(ctx, COMPACT_ESHAPE, "n_requests * max_kv_len beyond what one call indexes");
     {
         ProfileScope ps(ctx, COMPACT_K_ATTN_DECODE, s);
         auto few = tiles ? attn_paged_few_kernel<HD, NP, T, true> : attn_paged_few_kernel<HD, NP, T, false>;
-        few<<<(unsigned)std::min<int64_t>(most, 3 * n_cus), FEW_WAVES * 64, 0, s>>>(a);
+        const int slot_cols = std::min(a.max_new, FEW_COLS / G) * G, slot_bytes = slot_cols * (HD + 4) * (int)sizeof(float);
+        const int slots = std::max(1, std::min(FEW_REC_SLOTS, (16 << 10) / slot_bytes));
+        few<<<(unsigned)std::min<int64_t>(most, few_resident(HD, NP) * n_cus), FEW_WAVES * 64, slots * slot_bytes, s>>>(a, slot_cols, slots);
     }
     LAUNCH_CHECK(ctx);
     if (tiles) TRY_RC(launch_attn_paged_tiles(ctx, a, s));
     if (a.rec_stride == 0) return COMPACT_OK;
     // rows of a request whose keys may be split: 512 t * 2 <= max_kv for its t tiles
-    const int G = c.n_q_heads / c.n_kv_heads;
     const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * (a.max_kv / TILE_SPLIT / 2) / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
     const int most_pieces = std::max((a.max_kv - 1) / FEW_CHUNK + 1, tiles ? a.max_kv / TILE_SPLIT : 0);
