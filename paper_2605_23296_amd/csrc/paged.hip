@@ -229,12 +229,13 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
 }
 
 // ---------------------------------------------------------------------------
-// Write.  A segment is what a call writes to one page: rows with consecutive slots.  A workgroup of two wavefronts takes a
-// segment and KV head: the first its K rows (rotated on the way), the second its V rows (transposed in
-// registers: a lane holds 16 rows of 8 elements and stores 16 bytes per element).  Both read their rows twice, first for the
-// largest value, then (from the L2) for the codes.  Further workgroups rotate q.
+// Write.  A segment is what a call writes to one page: rows with consecutive slots.  A workgroup of four wavefronts takes a
+// segment and KV head: two of them its K rows (rotated on the way), two its V rows (transposed in registers: a lane holds
+// 16 rows of 4 elements, a granule, and stores 16 bytes per element).  Up to 64 rows (fp32 storage: 32 K rows) are read once and kept
+// in registers until the scale is known; of a longer segment all but the last rows are read a second time.
+// Further workgroups rotate q.
 // ---------------------------------------------------------------------------
-#define WR_NT 128
+#define WR_NT 256
 #define WR_QHEADS 8   // most query heads per wavefront of the q part
 
 template <typename T>
@@ -250,16 +251,252 @@ struct WriteArgs {
     int q_heads;          // query heads per wavefront of the q part
 };
 
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+// A segment as its workgroup sees it.
+struct Segment {
+    int row0, n;      // packed rows
+    int o;            // first row in the page; rows below it were written before
+    size_t ph;        // page * Hkv + KV head
+    int before;       // scale byte so far (1 where nothing was written before)
+};
+
+// Values that wait in registers as they came, as words (of an array of bf16 values the compiler gives every one a register of its
+// own).  Without as_they_are() between their two uses it keeps what the first one made of them instead.
+template <typename T, int N>
+struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Raw {
+    unsigned w[sizeof(T) * N / 4];
+    __device__ __forceinline__ float at(int i) const {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+        return __builtin_bit_cast(float, i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+    }
+    __device__ __forceinline__ void clear(int i) {
+        if constexpr (sizeof(T) == 4)
+            w[i] = 0;
+        else
+            w[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+    }
+    __device__ __forceinline__ void as_they_are() {
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(T) * N / 4; ++i) w[i] = (unsigned)here((int)w[i]);
+    }
+};
+
+// Sizes as the bits of a float without its sign: they order like the values, and what is not finite lies at INF_BITS and above.
+#define INF_BITS 0x7F800000u
+__device__ __forceinline__ unsigned size_bits(float x) { return __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu; }
+__device__ __forceinline__ unsigned wave_max_bits(unsigned v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o, 64));
+    return v;
+}
+
+// What the four wavefronts tell each other: their largest finite sizes (K, K, V, V), and the rows with a value that is not
+// finite, by bit.
+struct WriteShared {
+    unsigned top[4];
+    unsigned bad[4];
+};
+__device__ __forceinline__ bool is_bad(const WriteShared& sh, int j) { return sh.bad[j >> 5] >> (j & 31) & 1; }
+// scale byte of the segment's K (wave 0, 1) or V (2, 3); top: the wavefront's largest finite size
+__device__ __forceinline__ int new_byte(WriteShared& sh, unsigned top, int before) {
+    const int wave = wave_index();
+    if ((threadIdx.x & 63) == 0) sh.top[wave] = top;
+    __syncthreads();
+    return max(before, scale_byte(__builtin_bit_cast(float, max(sh.top[wave & 2], sh.top[wave | 1]))));
+}
+
+// K rows of the segment; wavefront `half` of the two takes rows half * HOLD .. of every 2 HOLD.
+template <int HD, typename T>
+__device__ __forceinline__ void write_k(const WriteArgs<T>& a, const Segment& sg, int kvh, int half, WriteShared& sh) {
+    constexpr int HALF = HD / 2, LPT = HALF / 8, TPW = 64 / LPT;   // lanes per row (8 elements of either half), rows side by side
+    constexpr int HOLD = sizeof(T) == 2 ? 32 : 16, NG = HOLD / TPW;
+    using Eight = Raw<T, 8>;
+    const int lane = threadIdx.x & 63, d = lane % LPT * 8, sub = lane / LPT + half * HOLD;
+    const int ld = (a.Hq + 2 * a.Hkv) * HD;
+    const T* src = a.qkv + (size_t)sg.row0 * ld + (a.Hq + kvh) * HD;
+    const float2* rot = a.rot + (size_t)sg.row0 * HALF;
+    Eight x[NG], y[NG];   // either half of the rows, as they came (in place of rows past the segment: its last one)
+    auto load = [&](int j0) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+            if (j0 + half * HOLD + g * TPW < sg.n) {
+                const unsigned at = (unsigned)min(j0 + g * TPW + sub, sg.n - 1) * ld + d;
+                x[g] = *reinterpret_cast<const Eight*>(src + at);
+                y[g] = *reinterpret_cast<const Eight*>(src + at + HALF);
+            }
+    };
+    auto rotated = [&](int g, int j, float (&lo)[8], float (&hi)[8]) {
+        const Raw<float, 16> cs = *reinterpret_cast<const Raw<float, 16>*>(rot + ((unsigned)min(j, sg.n - 1) * HALF + d));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rotate(x[g].at(e), y[g].at(e), cs.at(2 * e), cs.at(2 * e + 1), lo[e], hi[e]);
+    };
+    unsigned top = 0;
+    int j0 = 0;
+    for (;; j0 += 2 * HOLD) {
+        load(j0);
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+            if (j0 + half * HOLD + g * TPW < sg.n) {
+                const int j = j0 + g * TPW + sub;
+                float lo[8], hi[8];
+                rotated(g, j, lo, hi);
+                unsigned mine = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mine = max(mine, max(size_bits(lo[e]), size_bits(hi[e])));
+                if (__any(mine >= INF_BITS)) {
+                    if (mine >= INF_BITS) {
+                        if (j < sg.n) atomicOr(&sh.bad[j >> 5], 1u << (j & 31));
+                        mine = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (size_bits(lo[e]) < INF_BITS) mine = max(mine, size_bits(lo[e]));
+                            if (size_bits(hi[e]) < INF_BITS) mine = max(mine, size_bits(hi[e]));
+                        }
+                    }
+                }
+                top = max(top, mine);
+                __builtin_amdgcn_sched_barrier(0);   // (one group's rotations in registers at a time)
+            }
+        if (j0 + 2 * HOLD >= sg.n) break;
+    }
+    const int byte = new_byte(sh, wave_max_bits(top), sg.before);
+    uint8_t* kp = a.kv.k + (sg.ph << a.kv.page_shift) * HD;
+    if (byte > sg.before && sg.o > 0) {
+        const float down = e8m0(max(127 + sg.before - byte, 0));
+        for (int i = lane + 64 * half; i < sg.o * (HD / 16); i += 128) {
+            uintx4 w = reinterpret_cast<uintx4*>(kp)[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = recode4(w[e], down);
+            reinterpret_cast<uintx4*>(kp)[i] = w;
+        }
+    }
+    const float up = e8m0(254 - byte);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        x[g].as_they_are();
+        y[g].as_they_are();
+    }
+    for (;;) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const int j = j0 + g * TPW + sub;
+            if (j < sg.n) {
+                float lo[8], hi[8];
+                rotated(g, j, lo, hi);
+                uintx2 wl = {to_codes4(lo[0] * up, lo[1] * up, lo[2] * up, lo[3] * up), to_codes4(lo[4] * up, lo[5] * up, lo[6] * up, lo[7] * up)};
+                uintx2 wh = {to_codes4(hi[0] * up, hi[1] * up, hi[2] * up, hi[3] * up), to_codes4(hi[4] * up, hi[5] * up, hi[6] * up, hi[7] * up)};
+                if (is_bad(sh, j)) wl = wh = uintx2{0x7F7F7F7Fu, 0x7F7F7F7Fu};
+                uint8_t* dst = kp + ((unsigned)(sg.o + j) * HD + d);
+                *reinterpret_cast<uintx2*>(dst) = wl;
+                *reinterpret_cast<uintx2*>(dst + HALF) = wh;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (j0 == 0) break;
+        j0 -= 2 * HOLD;
+        load(j0);
+    }
+    if (lane + 64 * half == 0) a.kv.ks[sg.ph] = (uint8_t)byte;
+}
+
+// V rows of the segment, transposed; lanes of both wavefronts take granules side by side.
+template <int HD, typename T>
+__device__ __forceinline__ void write_v(const WriteArgs<T>& a, const Segment& sg, int kvh, int half, WriteShared& sh) {
+    constexpr int VL = HD / 4, VG = 128 / VL;   // lanes across a row, granules side by side in the two wavefronts
+    using Four = Raw<T, 4>;
+    const int lane = threadIdx.x & 63, d = lane % VL * 4, sub = lane / VL + half * (VG / 2);
+    const int ld = (a.Hq + 2 * a.Hkv) * HD, shift = a.kv.page_shift;
+    const T* src = a.qkv + (size_t)sg.row0 * ld + (a.Hq + a.Hkv + kvh) * HD;
+    uint8_t* vp = a.kv.v + (sg.ph << shift) * HD;
+    const int g_lo = sg.o / PAGED_GRAN, g_end = (sg.o + sg.n + PAGED_GRAN - 1) / PAGED_GRAN;
+    auto place = [&](int g, int e) { return reinterpret_cast<uintx4*>(vp + (((unsigned)(d + e) << shift) + g * PAGED_GRAN)); };
+    Four x[PAGED_GRAN];   // the rows of a granule (in place of those that are not in the segment: the nearest one); 0 for what is not finite
+    // returns the lane's largest finite size
+    auto load = [&](int g) {
+        unsigned mine = 0;
+        if (g < g_end) {
+#pragma unroll
+            for (int u = 0; u < PAGED_GRAN; ++u) x[u] = *reinterpret_cast<const Four*>(src + ((unsigned)min(max(g * PAGED_GRAN + u - sg.o, 0), sg.n - 1) * ld + d));
+#pragma unroll
+            for (int u = 0; u < PAGED_GRAN; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mine = max(mine, size_bits(x[u].at(e)));
+        }
+        if (__any(mine >= INF_BITS)) {
+            if (mine >= INF_BITS) {
+                mine = 0;
+#pragma unroll
+                for (int u = 0; u < PAGED_GRAN; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned size = size_bits(x[u].at(e));
+                        const int j = min(max(g * PAGED_GRAN + u - sg.o, 0), sg.n - 1);
+                        if (size >= INF_BITS) {
+                            atomicOr(&sh.bad[j >> 5], 1u << (j & 31));
+                            x[u].clear(e);
+                        } else {
+                            mine = max(mine, size);
+                        }
+                    }
+            }
+        }
+        return mine;
+    };
+    unsigned top = 0;
+    int g = g_lo + sub;
+    for (;; g += VG) {
+        top = max(top, load(g));
+        if (g - sub + VG >= g_end) break;
+    }
+    const int byte = new_byte(sh, wave_max_bits(top), sg.before);
+    const float up = e8m0(254 - byte), down = e8m0(max(127 + sg.before - byte, 0));
+    const bool grown = byte > sg.before;
+#pragma unroll
+    for (int u = 0; u < PAGED_GRAN; ++u) x[u].as_they_are();
+    if (grown && g_lo > 0) {   // granules of earlier rows alone
+        for (int i = lane + 64 * half; i < g_lo * HD; i += 128) {
+            uintx4* p = reinterpret_cast<uintx4*>(vp + (((unsigned)(i / g_lo) << shift) + i % g_lo * PAGED_GRAN));
+            uintx4 w = *p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = recode4(w[e], down);
+            *p = w;
+        }
+    }
+    for (;;) {
+        if (g < g_end) {
+            const int old = sg.o - g * PAGED_GRAN, end = sg.o + sg.n - g * PAGED_GRAN;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uintx4 w;   // 16 rows of one element
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+                    w[q4] = to_codes4(x[q4 * 4].at(e) * up, x[q4 * 4 + 1].at(e) * up, x[q4 * 4 + 2].at(e) * up, x[q4 * 4 + 3].at(e) * up);
+                if (old > 0 || end < PAGED_GRAN) {   // rows below o: what is there, at the new scale; behind the segment: what is there
+                    const uintx4 there = *place(g, e);
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        const unsigned below = low_bytes(old - 4 * q4), upto = low_bytes(end - 4 * q4);
+                        w[q4] = ((grown ? recode4(there[q4], down) : there[q4]) & below) | (w[q4] & upto & ~below) | (there[q4] & ~upto);
+                    }
+                }
+                *place(g, e) = w;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (g - sub == g_lo) break;
+        g -= VG;
+        load(g);
+    }
+    if (lane + 64 * half == 0) a.kv.vs[sg.ph] = (uint8_t)byte;
+}
 
 template <int HD, typename T>
-__global__ __launch_bounds__(WR_NT) void paged_write_kernel(const WriteArgs<T> a) {
-    constexpr int HALF = HD / 2, LPT = HALF / 8, TPW = 64 / LPT;   // K and q: lanes per row (either half), rows side by side
-    constexpr int VL = HD / 8, VG = 64 / VL;                         // V: lanes across a row, granules side by side
+__global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_kernel(const WriteArgs<T> a) {
+    constexpr int HALF = HD / 2, LPT = HALF / 8, TPW = 64 / LPT;
     const int lane = threadIdx.x & 63, wave = wave_index();
-    const int Hkv = a.Hkv, ld = (a.Hq + 2 * Hkv) * HD;
+    const int Hkv = a.Hkv;
 
-    if ((int)blockIdx.x >= a.n_kv_wgs) {   // ---- q: TPW rows of q_heads heads per wavefront
+    using Eight = Raw<T, 8>;
+    if ((int)blockIdx.x >= a.n_kv_wgs) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
         const int task = ((int)blockIdx.x - a.n_kv_wgs) * (WR_NT / 64) + wave;
         const int per_row = (a.Hq + a.q_heads - 1) / a.q_heads;
         const int row = task / per_row * TPW + lane / LPT, h0 = task % per_row * a.q_heads, d = lane % LPT * 8;
@@ -267,162 +504,68 @@ __global__ __launch_bounds__(WR_NT) void paged_write_kernel(const WriteArgs<T> a
         float2 cs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) cs[j] = a.rot[(size_t)row * HALF + d + j];
-        const T* src = a.qkv + (size_t)row * ld + d;
+        const T* src = a.qkv + (size_t)row * ((a.Hq + 2 * Hkv) * HD) + d;
         T* dst = a.q + (size_t)row * a.Hq * HD + d;
-        for (int h = h0; h < min(h0 + a.q_heads, a.Hq); ++h) {
-            float lo[8], hi[8], olo[8], ohi[8];
-            load8(src + h * HD, lo);
-            load8(src + h * HD + HALF, hi);
+        const int h_end = min(h0 + a.q_heads, a.Hq);
+        for (int h = h0; h < h_end; h += 4) {
+            Eight x[4], y[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) rotate(lo[j], hi[j], cs[j].x, cs[j].y, olo[j], ohi[j]);
-            store8(dst + h * HD, olo);
-            store8(dst + h * HD + HALF, ohi);
+            for (int u = 0; u < 4; ++u)
+                if (h + u < h_end) {
+                    x[u] = *reinterpret_cast<const Eight*>(src + (h + u) * HD);
+                    y[u] = *reinterpret_cast<const Eight*>(src + (h + u) * HD + HALF);
+                }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (h + u < h_end) {
+                    float lo[8], hi[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) rotate(x[u].at(j), y[u].at(j), cs[j].x, cs[j].y, lo[j], hi[j]);
+                    store8(dst + (h + u) * HD, lo);
+                    store8(dst + (h + u) * HD + HALF, hi);
+                }
         }
         return;
     }
 
     // ---- K and V: the segments that begin in this workgroup's rows
-    __shared__ unsigned bad_rows[2][4];   // rows of the segment with a value that is not finite, by wavefront
+    __shared__ WriteShared sh;
     const int kvh = blockIdx.x % Hkv, shift = a.kv.page_shift, P = 1 << shift;
     const int row_lo = (int)(blockIdx.x / Hkv) * a.chunk;
     const int64_t n_slots = (int64_t)a.kv.n_pages << shift;
     auto slot_of = [&](int row) { return row >= 0 && row < a.n_rows ? a.slot[row] : (int64_t)-1; };
-    uint64_t begins;
-    {
-        const int row = row_lo + lane;
-        const int64_t s = lane < a.chunk ? slot_of(row) : -1;
-        begins = __ballot(s >= 0 && s < n_slots && ((s & (P - 1)) == 0 || slot_of(row - 1) != s - 1));
-    }
+    // the slots of 64 rows from row_lo on: `cuts` marks those that do not continue the row before them in its page
+    const int64_t s = slot_of(row_lo + lane);
+    const bool cut = s < 0 || s >= n_slots || (s & (P - 1)) == 0 || slot_of(row_lo + lane - 1) != s - 1;
+    const uint64_t cuts = __ballot(cut);
+    uint64_t begins = __ballot(cut && s >= 0 && s < n_slots && lane < a.chunk);
     for (; begins; begins &= begins - 1) {
-        const int row0 = row_lo + __builtin_ctzll(begins);
-        const int64_t s0 = slot_of(row0);
-        const int o = (int)(s0 & (P - 1));
-        const int64_t page = s0 >> shift;
-        int n = 1;   // rows of the segment: up to the page's end, as long as the slots are consecutive
-        for (int j0 = 1; j0 < P - o; j0 += 64) {
-            const int j = j0 + lane;
-            const uint64_t ends = __ballot(j >= P - o || slot_of(row0 + j) != s0 + j);
-            n = ends ? j0 + __builtin_ctzll(ends) : j0 + 64;
-            if (ends) break;
+        const int at = __builtin_ctzll(begins);
+        Segment sg;
+        sg.row0 = row_lo + at;
+        const int64_t s0 = ((int64_t)__builtin_amdgcn_readlane((int)(s >> 32), at) << 32) | (unsigned)__builtin_amdgcn_readlane((int)s, at);
+        sg.o = (int)(s0 & (P - 1));
+        sg.ph = (size_t)(s0 >> shift) * Hkv + kvh;
+        sg.before = sg.o > 0 ? min(max((int)(wave < 2 ? a.kv.ks : a.kv.vs)[sg.ph], 1), 253) : 1;
+        const uint64_t later = at < 63 ? cuts >> (at + 1) : 0;
+        if (later) {
+            sg.n = __builtin_ctzll(later) + 1;
+        } else {   // (segments of pages of 128 rows, or that begin late in the 64)
+            sg.n = min(64 - at, P - sg.o);
+            while (sg.n < P - sg.o) {
+                const int j = sg.n + lane;
+                const uint64_t ends = __ballot(j >= P - sg.o || slot_of(sg.row0 + j) != s0 + j);
+                sg.n += ends ? __builtin_ctzll(ends) : 64;
+                if (ends) break;
+            }
         }
-        n = min(n, P - o);
-        const size_t ph = (size_t)page * Hkv + kvh;
         __syncthreads();   // (the rows marked for the segment before have been read)
-        if (threadIdx.x < 8) bad_rows[threadIdx.x >> 2][threadIdx.x & 3] = 0;
+        if (threadIdx.x < 4) sh.bad[threadIdx.x] = 0;
         __syncthreads();
-        if (wave == 0) {
-            const int d = lane % LPT * 8, sub = lane / LPT;
-            const T* src = a.qkv + (size_t)row0 * ld + (a.Hq + kvh) * HD + d;
-            auto rotated = [&](int j, float (&lo)[8], float (&hi)[8]) {
-                float x[8], y[8];
-                load8(src + (size_t)j * ld, x);
-                load8(src + (size_t)j * ld + HALF, y);
-                const float2* cs = a.rot + (size_t)(row0 + j) * HALF + d;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) rotate(x[e], y[e], cs[e].x, cs[e].y, lo[e], hi[e]);
-            };
-            float amax = 0.f;
-            for (int j = sub; j < n; j += TPW) {
-                float lo[8], hi[8];
-                rotated(j, lo, hi);
-                bool fine = true;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    fine = fine && finite(lo[e]) && finite(hi[e]);
-                    amax = fmaxf(amax, fmaxf(finite(lo[e]) ? fabsf(lo[e]) : 0.f, finite(hi[e]) ? fabsf(hi[e]) : 0.f));
-                }
-                if (!fine) atomicOr(&bad_rows[0][j >> 5], 1u << (j & 31));
-            }
-            amax = wave_max(amax);
-            __syncthreads();
-            const int before = o > 0 ? min(max((int)a.kv.ks[ph], 1), 253) : 1, byte = max(before, scale_byte(amax));
-            uint8_t* kp = a.kv.k + (ph << shift) * HD;
-            if (byte > before && o > 0) {
-                const float down = e8m0(max(127 + before - byte, 0));
-                for (int i = lane; i < o * (HD / 16); i += 64) {
-                    uintx4 w = reinterpret_cast<uintx4*>(kp)[i];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = recode4(w[e], down);
-                    reinterpret_cast<uintx4*>(kp)[i] = w;
-                }
-            }
-            const float up = e8m0(254 - byte);
-            for (int j = sub; j < n; j += TPW) {
-                float lo[8], hi[8];
-                rotated(j, lo, hi);
-                uintx2 wl = {to_codes4(lo[0] * up, lo[1] * up, lo[2] * up, lo[3] * up), to_codes4(lo[4] * up, lo[5] * up, lo[6] * up, lo[7] * up)};
-                uintx2 wh = {to_codes4(hi[0] * up, hi[1] * up, hi[2] * up, hi[3] * up), to_codes4(hi[4] * up, hi[5] * up, hi[6] * up, hi[7] * up)};
-                if ((bad_rows[0][j >> 5] | bad_rows[1][j >> 5]) >> (j & 31) & 1) wl = wh = uintx2{0x7F7F7F7Fu, 0x7F7F7F7Fu};
-                uint8_t* dst = kp + (size_t)(o + j) * HD + d;
-                *reinterpret_cast<uintx2*>(dst) = wl;
-                *reinterpret_cast<uintx2*>(dst + HALF) = wh;
-            }
-            if (lane == 0) a.kv.ks[ph] = (uint8_t)byte;
-        } else {
-            const int d = lane % VL * 8, sub = lane / VL;
-            const T* src = a.qkv + (size_t)row0 * ld + (a.Hq + Hkv + kvh) * HD + d;
-            float amax = 0.f;
-            for (int j = sub; j < n; j += VG) {
-                float x[8];
-                load8(src + (size_t)j * ld, x);
-                bool fine = true;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    fine = fine && finite(x[e]);
-                    amax = fmaxf(amax, finite(x[e]) ? fabsf(x[e]) : 0.f);
-                }
-                if (!fine) atomicOr(&bad_rows[1][j >> 5], 1u << (j & 31));
-            }
-            amax = wave_max(amax);
-            __syncthreads();
-            const int before = o > 0 ? min(max((int)a.kv.vs[ph], 1), 253) : 1, byte = max(before, scale_byte(amax));
-            uint8_t* vp = a.kv.v + (ph << shift) * HD;
-            if (byte > before && o > 0) {
-                const float down = e8m0(max(127 + before - byte, 0));
-                const int per = (o + PAGED_GRAN - 1) / PAGED_GRAN;   // granules that hold rows of before
-                for (int i = lane; i < per * HD; i += 64) {
-                    uintx4* p = reinterpret_cast<uintx4*>(vp + (size_t)(i / per) * P + i % per * PAGED_GRAN);
-                    uintx4 w = *p;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned rows = low_bytes(o - i % per * PAGED_GRAN - 4 * e);   // (those behind stay as they are)
-                        w[e] = (recode4(w[e], down) & rows) | (w[e] & ~rows);
-                    }
-                    *p = w;
-                }
-                wait_all_memory();   // the granule in which the new rows begin is there before single bytes of it are
-            }
-            const float up = e8m0(254 - byte);
-            for (int g = o / PAGED_GRAN + sub; g * PAGED_GRAN < o + n; g += VG) {
-                const int j0 = g * PAGED_GRAN - o;   // the granule's first row in the segment
-                unsigned w[8][4];                    // [element][row / 4]
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    float x[4][8];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int j = min(max(j0 + q4 * 4 + u, 0), n - 1);
-                        load8(src + (size_t)j * ld, x[u]);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[u][e] = finite(x[u][e]) ? x[u][e] * up : 0.f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e][q4] = to_codes4(x[0][e], x[1][e], x[2][e], x[3][e]);
-                }
-                uint8_t* dst = vp + (size_t)d * P + g * PAGED_GRAN;
-                if (j0 >= 0 && j0 + PAGED_GRAN <= n) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uintx4*>(dst + e * P) = uintx4{w[e][0], w[e][1], w[e][2], w[e][3]};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int u = 0; u < PAGED_GRAN; ++u)
-                            if (j0 + u >= 0 && j0 + u < n) dst[e * P + u] = (uint8_t)(w[e][u >> 2] >> (u & 3) * 8);
-                }
-            }
-            if (lane == 0) a.kv.vs[ph] = (uint8_t)byte;
-        }
+        if (wave < 2)
+            write_k<HD>(a, sg, kvh, wave, sh);
+        else
+            write_v<HD>(a, sg, kvh, wave - 2, sh);
     }
 }
 
@@ -451,8 +594,8 @@ extern "C" int compact_rope_paged_write(compact_ctx* ctx, int32_t n_rows, const 
     PagedView v;
     TRY_RC(paged_view(ctx, kv, true, &v));
     if (!d_qkv || !d_slot || !d_rot || !d_q) return set_err(ctx, COMPACT_EINVAL, "null qkv, slots, rotations or q");
-    if (((uintptr_t)d_qkv | (uintptr_t)d_q) & 15) return set_err(ctx, COMPACT_EINVAL, "qkv and q must be 16-byte aligned");
-    if (((uintptr_t)d_slot | (uintptr_t)d_rot) & 7) return set_err(ctx, COMPACT_EINVAL, "slots and rotations must be 8-byte aligned");
+    if (((uintptr_t)d_qkv | (uintptr_t)d_q | (uintptr_t)d_rot) & 15) return set_err(ctx, COMPACT_EINVAL, "qkv, q and the rotations must be 16-byte aligned");
+    if ((uintptr_t)d_slot & 7) return set_err(ctx, COMPACT_EINVAL, "slots must be 8-byte aligned");
     if (n_rows == 0) return COMPACT_OK;
     const bool b = ctx->cfg.dtype == COMPACT_BF16;
     auto launch = ctx->cfg.head_dim == 128 ? (b ? launch_write<128, bf16> : launch_write<128, float>)
