@@ -248,6 +248,7 @@ struct WriteArgs {
     int n_rows, Hq, Hkv;
     int chunk;            // rows whose segments one workgroup goes through
     int n_kv_wgs;         // workgroups of the K / V part
+    int kv_pitch;
     int q_heads;          // query heads per wavefront of the q part
 };
 
@@ -496,8 +497,10 @@ __global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_ker
     const int Hkv = a.Hkv;
 
     using Eight = Raw<T, 8>;
-    if ((int)blockIdx.x >= a.n_kv_wgs) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
-        const int task = ((int)blockIdx.x - a.n_kv_wgs) * (WR_NT / 64) + wave;
+    // the workgroups of the K / V part, which wait more than they move, lie among those of the q part: every kv_pitch-th one
+    const int kv_wg = blockIdx.x / (unsigned)a.kv_pitch;
+    if (kv_wg * a.kv_pitch != (int)blockIdx.x || kv_wg >= a.n_kv_wgs) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
+        const int task = ((int)blockIdx.x - min(kv_wg + 1, a.n_kv_wgs)) * (WR_NT / 64) + wave;
         const int per_row = (a.Hq + a.q_heads - 1) / a.q_heads;
         const int row = task / per_row * TPW + lane / LPT, h0 = task % per_row * a.q_heads, d = lane % LPT * 8;
         if (row >= a.n_rows) return;
@@ -530,8 +533,8 @@ __global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_ker
 
     // ---- K and V: the segments that begin in this workgroup's rows
     __shared__ WriteShared sh;
-    const int kvh = blockIdx.x % Hkv, shift = a.kv.page_shift, P = 1 << shift;
-    const int row_lo = (int)(blockIdx.x / Hkv) * a.chunk;
+    const int kvh = kv_wg % Hkv, shift = a.kv.page_shift, P = 1 << shift;
+    const int row_lo = kv_wg / Hkv * a.chunk;
     const int64_t n_slots = (int64_t)a.kv.n_pages << shift;
     auto slot_of = [&](int row) { return row >= 0 && row < a.n_rows ? a.slot[row] : (int64_t)-1; };
     // the slots of 64 rows from row_lo on: `cuts` marks those that do not continue the row before them in its page
@@ -574,14 +577,15 @@ static int launch_write(compact_ctx* ctx, int n_rows, const void* qkv, const Pag
                         hipStream_t s) {
     const int Hq = ctx->cfg.n_q_heads, Hkv = ctx->cfg.n_kv_heads;
     constexpr int TPW = 64 / (HD / 16);
-    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 1};
-    a.chunk = n_rows <= 1024 ? 1 : n_rows <= 8192 ? 8 : 32;
+    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 1, 1};
+    a.chunk = n_rows <= 1024 ? 1 : n_rows <= 8192 ? 8 : 64;
     const int64_t chunks = (n_rows + a.chunk - 1) / a.chunk, groups = (n_rows + TPW - 1) / TPW;
     a.q_heads = (int)std::min<int64_t>(WR_QHEADS, std::max<int64_t>(1, groups * Hq / 4096));
     const int64_t tasks = groups * ((Hq + a.q_heads - 1) / a.q_heads);
     const int64_t kv_wgs = chunks * Hkv, wgs = kv_wgs + (tasks + WR_NT / 64 - 1) / (WR_NT / 64);
     if (wgs >= INT32_MAX / WR_NT) return set_err(ctx, COMPACT_ESHAPE, "too many rows for one call");
     a.n_kv_wgs = (int)kv_wgs;
+    a.kv_pitch = (int)(wgs / kv_wgs);
     paged_write_kernel<HD, T><<<(unsigned)wgs, WR_NT, 0, s>>>(a);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
