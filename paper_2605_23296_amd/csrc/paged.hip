@@ -39,44 +39,24 @@ int paged_view(compact_ctx* ctx, const compact_paged_kv* kv, bool with_pages, Pa
 // pages are the first ones that want some, and the first page request i takes is number upto[i] - need[i] from the top of
 // the stack.  Sums saturate at 2^31 - 1 (saturating addition of numbers that are not negative is associative).
 //
-// One launch: every workgroup forms the sums over all requests itself (a request's three numbers stay in LDS) and then
-// handles PLAN_ROWS rows of the slot map and its share of the table and of the stack.  No workgroup reads what another one writes:
-// table columns that are read lie below a request's length, those written above it; stack entries that are read lie below
+// One launch: every workgroup forms the sums over all requests itself (a request's numbers stay in LDS) and then handles its
+// rows of the slot map and its share of the table and of the stack.  No workgroup reads what another one writes: table
+// columns that are read lie below a request's length, those written above it; stack entries that are read lie below
 // n_free, those written above; lengths and counters come in pairs.  Page numbers are copied, never followed, so whatever the
 // device arrays hold, nothing outside them is touched.
 // ---------------------------------------------------------------------------
 #define PLAN_NT 256
-#define PLAN_ROWS 64
+#define PLAN_MAX_ROWS 128   // rows of a workgroup at most
 
 struct PlanArgs {
     compact_paged_step st;
     PagedView kv;
     int half;             // head_dim / 2
+    int rows;             // rows per workgroup, a multiple of PLAN_NT / half
     double log2_theta;
 };
 
 __device__ __forceinline__ int sat_add(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7FFFFFFFu); }
-
-// inclusive saturating sum over the workgroup's threads; `red`: one int per wavefront
-__device__ __forceinline__ int block_scan(int v, int* red, int& total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-    for (int ofs = 1; ofs < 64; ofs <<= 1) {
-        const int u = __shfl_up(v, ofs, 64);
-        if (lane >= ofs) v = sat_add(v, u);
-    }
-    __syncthreads();
-    if (lane == 63) red[w] = v;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < PLAN_NT / 64; ++i) {
-        if (i < w) before = sat_add(before, red[i]);
-        total = sat_add(total, red[i]);
-    }
-    return sat_add(v, before);
-}
 
 // the last i in 0 .. n - 1 with a[i] <= x (a[0] = 0 <= x, a does not decrease)
 __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
@@ -93,48 +73,78 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
 
 __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
     extern __shared__ int lds[];
-    __shared__ int red[PLAN_NT / 64], s_pos[PLAN_ROWS], s_taken, s_refused;
+    __shared__ int red[2][3][PLAN_NT / 64], s_pos[PLAN_MAX_ROWS], s_refused;
     const compact_paged_step& st = a.st;
     const int N = a.kv.n_requests, shift = a.kv.page_shift, P = 1 << shift, width = a.kv.max_pages;
     int* cu = lds;                 // [N + 1] rows before request i
     int* back = cu + N + 1;        // [N + 1] pages given back by the requests before i
     int* want = back + N + 1;      // [N + 1] pages wanted by the requests before i
-    const int t = threadIdx.x;
+    int* len = want + N + 1;       // [N] rows cached, inside the table
+    const int t = threadIdx.x, lane = t & 63, wave = wave_index();
     const int n_free = min(max(st.d_n_free[0], 0), a.kv.n_pages);
     const int cap = width << shift;
-    auto len_of = [&](int i) { return min(max(st.d_len[i], 0), cap); };
     auto pages = [&](int rows) { return (int)(((unsigned)rows + P - 1) >> shift); };
-    // pages request i wants, its rows ending at packed row `end`; -1: it does not fit
-    auto need_of = [&](int n, int len, int end) {
-        if (n > cap - len || end > st.max_rows) return -1;
-        return pages(len + n) - pages(len);
+    // pages a request wants for n > 0 more rows, the last one at packed row `end` - 1; -1: it does not fit
+    auto need_of = [&](int n, int held, int end) {
+        if (n > cap - held || end > st.max_rows) return -1;
+        return pages(held + n) - pages(held);
     };
 
+    // ---- the running sums, 256 requests at a time: `c_` = of the requests before those
     int c_cu = 0, c_back = 0, c_want = 0;
-    for (int i0 = 0; i0 < N; i0 += PLAN_NT) {
+    for (int i0 = 0, turn = 0; i0 < N; i0 += PLAN_NT, turn ^= 1) {
         const int i = i0 + t;
-        const int n_new = i < N ? st.d_n_new[i] : 0, len = i < N ? len_of(i) : 0;
-        const int n = max(n_new, 0);
-        int tot;
-        const int end = sat_add(c_cu, block_scan(n, red, tot));
-        c_cu = sat_add(c_cu, tot);
-        const int gave = sat_add(c_back, block_scan(n_new < 0 ? pages(len) : 0, red, tot));
-        c_back = sat_add(c_back, tot);
-        const int need = n > 0 ? max(need_of(n, len, end), 0) : 0;
-        const int upto = sat_add(c_want, block_scan(need, red, tot));
-        c_want = sat_add(c_want, tot);
+        const int n_new = i < N ? st.d_n_new[i] : 0, held = i < N ? min(max(st.d_len[i], 0), cap) : 0, n = max(n_new, 0);
+        int end = n, gave = n_new < 0 ? pages(held) : 0;
+#pragma unroll
+        for (int ofs = 1; ofs < 64; ofs <<= 1) {
+            const int u = __shfl_up(end, ofs, 64), v = __shfl_up(gave, ofs, 64);
+            if (lane >= ofs) {
+                end = sat_add(end, u);
+                gave = sat_add(gave, v);
+            }
+        }
+        if (lane == 63) {
+            red[turn][0][wave] = end;
+            red[turn][1][wave] = gave;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < PLAN_NT / 64; ++k) {
+            if (k == wave) {
+                end = sat_add(end, c_cu);
+                gave = sat_add(gave, c_back);
+            }
+            c_cu = sat_add(c_cu, red[turn][0][k]);
+            c_back = sat_add(c_back, red[turn][1][k]);
+        }
+        int upto = n > 0 ? max(need_of(n, held, end), 0) : 0;
+#pragma unroll
+        for (int ofs = 1; ofs < 64; ofs <<= 1) {
+            const int u = __shfl_up(upto, ofs, 64);
+            if (lane >= ofs) upto = sat_add(upto, u);
+        }
+        if (lane == 63) red[turn][2][wave] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < PLAN_NT / 64; ++k) {
+            if (k == wave) upto = sat_add(upto, c_want);
+            c_want = sat_add(c_want, red[turn][2][k]);
+        }
         if (i < N) {
             cu[i + 1] = end;
             back[i + 1] = gave;
             want[i + 1] = upto;
+            len[i] = held;
         }
     }
-    if (t == 0) cu[0] = back[0] = want[0] = s_taken = s_refused = 0;
+    if (t == 0) cu[0] = back[0] = want[0] = s_refused = 0;
     __syncthreads();
-    const int total = min(sat_add(n_free, back[N]), a.kv.n_pages);   // pages there are
-    auto granted = [&](int i, int n, int len) {
+    const int total = min(sat_add(n_free, c_back), a.kv.n_pages);   // pages there are
+    auto granted = [&](int i) {
+        const int n = cu[i + 1] - cu[i];
         if (n <= 0) return false;
-        const int need = need_of(n, len, cu[i + 1]);
+        const int need = need_of(n, len[i], cu[i + 1]);
         return need == 0 || (need > 0 && want[i + 1] <= total);
     };
     // the page at position v of the stack once the pages given back lie on it
@@ -143,48 +153,44 @@ __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
         const int i = last_at_most(back, N + 1, v - n_free);
         return a.kv.table[(size_t)i * width + (v - n_free - back[i])];
     };
-    // per request: length, pages taken in all
-    {
-        int taken = 0, refused = 0;
+    // those granted pages are the first ones that want some: they take as many as the largest of the sums that is there
+    const int taken = want[last_at_most(want, N + 1, total)], left = total - taken;
+    if (blockIdx.x == 0) {
+        int refused = 0;
         for (int i = t; i < N; i += PLAN_NT) {
-            const int n_new = st.d_n_new[i], len = len_of(i);
-            const bool ok = granted(i, n_new, len);
-            if (ok && want[i + 1] > want[i]) taken = want[i + 1];   // (they do not decrease)
-            refused += n_new > 0 && !ok;
-            if (blockIdx.x == 0) {
-                st.d_len_out[i] = n_new < 0 ? 0 : ok ? len + n_new : len;
-                st.d_kv_len[i] = ok ? len + n_new : 0;
-                st.d_cu[i + 1] = cu[i + 1];
-                if (i == 0) st.d_cu[0] = 0;
-            }
+            const bool ok = granted(i);
+            const int n = cu[i + 1] - cu[i], held = len[i];
+            refused += !ok && st.d_n_new[i] > 0;   // (where the sum of the rows is at its limit, cu does not show them)
+            st.d_len_out[i] = back[i + 1] > back[i] ? 0 : ok ? held + n : held;   // (finished without a page: held = 0)
+            st.d_kv_len[i] = ok ? held + n : 0;
+            st.d_cu[i + 1] = cu[i + 1];
         }
-        if (taken) atomicMax(&s_taken, taken);
         if (refused) atomicAdd(&s_refused, refused);
-    }
-    __syncthreads();
-    const int taken = s_taken, left = total - taken;
-    if (blockIdx.x == 0 && t == 0) {
-        st.d_n_free_out[0] = left;
-        st.d_n_refused[0] = s_refused;
+        __syncthreads();
+        if (t == 0) {
+            st.d_cu[0] = 0;
+            st.d_n_free_out[0] = left;
+            st.d_n_refused[0] = s_refused;
+        }
     }
     const int gt = blockIdx.x * PLAN_NT + t, all = gridDim.x * PLAN_NT;
     for (int v = n_free + gt; v < left; v += all) st.d_free[v] = stack(v);
     for (int k = gt; k < taken; k += all) {   // the k-th page from the top of the stack
         const int i = last_at_most(want, N + 1, k);
-        a.kv.table[(size_t)i * width + pages(len_of(i)) + (k - want[i])] = stack(total - 1 - k);
+        a.kv.table[(size_t)i * width + pages(len[i]) + (k - want[i])] = stack(total - 1 - k);
     }
 
-    // ---- slot and position of this workgroup's rows, then their rotary angles --------------------
-    const int r0 = blockIdx.x * PLAN_ROWS, rows = min(PLAN_ROWS, st.max_rows - r0);
+    // ---- slot and position of this workgroup's rows
+    const int r0 = blockIdx.x * a.rows, rows = min(a.rows, st.max_rows - r0);
     if (t < rows) {
         const int r = r0 + t;
         int pos = 0;
         int64_t slot = -1;
-        if (r < cu[N]) {
-            const int i = last_at_most(cu, N + 1, r), n = cu[i + 1] - cu[i], len = len_of(i);
-            pos = len + (r - cu[i]);
-            if (granted(i, n, len)) {
-                const int p = pos >> shift, held = pages(len);
+        if (r < c_cu) {
+            const int i = last_at_most(cu, N + 1, r);
+            pos = len[i] + (r - cu[i]);
+            if (granted(i)) {
+                const int p = pos >> shift, held = pages(len[i]);
                 const int page = p < held ? a.kv.table[(size_t)i * width + p] : stack(total - 1 - (want[i] + p - held));
                 slot = (int64_t)page * P + (pos & (P - 1));
             }
@@ -193,13 +199,25 @@ __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
         s_pos[t] = pos;
     }
     __syncthreads();
-    // the angle in fp64, as the framework's other rotations form it; PLAN_NT is a multiple of half: a thread's frequency is fixed
-    const int i = t % a.half;
-    const double inv_freq = exp2(-2.0 * (double)i / (double)(2 * a.half) * a.log2_theta);
-    for (int idx = t; idx < rows * a.half; idx += PLAN_NT) {
-        double sn, cn;
-        sincos((double)s_pos[idx / a.half] * inv_freq, &sn, &cn);
-        reinterpret_cast<float2*>(st.d_rot)[(size_t)r0 * a.half + idx] = make_float2((float)cn, (float)sn);
+    // ---- their rotary angles, in fp64 as the framework's other rotations have them: a thread takes one frequency for a run of
+    // rows.  A row that follows the one before it in its request is that row turned by the frequency once more (four
+    // multiplications in place of a sine and a cosine; 16 turns lose no more than 2^-48)
+    const int run = a.rows * a.half / PLAN_NT, first = t / a.half * run, i = t % a.half;
+    const double freq = exp2(-2.0 * (double)i / (double)(2 * a.half) * a.log2_theta);
+    double c1 = 0.0, s1 = 0.0, cn = 0.0, sn = 0.0;
+    bool turns = false;
+    for (int r = first; r < min(first + run, rows); ++r) {
+        const int pos = s_pos[r];
+        if (r > first && pos == s_pos[r - 1] + 1) {
+            if (!turns) sincos(freq, &s1, &c1);
+            turns = true;
+            const double c = cn * c1 - sn * s1;
+            sn = sn * c1 + cn * s1;
+            cn = c;
+        } else {
+            sincos((double)pos * freq, &sn, &cn);
+        }
+        reinterpret_cast<float2*>(st.d_rot)[(size_t)(r0 + r) * a.half + i] = make_float2((float)cn, (float)sn);
     }
 }
 
@@ -222,8 +240,15 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
     a.st = *step;
     a.half = ctx->cfg.head_dim / 2;
     a.log2_theta = log2((double)ctx->cfg.rope_theta);
-    const size_t smem = (size_t)3 * (kv->n_requests + 1) * sizeof(int);
-    paged_plan_kernel<<<(step->max_rows + PLAN_ROWS - 1) / PLAN_ROWS, PLAN_NT, smem, (hipStream_t)hip_stream>>>(a);
+    // rows per workgroup: one run of a row per thread as long as that gives no more than 256 workgroups, up to 16 beyond, where
+    // consecutive rows are cheap
+    const int at_once = PLAN_NT / a.half;
+    a.rows = at_once;
+    while (a.rows < 16 * at_once && step->max_rows > 256 * a.rows) a.rows *= 2;
+    const size_t smem = (size_t)(4 * kv->n_requests + 3) * sizeof(int);
+    if (smem > (60 << 10))
+        HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(paged_plan_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    paged_plan_kernel<<<(step->max_rows + a.rows - 1) / a.rows, PLAN_NT, smem, (hipStream_t)hip_stream>>>(a);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }
