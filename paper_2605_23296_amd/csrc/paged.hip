@@ -46,7 +46,6 @@ int paged_view(compact_ctx* ctx, const compact_paged_kv* kv, bool with_pages, Pa
 // device arrays hold, nothing outside them is touched.
 // ---------------------------------------------------------------------------
 #define PLAN_NT 256
-#define PLAN_MAX_ROWS 128   // rows of a workgroup at most
 
 struct PlanArgs {
     compact_paged_step st;
@@ -57,6 +56,25 @@ struct PlanArgs {
 };
 
 __device__ __forceinline__ int sat_add(int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7FFFFFFFu); }
+
+// inclusive saturating sum over the lanes of a wavefront: inside rows of 16 lanes, then across them
+__device__ __forceinline__ int wave_scan(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    v = sat_add(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));   // row_shr:1
+    v = sat_add(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+    v = sat_add(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+    v = sat_add(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+    v = sat_add(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));   // row_bcast:15 to rows 1 and 3
+    v = sat_add(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));   // row_bcast:31 to rows 2 and 3
+#endif
+    return v;
+}
+
+// the value of the lane before, 0 in lane 0
+__device__ __forceinline__ int lane_before(int v) {
+    const int u = __shfl_up(v, 1, 64);
+    return (threadIdx.x & 63) ? u : 0;
+}
 
 // the last i in 0 .. n - 1 with a[i] <= x (a[0] = 0 <= x, a does not decrease)
 __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
@@ -73,7 +91,7 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
 
 __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
     extern __shared__ int lds[];
-    __shared__ int red[2][3][PLAN_NT / 64], s_pos[PLAN_MAX_ROWS], s_refused;
+    __shared__ int red[2][3][PLAN_NT / 64], s_refused;
     const compact_paged_step& st = a.st;
     const int N = a.kv.n_requests, shift = a.kv.page_shift, P = 1 << shift, width = a.kv.max_pages;
     int* cu = lds;                 // [N + 1] rows before request i
@@ -90,52 +108,71 @@ __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
         return pages(held + n) - pages(held);
     };
 
-    // ---- the running sums, 256 requests at a time: `c_` = of the requests before those
+    // a thread takes one frequency of the rotary angles; formed while the lengths are on their way
+    const int run = a.rows * a.half / PLAN_NT, my_run = t / a.half * run, my_freq = t % a.half;
+
+    // ---- the running sums, two requests per thread at a time: `c_` = of the requests before those
     int c_cu = 0, c_back = 0, c_want = 0;
-    for (int i0 = 0, turn = 0; i0 < N; i0 += PLAN_NT, turn ^= 1) {
-        const int i = i0 + t;
-        const int n_new = i < N ? st.d_n_new[i] : 0, held = i < N ? min(max(st.d_len[i], 0), cap) : 0, n = max(n_new, 0);
-        int end = n, gave = n_new < 0 ? pages(held) : 0;
+    double freq = 0.0;
+    for (int i0 = 0, turn = 0; i0 < N; i0 += 2 * PLAN_NT, turn ^= 1) {
+        int n_new[2], held[2], end[2], gave[2], upto[2];
 #pragma unroll
-        for (int ofs = 1; ofs < 64; ofs <<= 1) {
-            const int u = __shfl_up(end, ofs, 64), v = __shfl_up(gave, ofs, 64);
-            if (lane >= ofs) {
-                end = sat_add(end, u);
-                gave = sat_add(gave, v);
-            }
+        for (int u = 0; u < 2; ++u) {
+            const int i = i0 + 2 * t + u;
+            n_new[u] = i < N ? st.d_n_new[i] : 0;
+            held[u] = i < N ? st.d_len[i] : 0;
         }
+        if (i0 == 0) freq = exp2(-2.0 * (double)my_freq / (double)(2 * a.half) * a.log2_theta);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            held[u] = min(max(held[u], 0), cap);
+            end[u] = max(n_new[u], 0);
+            gave[u] = n_new[u] < 0 ? pages(held[u]) : 0;
+        }
+        int s_end = wave_scan(sat_add(end[0], end[1])), s_gave = wave_scan(sat_add(gave[0], gave[1]));
         if (lane == 63) {
-            red[turn][0][wave] = end;
-            red[turn][1][wave] = gave;
+            red[turn][0][wave] = s_end;
+            red[turn][1][wave] = s_gave;
         }
+        // sums before the thread's two requests: of the lanes before it, and of the wavefronts before its own
+        s_end = lane_before(s_end);
+        s_gave = lane_before(s_gave);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < PLAN_NT / 64; ++k) {
             if (k == wave) {
-                end = sat_add(end, c_cu);
-                gave = sat_add(gave, c_back);
+                s_end = sat_add(s_end, c_cu);
+                s_gave = sat_add(s_gave, c_back);
             }
             c_cu = sat_add(c_cu, red[turn][0][k]);
             c_back = sat_add(c_back, red[turn][1][k]);
         }
-        int upto = n > 0 ? max(need_of(n, held, end), 0) : 0;
+        end[0] = sat_add(s_end, end[0]);
+        end[1] = sat_add(end[0], end[1]);
+        gave[0] = sat_add(s_gave, gave[0]);
+        gave[1] = sat_add(gave[0], gave[1]);
 #pragma unroll
-        for (int ofs = 1; ofs < 64; ofs <<= 1) {
-            const int u = __shfl_up(upto, ofs, 64);
-            if (lane >= ofs) upto = sat_add(upto, u);
-        }
-        if (lane == 63) red[turn][2][wave] = upto;
+        for (int u = 0; u < 2; ++u) upto[u] = n_new[u] > 0 ? max(need_of(n_new[u], held[u], end[u]), 0) : 0;
+        int s_upto = wave_scan(sat_add(upto[0], upto[1]));
+        if (lane == 63) red[turn][2][wave] = s_upto;
+        s_upto = lane_before(s_upto);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < PLAN_NT / 64; ++k) {
-            if (k == wave) upto = sat_add(upto, c_want);
+            if (k == wave) s_upto = sat_add(s_upto, c_want);
             c_want = sat_add(c_want, red[turn][2][k]);
         }
-        if (i < N) {
-            cu[i + 1] = end;
-            back[i + 1] = gave;
-            want[i + 1] = upto;
-            len[i] = held;
+        upto[0] = sat_add(s_upto, upto[0]);
+        upto[1] = sat_add(upto[0], upto[1]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int i = i0 + 2 * t + u;
+            if (i < N) {
+                cu[i + 1] = end[u];
+                back[i + 1] = gave[u];
+                want[i + 1] = upto[u];
+                len[i] = held[u];
+            }
         }
     }
     if (t == 0) cu[0] = back[0] = want[0] = s_refused = 0;
@@ -180,35 +217,35 @@ __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
         a.kv.table[(size_t)i * width + pages(len[i]) + (k - want[i])] = stack(total - 1 - k);
     }
 
-    // ---- slot and position of this workgroup's rows
+    // ---- slots of this workgroup's rows (their pages' numbers are on their way during the angles)
     const int r0 = blockIdx.x * a.rows, rows = min(a.rows, st.max_rows - r0);
-    if (t < rows) {
-        const int r = r0 + t;
-        int pos = 0;
-        int64_t slot = -1;
-        if (r < c_cu) {
-            const int i = last_at_most(cu, N + 1, r);
-            pos = len[i] + (r - cu[i]);
-            if (granted(i)) {
-                const int p = pos >> shift, held = pages(len[i]);
-                const int page = p < held ? a.kv.table[(size_t)i * width + p] : stack(total - 1 - (want[i] + p - held));
-                slot = (int64_t)page * P + (pos & (P - 1));
-            }
+    int page = -1, in_page = 0;
+    if (t < rows && r0 + t < c_cu) {
+        const int i = last_at_most(cu, N + 1, r0 + t);
+        if (granted(i)) {
+            const int pos = len[i] + (r0 + t - cu[i]), p = pos >> shift, held = pages(len[i]);
+            page = p < held ? a.kv.table[(size_t)i * width + p] : stack(total - 1 - (want[i] + p - held));
+            in_page = pos & (P - 1);
         }
-        st.d_slot[r] = slot;
-        s_pos[t] = pos;
     }
-    __syncthreads();
-    // ---- their rotary angles, in fp64 as the framework's other rotations have them: a thread takes one frequency for a run of
-    // rows.  A row that follows the one before it in its request is that row turned by the frequency once more (four
-    // multiplications in place of a sine and a cosine; 16 turns lose no more than 2^-48)
-    const int run = a.rows * a.half / PLAN_NT, first = t / a.half * run, i = t % a.half;
-    const double freq = exp2(-2.0 * (double)i / (double)(2 * a.half) * a.log2_theta);
+    // ---- rotary angles, in fp64 as the framework's other rotations have them, for a run of rows.  A row that follows the one
+    // before it in its request is that row turned by the frequency once more (four multiplications in place of a sine and a
+    // cosine; 16 turns lose no more than 2^-48)
     double c1 = 0.0, s1 = 0.0, cn = 0.0, sn = 0.0;
     bool turns = false;
-    for (int r = first; r < min(first + run, rows); ++r) {
-        const int pos = s_pos[r];
-        if (r > first && pos == s_pos[r - 1] + 1) {
+    int i = r0 + my_run < c_cu ? last_at_most(cu, N + 1, r0 + my_run) : N;
+    int ends = i < N ? cu[i + 1] : 0x7FFFFFFF, pos = i < N ? len[i] + (r0 + my_run - cu[i]) : 0;
+    for (int r = r0 + my_run; r < min(r0 + my_run + run, r0 + rows); ++r) {
+        bool follows = r > r0 + my_run && i < N;
+        if (r >= ends) {   // the next request that has rows
+            do {
+                ++i;
+            } while (i < N && cu[i + 1] <= r);
+            ends = i < N ? cu[i + 1] : 0x7FFFFFFF;
+            pos = i < N ? len[i] : 0;
+            follows = false;
+        }
+        if (follows) {
             if (!turns) sincos(freq, &s1, &c1);
             turns = true;
             const double c = cn * c1 - sn * s1;
@@ -217,8 +254,10 @@ __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
         } else {
             sincos((double)pos * freq, &sn, &cn);
         }
-        reinterpret_cast<float2*>(st.d_rot)[(size_t)(r0 + r) * a.half + i] = make_float2((float)cn, (float)sn);
+        reinterpret_cast<float2*>(st.d_rot)[(size_t)r * a.half + my_freq] = make_float2((float)cn, (float)sn);
+        pos += i < N;
     }
+    if (t < rows) st.d_slot[r0 + t] = page < 0 ? -1 : (int64_t)page * P + in_page;
 }
 
 extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, const compact_paged_step* step, void* hip_stream) {
