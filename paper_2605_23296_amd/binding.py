@@ -138,6 +138,16 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _addr(t):
+    assert t.is_contiguous()
+    return t.data_ptr()
+
+
+def _raw_stream():
+    # (0.3 us; torch.cuda.current_stream().cuda_stream takes 2.7, half of a small call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
 def _i32arr(vals):
     return (C.c_int32 * len(vals))(*[int(v) for v in vals])
 
@@ -205,6 +215,7 @@ class PagedKV:
         assert table.dtype == torch.int32 and table.is_contiguous()
         self.c = PagedKVStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), self.n_pages,
                                self.page_rows, self.max_pages, self.n_requests)
+        self.ref = C.byref(self.c)
 
     @classmethod
     def allocate(cls, layer, n_requests, max_pages, n_pages, page_rows, device):
@@ -240,12 +251,19 @@ class PagedStep:
         self.slot = torch.empty(max_rows, dtype=torch.int64, device=device)
         self.rot = torch.empty((max_rows, layer.head_dim // 2, 2), dtype=torch.float32, device=device)
         self.n_requests, self.max_rows = n_requests, max_rows
-        assert self.n_new.numel() == n_requests and self.len.numel() == n_requests
-        assert all(x.dtype == torch.int32 for x in (self.n_new, self.len, self.free, self.n_free))
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_c", None)   # (made again by the next call)
 
     def struct(self):
-        return PagedStepStruct(*[x.data_ptr() for x in (self.n_new, self.len, self.n_free, self.free, self.n_free_out, self.n_refused,
-                                                        self.len_out, self.kv_len, self.cu, self.slot, self.rot)], self.max_rows)
+        if self._c is None:
+            arrays = (self.n_new, self.len, self.n_free, self.free, self.n_free_out, self.n_refused, self.len_out, self.kv_len, self.cu,
+                      self.slot, self.rot)
+            assert self.n_new.numel() == self.n_requests and self.len.numel() == self.n_requests
+            assert all(x.is_contiguous() and x.dtype == d for x, d in zip(arrays, [torch.int32] * 9 + [torch.int64, torch.float32]))
+            object.__setattr__(self, "_c", PagedStepStruct(*[x.data_ptr() for x in arrays], self.max_rows))
+        return self._c
 
     def advance(self):
         """After a step: its lengths and its stack are the next one's."""
@@ -409,11 +427,11 @@ class Layer:
     # -- paged cache in 8 bits ------------------------------------------------------
     def compact_paged_plan(self, kv, step):
         assert step.n_requests == kv.n_requests and step.free.numel() >= kv.n_pages
-        self.check(self.L.compact_paged_plan(self.ctx, C.byref(kv.c), C.byref(step.struct()), _stream()))
+        self.check(self.L.compact_paged_plan(self.ctx, kv.ref, C.byref(step.struct()), _raw_stream()))
 
     def compact_rope_paged_write(self, qkv, kv, slot, rot, q):
         """qkv [rows, Dq + 2 Dkv] -> q [rows, Dq] (rotated), k and v into kv's pages at slot [rows]."""
-        self.check(self.L.compact_rope_paged_write(self.ctx, qkv.shape[0], _ptr(qkv), C.byref(kv.c), _ptr(slot), _ptr(rot), _ptr(q), _stream()))
+        self.check(self.L.compact_rope_paged_write(self.ctx, qkv.shape[0], _addr(qkv), kv.ref, _addr(slot), _addr(rot), _addr(q), _raw_stream()))
 
     def paged_workspace_bytes(self, n_requests, n_rows, max_new, max_kv_len):
         n = C.c_size_t()
@@ -428,10 +446,11 @@ class Layer:
 
     def compact_attn_paged(self, q, kv, cu, kv_len, max_new, max_kv_len, o):
         """q [rows, >= Dq] (its rows may be apart), o [rows, Dq]."""
-        assert q.stride(1) == 1
-        wsp, wsn = self._ws()
-        self.check(self.L.compact_attn_paged(self.ctx, C.byref(kv.c), q.shape[0], _ptr(cu), _ptr(kv_len), max_new, max_kv_len,
-                                             C.c_void_p(q.data_ptr()), q.stride(0), _ptr(o), wsp, wsn, _stream()))
+        rows, stride = q.shape[0], q.stride()
+        assert stride[1] == 1
+        ws = self.ws
+        self.check(self.L.compact_attn_paged(self.ctx, kv.ref, rows, _addr(cu), _addr(kv_len), max_new, max_kv_len, q.data_ptr(), stride[0],
+                                             _addr(o), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream()))
 
     # -- profiling --------------------------------------------------------------
     def compact_profile_select(self, klass):

@@ -549,12 +549,12 @@ extern "C" int compact_attn_paged(compact_ctx* ctx, const compact_paged_kv* kv, 
     PagedAttnArgs a{};
     TRY_RC(paged_view(ctx, kv, true, &a.kv));
     TRY_RC(check_bounds(ctx, kv->n_requests, n_rows, max_new, max_kv_len));
+    if (n_rows == 0) return COMPACT_OK;
     if (!d_cu || !d_kv_len || !d_q || !d_o) return set_err(ctx, COMPACT_EINVAL, "null cu, kv_len, q or o");
     const compact_layer_cfg& c = ctx->cfg;
     if (q_stride < (int64_t)c.n_q_heads * c.head_dim || q_stride % 8 != 0)
         return set_err(ctx, COMPACT_EINVAL, "q_stride must be at least n_q_heads * head_dim and a multiple of 8");
     if (((uintptr_t)d_q | (uintptr_t)d_o) & 15) return set_err(ctx, COMPACT_EINVAL, "q and o must be 16-byte aligned");
-    if (n_rows == 0) return COMPACT_OK;
     max_new = std::min(max_new, n_rows);
     if (!d_workspace || ((uintptr_t)d_workspace & 15) || ws_bytes < paged_workspace(c, kv->n_requests, max_new, max_kv_len))
         return set_err(ctx, COMPACT_EWORKSPACE, "workspace missing, not 16-byte aligned or too small for the paged attention");

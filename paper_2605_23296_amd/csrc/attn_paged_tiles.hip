@@ -601,7 +601,10 @@ template <int HD>
 static int launch_tiles(compact_ctx* ctx, const PagedAttnArgs& a, bool b, hipStream_t s) {
     auto kern = b ? attn_paged_tile_kernel<HD> : attn_paged_tile_f32_kernel<HD>;
     const size_t smem = (size_t)4 * TILE_KEYS * HD * sizeof(bf16);
-    HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (!ctx->paged_lds_set) {   // (a context has one storage type and head_dim: one of the kernels)
+        HIP_TRY(ctx, hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        ctx->paged_lds_set = true;
+    }
     int n_cus = 0;
     if (int rc = device_cu_count(ctx, &n_cus)) return rc;
     ProfileScope ps(ctx, COMPACT_K_ATTN_PREFILL, s);

@@ -84,6 +84,7 @@ struct compact_ctx {
     int64_t prof_launches = 0;
     double prof_ms = 0.0;
     int n_cus = 0;                       // compute units of the device, 0 = not looked up yet
+    bool paged_lds_set = false;          // the paged attention's tile kernel may use the LDS it needs
 };
 
 // RAII-free helper used by launchers: brackets a launch with events when its

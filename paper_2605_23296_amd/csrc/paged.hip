@@ -661,10 +661,10 @@ extern "C" int compact_rope_paged_write(compact_ctx* ctx, int32_t n_rows, const 
     if (n_rows < 0) return set_err(ctx, COMPACT_EINVAL, "n_rows must be >= 0");
     PagedView v;
     TRY_RC(paged_view(ctx, kv, true, &v));
+    if (n_rows == 0) return COMPACT_OK;
     if (!d_qkv || !d_slot || !d_rot || !d_q) return set_err(ctx, COMPACT_EINVAL, "null qkv, slots, rotations or q");
     if (((uintptr_t)d_qkv | (uintptr_t)d_q | (uintptr_t)d_rot) & 15) return set_err(ctx, COMPACT_EINVAL, "qkv, q and the rotations must be 16-byte aligned");
     if ((uintptr_t)d_slot & 7) return set_err(ctx, COMPACT_EINVAL, "slots must be 8-byte aligned");
-    if (n_rows == 0) return COMPACT_OK;
     const bool b = ctx->cfg.dtype == COMPACT_BF16;
     auto launch = ctx->cfg.head_dim == 128 ? (b ? launch_write<128, bf16> : launch_write<128, float>)
                                            : (b ? launch_write<64, bf16> : launch_write<64, float>);
