@@ -345,6 +345,14 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Raw {
     }
 };
 
+// The rotation of a pair, with what the rounded product leaves behind added again: within one rounding of the exact values, so that
+// hardly a code is another one than theirs.
+__device__ __forceinline__ void rotate_closely(float lo, float hi, float c, float s, float& olo, float& ohi) {
+    const float p = hi * s, q = lo * s;
+    olo = fmaf(lo, c, -p) - fmaf(hi, s, -p);
+    ohi = fmaf(hi, c, q) + fmaf(lo, s, -q);
+}
+
 // Sizes as the bits of a float without its sign: they order like the values, and what is not finite lies at INF_BITS and above.
 #define INF_BITS 0x7F800000u
 __device__ __forceinline__ unsigned size_bits(float x) { return __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu; }
@@ -392,7 +400,7 @@ __device__ __forceinline__ void write_k(const WriteArgs<T>& a, const Segment& sg
     auto rotated = [&](int g, int j, float (&lo)[8], float (&hi)[8]) {
         const Raw<float, 16> cs = *reinterpret_cast<const Raw<float, 16>*>(rot + ((unsigned)min(j, sg.n - 1) * HALF + d));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rotate(x[g].at(e), y[g].at(e), cs.at(2 * e), cs.at(2 * e + 1), lo[e], hi[e]);
+        for (int e = 0; e < 8; ++e) rotate_closely(x[g].at(e), y[g].at(e), cs.at(2 * e), cs.at(2 * e + 1), lo[e], hi[e]);
     };
     unsigned top = 0;
     int j0 = 0;
