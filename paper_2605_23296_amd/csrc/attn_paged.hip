@@ -392,75 +392,86 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
 }
 
 // ---------------------------------------------------------------------------
-// Joins the pieces of the (row, query head) pairs of split requests: WAVES wavefronts each, HD / 4 lanes span a record, and a
-// lane sends for MERGE_FLIGHT records before it uses one.  One wavefront where it can send for all of a request's records at
-// once, four beyond (up to 32 pieces of head_dim 64: 7.2 us with four, 4.0 with one).
+// Joins the pieces of the (row, query head) pairs of split requests.  HD / 4 lanes span a record; a lane sends for up to
+// MERGE_FLIGHT records before it uses one.  A request whose records one wavefront can send for at once has a wavefront per pair
+// (32 pieces of head_dim 64: 4.0 us instead of 7.2), one with more of them all four wavefronts of the workgroup.
 // ---------------------------------------------------------------------------
 #define MERGE_FLIGHT 8
+
+// WAVES wavefronts join one pair
 template <int HD, int WAVES, typename T>
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnArgs a, int rows_per_req, int heads_per_wg) {
+__device__ __forceinline__ void merge_pair(const PagedAttnArgs& a, const PagedReq& rq, int req, int row, int head, int pieces, floatx4* part) {
     constexpr int TPR = HD / 4, NS = 64 / TPR, STEP = NS * WAVES;   // lanes per record, records side by side
-    constexpr int PAIRS = 4 / WAVES;                                  // pairs that a workgroup has in hand at a time
-    __shared__ floatx4 part[WAVES == 1 ? 1 : WAVES * TPR];
-    const int lane = threadIdx.x & 63, wave = wave_index(), G = a.Hq / a.Hkv;
+    const int lane = threadIdx.x & 63, wave = wave_index();
+    const int sub = WAVES == 1 ? lane / TPR : wave * NS + lane / TPR, e4 = lane % TPR;
+    const int64_t rec = ((int64_t)req * a.rec_stride + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces;
+    const floatx4* val = reinterpret_cast<const floatx4*>(a.rec + rec * HD) + e4;
+    const float2* ml = reinterpret_cast<const float2*>(a.rec + a.n_rec * HD) + rec;
+    floatx4 v[MERGE_FLIGHT];
+    float2 w[MERGE_FLIGHT];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < MERGE_FLIGHT; ++u)
+            if (i0 + u * STEP < pieces) {
+                const int i = min(i0 + u * STEP + sub, pieces - 1);
+                v[u] = val[(size_t)i * TPR];
+                w[u] = ml[i];
+            }
+    };
+    load(0);
+    float m = -3e38f, l = 0.f;
+    for (int i = lane; i < pieces; i += 64) m = fmaxf(m, ml[i].x);
+    m = wave_max(m);
+    for (int i = lane; i < pieces; i += 64) l += exp2_fast(ml[i].x - m) * ml[i].y;
+    l = wave_sum(l);
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0;;) {
+#pragma unroll
+        for (int u = 0; u < MERGE_FLIGHT; ++u)
+            if (i0 + u * STEP < pieces) {
+                const float f = i0 + u * STEP + sub < pieces ? exp2_fast(w[u].x - m) : 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += f != 0.f ? f * v[u][e] : 0.f;
+            }
+        i0 += MERGE_FLIGHT * STEP;
+        if (i0 >= pieces) break;
+        load(i0);
+    }
+#pragma unroll
+    for (int ofs = TPR; ofs < 64; ofs <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], ofs, 64);
+    if (WAVES > 1) {
+        __syncthreads();
+        if (lane < TPR) part[wave * TPR + lane] = acc;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += part[i * TPR + e4][e];
+    }
+    if (lane < TPR) {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        put4((T*)a.o + ((size_t)(rq.row0 + row) * a.Hq + head) * HD + lane * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    }
+}
+
+template <int HD, typename T>
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnArgs a, int rows_per_req, int heads_per_wg) {
+    __shared__ floatx4 part[HD];
+    const int G = a.Hq / a.Hkv;
     const int per_row = (a.Hq + heads_per_wg - 1) / heads_per_wg;
-    const int id = blockIdx.x / per_row, h_lo = blockIdx.x % per_row * heads_per_wg;
+    const int id = blockIdx.x / per_row, h_lo = blockIdx.x % per_row * heads_per_wg, h_end = min(h_lo + heads_per_wg, a.Hq);
     const int row = id % rows_per_req, req = id / rows_per_req;
     const PagedReq rq = paged_req(a, req);
     if (row >= rq.n) return;
     const int pieces = is_few(rq.n, G) ? few_pieces(rq.kv) : tile_pieces(n_tiles(rq.n, G), rq.kv);
     if (pieces == 1) return;   // written by the kernel before
-    const int sub = WAVES == 1 ? lane / TPR : wave * NS + lane / TPR, e4 = lane % TPR;
-    for (int head = h_lo + wave / WAVES; head < min(h_lo + heads_per_wg, a.Hq); head += PAIRS) {
-        const int64_t rec = ((int64_t)req * a.rec_stride + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces;
-        const floatx4* val = reinterpret_cast<const floatx4*>(a.rec + rec * HD) + e4;
-        const float2* ml = reinterpret_cast<const float2*>(a.rec + a.n_rec * HD) + rec;
-        floatx4 v[MERGE_FLIGHT];
-        float2 w[MERGE_FLIGHT];
-        auto load = [&](int i0) {
-#pragma unroll
-            for (int u = 0; u < MERGE_FLIGHT; ++u) {
-                const int i = min(i0 + u * STEP + sub, pieces - 1);
-                v[u] = val[(size_t)i * TPR];
-                w[u] = ml[i];
-            }
-        };
-        load(0);
-        float m = -3e38f, l = 0.f;
-        for (int i = lane; i < pieces; i += 64) m = fmaxf(m, ml[i].x);
-        m = wave_max(m);
-        for (int i = lane; i < pieces; i += 64) l += exp2_fast(ml[i].x - m) * ml[i].y;
-        l = wave_sum(l);
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int i0 = 0;;) {
-#pragma unroll
-            for (int u = 0; u < MERGE_FLIGHT; ++u) {
-                const float f = i0 + u * STEP + sub < pieces ? exp2_fast(w[u].x - m) : 0.f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += f != 0.f ? f * v[u][e] : 0.f;
-            }
-            i0 += MERGE_FLIGHT * STEP;
-            if (i0 >= pieces) break;
-            load(i0);
-        }
-#pragma unroll
-        for (int ofs = TPR; ofs < 64; ofs <<= 1)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], ofs, 64);
-        if (WAVES > 1) {
-            __syncthreads();
-            if (lane < TPR) part[wave * TPR + lane] = acc;
-            __syncthreads();
-            if (wave > 0) continue;
-#pragma unroll
-            for (int i = 1; i < WAVES; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += part[i * TPR + e4][e];
-        }
-        if (lane < TPR) {
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
-            put4((T*)a.o + ((size_t)(rq.row0 + row) * a.Hq + head) * HD + lane * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-        }
+    if (pieces <= MERGE_FLIGHT * (256 / HD)) {
+        for (int head = h_lo + wave_index(); head < h_end; head += 4) merge_pair<HD, 1, T>(a, rq, req, row, head, pieces, part);
+    } else {
+        for (int head = h_lo; head < h_end; ++head) merge_pair<HD, 4, T>(a, rq, req, row, head, pieces, part);
     }
 }
 
@@ -529,15 +540,13 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     // rows of a request whose keys may be split: 512 t * 2 <= max_kv for its t tiles
     const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * (a.max_kv / TILE_SPLIT / 2) / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
-    const int most_pieces = std::max((a.max_kv - 1) / FEW_CHUNK + 1, tiles ? a.max_kv / TILE_SPLIT : 0);
-    const int pairs = most_pieces > MERGE_FLIGHT * (256 / HD) ? 1 : 4;   // side by side in a workgroup
-    // (workgroups of rows that are not split leave at once: no more than some thousand of them)
-    int heads = pairs;
-    while (heads < c.n_q_heads && rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads) > 4096) heads *= 2;
+    // query heads per workgroup: one while that gives no more than some thousand workgroups, else four and more (those of rows
+    // that are not split leave at once)
+    int heads = 1;
+    while (heads < c.n_q_heads && rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads) > 4096) heads = std::max(4, 2 * heads);
     const int64_t wgs = rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads);
     if (wgs >= INT32_MAX / 256) return set_err(ctx, COMPACT_ESHAPE, "too many rows of split requests for one call");
-    auto merge = pairs == 1 ? attn_paged_merge_kernel<HD, 4, T> : attn_paged_merge_kernel<HD, 1, T>;
-    merge<<<(unsigned)wgs, 256, 0, s>>>(a, (int)rows, heads);
+    attn_paged_merge_kernel<HD, T><<<(unsigned)wgs, 256, 0, s>>>(a, (int)rows, heads);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }
