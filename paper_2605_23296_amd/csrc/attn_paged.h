@@ -9,7 +9,9 @@
 #define TILE_COLS 128    // query columns of a tile of the other kernel
 #define TILE_KEYS 64     // cached rows of a step of it
 #define SCHED_PITCH 32   // ints between the XCDs' counters: a 128-byte line each
-#define SCHED_UNITS (8 * SCHED_PITCH)
+#define SCHED_LISTED 1   // (in the first counter's line) requests in the schedule
+#define SCHED_ORDER (8 * SCHED_PITCH)                      // [listed] those requests
+#define SCHED_UNITS (SCHED_ORDER + PAGED_MAX_REQUESTS)     // [listed + 1] units before each of them
 #define SCHED_BYTES (sizeof(int32_t) * (SCHED_UNITS + PAGED_MAX_REQUESTS + 1))
 #define TILE_SPLIT 512   // a request of t tiles has its keys cut into pieces of 512 t to 1024 t rows
 
@@ -26,7 +28,7 @@ struct PagedAttnArgs {
     float* rec;
     int64_t rec_stride;       // row-pieces of a request
     int64_t n_rec;            // records in all
-    int32_t* sched;           // tile kernel: units taken per XCD (SCHED_PITCH apart), then [N + 1] units before request i
+    int32_t* sched;           // the tile kernel's schedule: units taken per XCD (SCHED_PITCH apart), requests, units before them
 };
 
 struct PagedReq {

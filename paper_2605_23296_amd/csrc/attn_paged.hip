@@ -72,27 +72,56 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
     const int r = lane & 15, c = lane >> 4, r_row = r / G, r_head = r % G;
     const int shift = a.kv.page_shift, P = 1 << shift;
 
-    // ---- the other kernel's schedule: units (tile, piece) before every request, nothing taken yet ----
-    if (TILES && blockIdx.x == 0) {
-        int before = 0;
-        for (int i0 = 0; i0 < N; i0 += FEW_WAVES * 64) {
-            const int i = i0 + t;
-            int units = 0;
-            if (i < N) {
-                const PagedReq rq = paged_req(a, i);
-                if (rq.n > 0 && !is_few(rq.n, G)) {
-                    const int tiles = n_tiles(rq.n, G);
-                    units = tiles * tile_pieces(tiles, rq.kv);
-                }
+    // ---- the other kernel's schedule: the requests with the longest units first (by the first two bits of their keys' number:
+    // what comes last is short), units before every one of them, nothing taken yet ----
+    if constexpr (TILES) {
+        __shared__ int bucket[128];
+        __shared__ uint16_t order[PAGED_MAX_REQUESTS];
+        if (blockIdx.x == 0) {
+            auto units_of = [&](const PagedReq& rq, int& length) {
+                if (rq.n <= 0 || is_few(rq.n, G)) return 0;
+                const int tiles = n_tiles(rq.n, G), pieces = tile_pieces(tiles, rq.kv);
+                length = rq.kv / pieces;
+                return tiles * pieces;
+            };
+            auto bucket_of = [](int length) { return 127 - (int)min(__builtin_bit_cast(unsigned, (float)length) >> 21, 639u) + 508; };   // 1 .. 2^31
+            if (t < 128) bucket[t] = 0;
+            __syncthreads();
+            for (int i = t; i < N; i += FEW_WAVES * 64) {
+                int length = 0;
+                if (units_of(paged_req(a, i), length)) atomicAdd(&bucket[bucket_of(max(length, 1))], 1);
             }
-            int all;
-            const int upto = block_prefix(units, red, all);
-            if (i < N) a.sched[SCHED_UNITS + i + 1] = before + upto;
-            before += all;
+            __syncthreads();
+            int n_listed;
+            {
+                const int n = t < 128 ? bucket[t] : 0, upto = block_prefix(n, red, n_listed);
+                __syncthreads();
+                if (t < 128) bucket[t] = upto - n;
+            }
+            __syncthreads();
+            for (int i = t; i < N; i += FEW_WAVES * 64) {
+                int length = 0;
+                if (units_of(paged_req(a, i), length)) order[atomicAdd(&bucket[bucket_of(max(length, 1))], 1)] = (uint16_t)i;
+            }
+            __syncthreads();
+            int before = 0;
+            for (int k0 = 0; k0 < n_listed; k0 += FEW_WAVES * 64) {
+                const int k = k0 + t, req = k < n_listed ? order[k] : 0;
+                int length, all;
+                const int upto = block_prefix(k < n_listed ? units_of(paged_req(a, req), length) : 0, red, all);
+                if (k < n_listed) {
+                    a.sched[SCHED_UNITS + k + 1] = before + upto;
+                    a.sched[SCHED_ORDER + k] = req;
+                }
+                before += all;
+            }
+            if (t == 0) {
+                a.sched[SCHED_UNITS] = 0;
+                a.sched[SCHED_LISTED] = n_listed;
+            }
+            if (t < 8) a.sched[t * SCHED_PITCH] = 0;
+            __syncthreads();
         }
-        if (t == 0) a.sched[SCHED_UNITS] = 0;
-        if (t < 8) a.sched[t * SCHED_PITCH] = 0;
-        __syncthreads();
     }
 
     // ---- this workgroup's share: items are numbered by request, KV head, chunk.  Every wavefront goes over the requests by

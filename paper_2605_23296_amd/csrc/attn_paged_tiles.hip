@@ -51,20 +51,21 @@ __device__ __forceinline__ int next_place(const PagedAttnArgs& a, int mine, int 
 __device__ __forceinline__ Unit unit_at(const PagedAttnArgs& a, int mine, int units, int xcd_heads) {
     Unit un;
     const int r = threadIdx.x & 31, lane = threadIdx.x & 63, wave = wave_index(), x = blockIdx.x & 7;
-    const int G = a.Hq / a.Hkv, N = a.kv.n_requests;
+    const int G = a.Hq / a.Hkv, N = a.sched[SCHED_LISTED];
     const int32_t* before = a.sched + SCHED_UNITS;
     const int at = mine * (8 / xcd_heads) + x / xcd_heads;
     const int unit = at % units;
     un.kvh = at / units * xcd_heads + x % xcd_heads;
-    int req = 0;   // the last request with no more than `unit` units before it
+    int k = 0;   // the last request in the schedule with no more than `unit` units before it
     for (int i0 = 0; i0 < N; i0 += 64) {
         const uint64_t upto = __ballot(i0 + lane < N && before[min(i0 + lane, N)] <= unit);
         if (upto == 0) break;
-        req = i0 + 63 - __builtin_clzll(upto);
+        k = i0 + 63 - __builtin_clzll(upto);
     }
+    const int req = a.sched[SCHED_ORDER + k];
     un.req = req;
     const PagedReq rq = un.rq = paged_req(a, req);
-    const int tiles = n_tiles(rq.n, G), in_req = unit - before[req];
+    const int tiles = n_tiles(rq.n, G), in_req = unit - before[k];
     un.pieces = tile_pieces(tiles, rq.kv);
     const int tile = tiles - 1 - in_req / un.pieces, c0 = tile * TILE_COLS;   // most keys first
     un.piece = in_req % un.pieces;
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(256, 1) void attn_paged_tile_f32_kernel(const Paged
     const int t = threadIdx.x, lane = t & 63;
     const int r = lane & 31, h = lane >> 5;
     const int shift = a.kv.page_shift, P = 1 << shift;
-    const int units = a.sched[SCHED_UNITS + a.kv.n_requests];
+    const int units = a.sched[SCHED_UNITS + a.sched[SCHED_LISTED]];
     const int pi_r = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
 
     const int n_mine = units_of_xcd(blockIdx.x & 7, units, Hkv, xcd_heads);
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedAttn
     const int t = threadIdx.x, lane = t & 63, wave = wave_index();
     const int r = lane & 31, h = lane >> 5;
     const int shift = a.kv.page_shift, P = 1 << shift;
-    const int units = a.sched[SCHED_UNITS + a.kv.n_requests];
+    const int units = a.sched[SCHED_UNITS + a.sched[SCHED_LISTED]];
     const int pi_r = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
     const float scale_log2 = a.scale_log2;
 
