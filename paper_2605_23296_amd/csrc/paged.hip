@@ -296,8 +296,12 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
 // Write.  A segment is what a call writes to one page: rows with consecutive slots.  A workgroup of four wavefronts takes a
 // segment and KV head: two of them its K rows (rotated on the way), two its V rows (transposed in registers: a lane holds
 // 16 rows of 4 elements, a granule, and stores 16 bytes per element).  Up to 64 rows (fp32 storage: 32 K rows) are read once and kept
-// in registers until the scale is known; of a longer segment all but the last rows are read a second time.
+// in registers until the scale is known; of a longer segment all but the last rows are read a second time.  Segments of one row
+// (decode steps) go four and more side by side in a wavefront, without a barrier (200 of them: 13.7 -> 8.3 us).
 // Further workgroups rotate q.
+// Bound by HBM from some thousand rows on: every row is read once, q and the codes are written once (8 x 4096 rows of 32 + 16
+// heads of 128: 755 MB in 146 us, 5.2 TB/s, where a copy reaches 4.9 and a sum 6.2); by the launch and one chain of
+// dependent loads (slot, scale, row) below: 24 decode rows 6.3 us.
 // ---------------------------------------------------------------------------
 #define WR_NT 256
 #define WR_QHEADS 8   // most query heads per wavefront of the q part
@@ -311,8 +315,7 @@ struct WriteArgs {
     PagedView kv;
     int n_rows, Hq, Hkv;
     int chunk;            // rows whose segments one workgroup goes through
-    int n_kv_wgs;         // workgroups of the K / V part
-    int kv_pitch;
+    uint64_t kv_share;    // share of the workgroups that do K and V, times 2^32 (rounded up)
     int q_heads;          // query heads per wavefront of the q part
 };
 
@@ -562,6 +565,85 @@ __device__ __forceinline__ void write_v(const WriteArgs<T>& a, const Segment& sg
     if (lane + 64 * half == 0) a.kv.vs[sg.ph] = (uint8_t)byte;
 }
 
+// One row that is a segment by itself (a decode step), K and V, by HD / 8 lanes.  Nothing is read that the row does not need: its V
+// codes are stored byte by byte, and earlier rows are touched only where a scale grows.
+template <int HD, typename T>
+__device__ __forceinline__ void write_single(const WriteArgs<T>& a, int row, int64_t slot, int kvh) {
+    constexpr int HALF = HD / 2, LANES = HD / 8;
+    const int l = threadIdx.x % LANES, shift = a.kv.page_shift, o = (int)(slot & ((1 << shift) - 1));
+    const size_t ph = (size_t)(slot >> shift) * a.Hkv + kvh;
+    const T* src = a.qkv + (size_t)row * ((a.Hq + 2 * a.Hkv) * HD) + (a.Hq + kvh) * HD;
+    const Raw<T, 4> x = *reinterpret_cast<const Raw<T, 4>*>(src + l * 4), y = *reinterpret_cast<const Raw<T, 4>*>(src + HALF + l * 4);
+    const Raw<T, 8> v = *reinterpret_cast<const Raw<T, 8>*>(src + a.Hkv * HD + l * 8);
+    const Raw<float, 8> cs = *reinterpret_cast<const Raw<float, 8>*>(a.rot + (size_t)row * HALF + l * 4);
+    const int k_before = o > 0 ? min(max((int)a.kv.ks[ph], 1), 253) : 1, v_before = o > 0 ? min(max((int)a.kv.vs[ph], 1), 253) : 1;
+    float k[8], val[8];
+    unsigned k_top = 0, v_top = 0;
+    int bad = 0;
+    auto see = [&](float f, unsigned& top) {
+        const unsigned size = size_bits(f);
+        bad |= size >= INF_BITS;
+        top = max(top, size < INF_BITS ? size : 0u);
+        return size < INF_BITS ? f : 0.f;
+    };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rotate_closely(x.at(e), y.at(e), cs.at(2 * e), cs.at(2 * e + 1), k[e], k[4 + e]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        see(k[e], k_top);
+        val[e] = see(v.at(e), v_top);
+    }
+#pragma unroll
+    for (int ofs = LANES / 2; ofs > 0; ofs >>= 1) {
+        k_top = max(k_top, (unsigned)__shfl_xor((int)k_top, ofs, 64));
+        v_top = max(v_top, (unsigned)__shfl_xor((int)v_top, ofs, 64));
+        bad |= __shfl_xor(bad, ofs, 64);
+    }
+    const int k_byte = max(k_before, scale_byte(__builtin_bit_cast(float, k_top))), v_byte = max(v_before, scale_byte(__builtin_bit_cast(float, v_top)));
+    const float k_up = e8m0(254 - k_byte), v_up = e8m0(254 - v_byte);
+    uint8_t* kp = a.kv.k + (ph << shift) * HD;
+    uint8_t* vp = a.kv.v + (ph << shift) * HD + ((size_t)(l * 8) << shift);
+    if (k_byte > k_before && o > 0) {
+        const float down = e8m0(max(127 + k_before - k_byte, 0));
+        for (int i = l; i < o * (HD / 16); i += LANES) {
+            uintx4 w = reinterpret_cast<uintx4*>(kp)[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = recode4(w[e], down);
+            reinterpret_cast<uintx4*>(kp)[i] = w;
+        }
+    }
+    unsigned wl = to_codes4(k[0] * k_up, k[1] * k_up, k[2] * k_up, k[3] * k_up), wh = to_codes4(k[4] * k_up, k[5] * k_up, k[6] * k_up, k[7] * k_up);
+    if (bad) wl = wh = 0x7F7F7F7Fu;
+    *reinterpret_cast<unsigned*>(kp + o * HD + l * 4) = wl;
+    *reinterpret_cast<unsigned*>(kp + o * HD + HALF + l * 4) = wh;
+    unsigned code[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) code[u] = to_codes4(val[4 * u] * v_up, val[4 * u + 1] * v_up, val[4 * u + 2] * v_up, val[4 * u + 3] * v_up);
+    if (v_byte > v_before && o > 0) {   // the lane's elements of the earlier rows, granule by granule
+        const float down = e8m0(max(127 + v_before - v_byte, 0));
+        for (int g = 0; g * PAGED_GRAN < o; ++g) {
+            uintx4 w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uintx4*>(vp + (e << shift) + g * PAGED_GRAN);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    const unsigned below = low_bytes(o - g * PAGED_GRAN - 4 * q4);
+                    w[e][q4] = (recode4(w[e][q4], down) & below) | (w[e][q4] & ~below);
+                }
+                *reinterpret_cast<uintx4*>(vp + (e << shift) + g * PAGED_GRAN) = w[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) vp[(e << shift) + o] = (uint8_t)(code[e >> 2] >> 8 * (e & 3));
+    if (l == 0) {
+        a.kv.ks[ph] = (uint8_t)k_byte;
+        a.kv.vs[ph] = (uint8_t)v_byte;
+    }
+}
+
 template <int HD, typename T>
 __global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_kernel(const WriteArgs<T> a) {
     constexpr int HALF = HD / 2, LPT = HALF / 8, TPW = 64 / LPT;
@@ -569,10 +651,11 @@ __global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_ker
     const int Hkv = a.Hkv;
 
     using Eight = Raw<T, 8>;
-    // the workgroups of the K / V part, which wait more than they move, lie among those of the q part: every kv_pitch-th one
-    const int kv_wg = blockIdx.x / (unsigned)a.kv_pitch;
-    if (kv_wg * a.kv_pitch != (int)blockIdx.x || kv_wg >= a.n_kv_wgs) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
-        const int task = ((int)blockIdx.x - min(kv_wg + 1, a.n_kv_wgs)) * (WR_NT / 64) + wave;
+    // the workgroups of the K / V part, which wait more than they move (and of which those in the middle of a segment leave at once),
+    // lie evenly among those of the q part
+    const int kv_wg = (int)(blockIdx.x * a.kv_share >> 32);   // how many of them come before this workgroup
+    if ((int)((blockIdx.x + 1ull) * a.kv_share >> 32) == kv_wg) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
+        const int task = ((int)blockIdx.x - kv_wg) * (WR_NT / 64) + wave;
         const int per_row = (a.Hq + a.q_heads - 1) / a.q_heads;
         const int row = task / per_row * TPW + lane / LPT, h0 = task % per_row * a.q_heads, d = lane % LPT * 8;
         if (row >= a.n_rows) return;
@@ -610,10 +693,24 @@ __global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_ker
     const int64_t n_slots = (int64_t)a.kv.n_pages << shift;
     auto slot_of = [&](int row) { return row >= 0 && row < a.n_rows ? a.slot[row] : (int64_t)-1; };
     // the slots of 64 rows from row_lo on: `cuts` marks those that do not continue the row before them in its page
-    const int64_t s = slot_of(row_lo + lane);
+    const int64_t s = slot_of(row_lo + lane), next = slot_of(row_lo + lane + 1);
     const bool cut = s < 0 || s >= n_slots || (s & (P - 1)) == 0 || slot_of(row_lo + lane - 1) != s - 1;
     const uint64_t cuts = __ballot(cut);
     uint64_t begins = __ballot(cut && s >= 0 && s < n_slots && lane < a.chunk);
+    // rows that are segments by themselves: 64 / (HD / 8) of them side by side in a wavefront
+    const uint64_t singles = begins & __ballot(next != s + 1 || (next & (P - 1)) == 0);
+    if (singles) {
+        constexpr int SIDE = 64 / (HD / 8);
+        const int n = __builtin_popcountll(singles), lower = __builtin_popcountll(singles & ((1ull << lane) - 1));
+        // lane k of `place` holds the k-th of them
+        const int place = __builtin_amdgcn_ds_permute((singles >> lane & 1 ? lower : n + lane - lower) * 4, lane);
+        for (int k0 = wave * SIDE; k0 < n; k0 += WR_NT / 64 * SIDE) {
+            const int k = k0 + lane / (HD / 8), at = __shfl(place, min(k, n - 1), 64);
+            const int64_t slot = ((int64_t)__shfl((int)(s >> 32), at, 64) << 32) | (unsigned)__shfl((int)s, at, 64);
+            if (k < n) write_single<HD>(a, row_lo + at, slot, kvh);
+        }
+        begins &= ~singles;
+    }
     for (; begins; begins &= begins - 1) {
         const int at = __builtin_ctzll(begins);
         Segment sg;
@@ -649,15 +746,17 @@ static int launch_write(compact_ctx* ctx, int n_rows, const void* qkv, const Pag
                         hipStream_t s) {
     const int Hq = ctx->cfg.n_q_heads, Hkv = ctx->cfg.n_kv_heads;
     constexpr int TPW = 64 / (HD / 16);
-    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 1, 1};
-    a.chunk = n_rows <= 1024 ? 1 : n_rows <= 8192 ? 8 : 64;
+    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 1};
+    // rows per workgroup of the K / V part: its segments of several rows follow each other, those of one row go side by side, and
+    // a prompt leaves all but the first workgroup of a segment idle.  us, 32 + 8 heads of 128, pages of 64: 64 x 4 rows 11.2 by 4, 14.4 by 8,
+    // 61.5 by 64; 1024 rows of a prompt 14.3, 11.8, 11.5; 2 x 4096 52.5, 45.8, 41.3; 4 x 4096 97, 83, 78 (pages of 16: 84 by 16, 100 by 64)
+    a.chunk = n_rows <= 512 ? 4 : n_rows <= 8192 ? 8 : std::min(1 << kv.page_shift, 64);
     const int64_t chunks = (n_rows + a.chunk - 1) / a.chunk, groups = (n_rows + TPW - 1) / TPW;
     a.q_heads = (int)std::min<int64_t>(WR_QHEADS, std::max<int64_t>(1, groups * Hq / 4096));
     const int64_t tasks = groups * ((Hq + a.q_heads - 1) / a.q_heads);
     const int64_t kv_wgs = chunks * Hkv, wgs = kv_wgs + (tasks + WR_NT / 64 - 1) / (WR_NT / 64);
     if (wgs >= INT32_MAX / WR_NT) return set_err(ctx, COMPACT_ESHAPE, "too many rows for one call");
-    a.n_kv_wgs = (int)kv_wgs;
-    a.kv_pitch = (int)(wgs / kv_wgs);
+    a.kv_share = (((uint64_t)kv_wgs << 32) + wgs - 1) / wgs;
     paged_write_kernel<HD, T><<<(unsigned)wgs, WR_NT, 0, s>>>(a);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
