@@ -171,6 +171,49 @@ def test_written_pages_hold_the_rounded_rows(lc, P, steps):
         assert (kv.k[page, :, n:] == 0x7F).all() and (kv.v[page, :, :, n:] == 0x7F).all()
 
 
+@pytest.mark.parametrize("lc", [layer(2, 1, 64), layer(3, 3, 128), layer(2, 1, 64, "fp32")], ids=lambda c: "%d_%d_%s" % (c.n_kv_heads, c.head_dim, c.dtype))
+@pytest.mark.parametrize("P", [16, 128])
+@pytest.mark.parametrize("N,prompt", [(150, 0), (700, 300), (1000, 8000)])
+def test_single_rows_among_others(lc, P, N, prompt):
+    """A batch of mostly one row per request, at every place of a page, behind rows that are smaller, alike and larger (so that
+    scales grow or stay), some rows not finite, segments of a few rows and a prompt among them."""
+    if N > 700 and lc.head_dim == 128:
+        pytest.skip("the same paths as with 700 requests; slow on the host")
+    rng = np.random.default_rng(N + P)
+    Hq, H, hd, dt = lc.n_q_heads, lc.n_kv_heads, lc.head_dim, tdtype(lc)
+    before = rng.integers(0, P, N)
+    n_new = rng.choice([0, 1, 1, 1, 1, 1, 1, 2, 3, 5], N)
+    before[N // 2], n_new[N // 2] = 0, prompt
+    start = np.concatenate([[0], np.cumsum((before + n_new + P - 1) // P)])      # request i has pages start[i] ..
+    kv, ref, lay = gpu_pages(lc, int(start[-1]), P, [[0]], 0x7F), P8.Pages(int(start[-1]), P, H, hd), handle(lc)
+    live = {}
+    for lo, n in ((np.zeros_like(before), before), (before, n_new)):
+        T = int(n.sum())
+        x = rng.standard_normal((T, Hq + 2 * H, hd)) * np.exp(1.5 * rng.standard_normal((T, 1, 1)))
+        if lo is before:
+            x[rng.random(T) < 0.1, Hq + H - 1, 5] = np.inf
+            x[rng.random(T) < 0.1, Hq + 2 * H - 1, 60] = np.nan
+        slot, at = np.full(T, -1), 0
+        for i in range(N):
+            rows = np.arange(lo[i], lo[i] + n[i])
+            slot[at:at + n[i]] = start[i] * P + rows
+            at += n[i]
+            live.update({int(start[i] + r // P): int(r % P) + 1 for r in rows})
+        qkv = torch.tensor(x).to(dt).reshape(T, -1).to(DEV)
+        rot = torch.zeros((T, hd // 2, 2), device=DEV)
+        rot[..., 0] = 1.0
+        q = torch.empty((T, Hq * hd), dtype=dt, device=DEV)
+        lay.compact_rope_paged_write(qkv, kv, torch.tensor(slot, device=DEV), rot, q)
+        y = f64(qkv).reshape(T, Hq + 2 * H, hd)
+        with np.errstate(invalid="ignore"):
+            k = P8.rope(y[:, Hq:Hq + H], f64(rot))     # (an infinity times a sine of 0 breaks its partner too)
+        ref.write(slot.tolist(), k, y[:, Hq + H:])
+        assert torch.equal(q, qkv[:, :Hq * hd])
+    compare_pages(kv, ref, live)
+    for page, n in live.items():
+        assert (kv.k[page, :, n:] == 0x7F).all() and (kv.v[page, :, :, n:] == 0x7F).all()
+
+
 @pytest.mark.parametrize("lc", WRITE_LAYERS, ids=lambda c: "%d_%d_%d_%s" % (c.n_q_heads, c.n_kv_heads, c.head_dim, c.dtype))
 def test_rotated_rows(lc):
     """q and K rotated at large positions: q to one rounding, a K code to half a step of its value."""
