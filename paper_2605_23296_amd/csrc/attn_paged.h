@@ -4,7 +4,7 @@
 
 #define LOG2E 1.4426950408889634f
 
-#define FEW_COLS 16      // query columns (rows x heads of a KV group) of a request that the streaming kernel takes: one MFMA tile
+#define FEW_COLS 32      // query columns (rows x heads of a KV group) of a request that the streaming kernel takes: two MFMA tiles
 #define FEW_CHUNK 256    // cached rows of one of its work items
 #define TILE_COLS 128    // query columns of a tile of the other kernel
 #define TILE_KEYS 64     // cached rows of a step of it

@@ -8,14 +8,20 @@
 #define FEW_WAVES 4
 #define FEW_PLD (FEW_CHUNK + 8)   // bf16 per column of the probability tile (padded against bank conflicts)
 
-// inclusive sum over the workgroup's threads; `red`: one int per wavefront
-__device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// inclusive sum over the wavefront's lanes
+__device__ __forceinline__ int wave_prefix(int v) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int ofs = 1; ofs < 64; ofs <<= 1) {
         const int u = __shfl_up(v, ofs, 64);
         if (lane >= ofs) v += u;
     }
+    return v;
+}
+// inclusive sum over the workgroup's threads; `red`: one int per wavefront
+__device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    v = wave_prefix(v);
     __syncthreads();
     if (lane == 63) red[w] = v;
     __syncthreads();
@@ -29,7 +35,7 @@ __device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
 }
 
 // ---------------------------------------------------------------------------
-// Requests of at most 16 query columns: memory-bound, every cached byte is read once.  A work item is (request, KV head, 256
+// Requests of at most 32 query columns: memory-bound, every cached byte is read once.  A work item is (request, KV head, 256
 // cached rows); a persistent workgroup of four wavefronts takes a contiguous share of them.  Scores S^T = K Q^T by
 // v_mfma_f32_16x16x32_bf16, 64 cached rows per wavefront; the codes go straight from memory into MFMA operands (exact in
 // bf16); probabilities through LDS; output O^T = V^T P^T, HD / 4 elements per wavefront.
@@ -38,11 +44,13 @@ __device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
 // than it needs (it counts outstanding loads), every load of the loop is issued unconditionally, with an address that is
 // read anyway where there is no next item, and the stores stand right before the V loads.  Records are held back in LDS until the
 // buffer is full or the share is done: a store in the load stream stalls it out of proportion.
-// NP: bf16 parts of a query and of a probability (3 for fp32 storage: all 24 bits).
+// NP: bf16 parts of a query and of a probability (3 for fp32 storage: all 24 bits).  CT: tiles of 16 columns, two where a call may
+// have requests of more than 16; a column's sums are the same either way.
 // ---------------------------------------------------------------------------
 #define FEW_REC_SLOTS 8
-// workgroups per CU (head_dim 64 has registers for four: 16 caches of 512 to 8192 rows 21.2 us instead of 18.8)
-__host__ __device__ constexpr int few_resident(int np) { return np > 1 ? 2 : 3; }
+// workgroups per CU (head_dim 64 has registers for four: 16 caches of 512 to 8192 rows 21.2 us instead of 18.8; two column tiles of
+// head_dim 128 spill with three: 8 x 8 rows behind 16384 103 us instead of 95)
+__host__ __device__ constexpr int few_resident(int hd, int np, int ct) { return (np > 1 ? 2 : 3) - (ct > 1 && hd > 64); }
 
 // barrier that waits for this wavefront's LDS operations only: loads from memory stay in flight
 __device__ __forceinline__ void lds_barrier() {
@@ -54,22 +62,26 @@ __device__ __forceinline__ void lds_barrier() {
 #endif
 }
 
-template <int HD, int NP, typename T, bool TILES>
-__global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_few_kernel(const PagedAttnArgs a, int slot_cols, int rec_slots) {
+template <int HD, int NP, typename T, bool TILES, int CT>
+__global__ __launch_bounds__(FEW_WAVES * 64, few_resident(HD, NP, CT)) void attn_paged_few_kernel(const PagedAttnArgs a, int slot_cols, int rec_slots) {
+    constexpr int COLS = 16 * CT;              // query columns
     constexpr int KH = HD / 64;                // 16-byte pieces of a K row per lane
     constexpr int RT = HD / 16 / FEW_WAVES;    // 16-element tiles of O^T per wavefront
     constexpr int VS = FEW_CHUNK / 64;         // 16-byte pieces of a V row per lane
     constexpr int RLD = HD + 4;                // floats of a held record: values, maximum, sum
-    __shared__ __attribute__((aligned(16))) bf16 qs[NP][FEW_COLS * HD];
-    __shared__ __attribute__((aligned(16))) bf16 ps[NP][FEW_COLS * FEW_PLD];
-    __shared__ float s_max[FEW_WAVES][16], s_sum[FEW_WAVES][16];
+    __shared__ __attribute__((aligned(16))) bf16 qs[NP][COLS * HD];
+    __shared__ __attribute__((aligned(16))) bf16 ps[NP][COLS * FEW_PLD];
+    __shared__ float s_max[FEW_WAVES][COLS], s_sum[FEW_WAVES][COLS];
     __shared__ int red[FEW_WAVES];
     extern __shared__ __attribute__((aligned(16))) float recbuf[];   // [slot][column][RLD]
     __shared__ int64_t held_rec[FEW_REC_SLOTS];
     __shared__ int held_pieces[FEW_REC_SLOTS], held_cols[FEW_REC_SLOTS];
     const int N = a.kv.n_requests, G = a.Hq / a.Hkv, Hkv = a.Hkv;
     const int t = threadIdx.x, lane = t & 63, wave = wave_index();
-    const int r = lane & 15, c = lane >> 4, r_row = r / G, r_head = r % G;
+    const int r = lane & 15, c = lane >> 4;
+    int r_row[CT], r_head[CT];   // of column u * 16 + r
+#pragma unroll
+    for (int u = 0; u < CT; ++u) r_row[u] = (u * 16 + r) / G, r_head[u] = (u * 16 + r) % G;
     const int shift = a.kv.page_shift, P = 1 << shift;
 
     // ---- the other kernel's schedule: the requests with the longest units first (by the first two bits of their keys' number:
@@ -133,12 +145,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
     auto scan = [&](int i0) {
         rq = paged_req(a, min(i0 + lane, N - 1));
         n_items = i0 + lane < N ? items_of(rq) : 0;
-        upto = n_items;
-#pragma unroll
-        for (int ofs = 1; ofs < 64; ofs <<= 1) {
-            const int u = __shfl_up(upto, ofs, 64);
-            if (lane >= ofs) upto += u;
-        }
+        upto = wave_prefix(n_items);
     };
     int total = 0;
     for (int i0 = 0; i0 < N; i0 += 64) {
@@ -226,12 +233,19 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
     };
     // the item's query rows: columns row * G + head of the group, 8 elements per thread
     struct alignas(16) Eight { T x[8]; };
-    Eight qreg;
-    const int q_col = min(t / (HD / 8), FEW_COLS - 1), q_e = t % (HD / 8) * 8, q_row = q_col / G, q_head = q_col % G;
-    static_assert(FEW_COLS * HD / 8 <= FEW_WAVES * 64, "a thread holds at most one piece of the query rows");
+    constexpr int QP = (COLS * HD / 8 + FEW_WAVES * 64 - 1) / (FEW_WAVES * 64);   // pieces per thread
+    Eight qreg[QP];
+    int q_row[QP], q_head[QP];
+    const int q_e = t % (HD / 8) * 8;
+    auto q_col = [&](int j) { return min((j * FEW_WAVES * 64 + t) / (HD / 8), COLS - 1); };
+#pragma unroll
+    for (int j = 0; j < QP; ++j) q_row[j] = q_col(j) / G, q_head[j] = q_col(j) % G;
     auto load_q = [&](const Item& it) {
-        const int row = it.row0 + min(q_row, it.n - 1);
-        qreg = *reinterpret_cast<const Eight*>((const T*)a.q + (size_t)row * a.q_stride + (it.kvh * G + q_head) * HD + q_e);
+#pragma unroll
+        for (int j = 0; j < QP; ++j) {
+            const int row = it.row0 + min(q_row[j], it.n - 1);
+            qreg[j] = *reinterpret_cast<const Eight*>((const T*)a.q + (size_t)row * a.q_stride + (it.kvh * G + q_head[j]) * HD + q_e);
+        }
     };
 
     // (sent in the order that the loop sends them: the compiler waits for a load by the least number of later ones)
@@ -254,6 +268,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
         const bool has_next = left > 1;
         const int keep = here(has_next ? -1 : 0);
         const int base = cur.ch * FEW_CHUNK, n_keys = min(cur.kv - base, FEW_CHUNK), cols = cur.n * G;
+        const bool wide = CT > 1 && (!TILES || cols > 16);   // (beside prompts most requests have one row: 64 of them 4 us in 100)
         // pages and scales of the next item; the page numbers of the one after it
         pid = in_range(pid_n);
         Item nn = nxt;
@@ -266,82 +281,106 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
             q_req = cur.req;
             q_kvh = cur.kvh;
             lds_barrier();   // (the rows before have been read)
-            if (t < FEW_COLS * HD / 8) {
-                bf16x8 part[NP];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    bf16 p[NP];
-                    split_bf16<NP>(q_col < cols ? to_f32(qreg.x[j]) : 0.f, p);
+            for (int jj = 0; jj < QP; ++jj)
+                if (t + jj * FEW_WAVES * 64 < COLS * HD / 8) {
+                    bf16x8 part[NP];
 #pragma unroll
-                    for (int u = 0; u < NP; ++u) part[u][j] = p[u];
+                    for (int j = 0; j < 8; ++j) {
+                        bf16 p[NP];
+                        split_bf16<NP>(q_col(jj) < cols ? to_f32(qreg[jj].x[j]) : 0.f, p);
+#pragma unroll
+                        for (int u = 0; u < NP; ++u) part[u][j] = p[u];
+                    }
+#pragma unroll
+                    for (int u = 0; u < NP; ++u) *reinterpret_cast<bf16x8*>(&qs[u][q_col(jj) * HD + q_e]) = part[u];
                 }
-#pragma unroll
-                for (int u = 0; u < NP; ++u) *reinterpret_cast<bf16x8*>(&qs[u][q_col * HD + q_e]) = part[u];
-            }
             lds_barrier();
         }
 
-        // ---- S^T = K Q^T: lane (r, c) of tile tt gets column r, rows wave * 64 + tt * 16 + 4c .. + 3 ----
-        float sv[4][4];
-        float mx = -INFINITY;
-        const int sees = min(cur.kv - cur.n + (r < cols ? r_row : 0) + 1 - base, n_keys);   // rows of the chunk that column r sees
+        // ---- S^T = K Q^T: lane (r, c) of tile tt gets columns u * 16 + r, rows wave * 64 + tt * 16 + 4c .. + 3 ----
+        float sv[CT][4][4], mx[CT];
+        int sees[CT];   // rows of the chunk that the column sees
+#pragma unroll
+        for (int u = 0; u < CT; ++u) {
+            mx[u] = -INFINITY;
+            sees[u] = min(cur.kv - cur.n + (u * 16 + r < cols ? r_row[u] : 0) + 1 - base, n_keys);
+        }
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt) {
-            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+            floatx4 acc[CT];
+#pragma unroll
+            for (int w = 0; w < CT; ++w) acc[w] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < KH; ++s)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const bf16x8 kb = codes8_to_bf16(kf[tt][s][2 * i], kf[tt][s][2 * i + 1], 1.0f);
 #pragma unroll
-                    for (int u = 0; u < NP; ++u) {
-                        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(&qs[u][r * HD + s * 64 + c * 16 + i * 8]);
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qf, acc, 0, 0, 0);
+                    for (int w = 0; w < CT; ++w) {
+                        if (w > 0 && !wide) continue;
+#pragma unroll
+                        for (int u = 0; u < NP; ++u) {
+                            const bf16x8 qf = *reinterpret_cast<const bf16x8*>(&qs[u][(w * 16 + r) * HD + s * 64 + c * 16 + i * 8]);
+                            acc[w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qf, acc[w], 0, 0, 0);
+                        }
                     }
                 }
             const int g = wave * 4 + tt;
             const float f = a.scale_log2 * e8m0(__builtin_amdgcn_readlane(ksb, g));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sv[tt][e] = g * PAGED_GRAN + 4 * c + e < sees ? acc[e] * f : -INFINITY;
-                mx = fmaxf(mx, sv[tt][e]);
-            }
+            for (int w = 0; w < CT; ++w)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sv[w][tt][e] = g * PAGED_GRAN + 4 * c + e < sees[w] ? acc[w][e] * f : -INFINITY;
+                    mx[w] = fmaxf(mx[w], sv[w][tt][e]);
+                }
         }
         // the K registers are free
         load_k(nxt, pid, keep);
         load_q(nxt);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        if (c == 0) s_max[wave][r] = mx;
-        lds_barrier();
-        float m = -3e38f;   // (finite where a column sees nothing: its probabilities are exp2(-inf) = 0)
 #pragma unroll
-        for (int i = 0; i < FEW_WAVES; ++i) m = fmaxf(m, s_max[i][r]);
-        float l = 0.f;
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-            bf16x4 pv[NP];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = exp2_fast(sv[tt][e] - m);
-                l += p;
-                bf16 part[NP];
-                split_bf16<NP>(p, part);
-#pragma unroll
-                for (int u = 0; u < NP; ++u) pv[u][e] = part[u];
-            }
-#pragma unroll
-            for (int u = 0; u < NP; ++u) *reinterpret_cast<bf16x4*>(&ps[u][r * FEW_PLD + wave * 64 + tt * 16 + 4 * c]) = pv[u];
+        for (int w = 0; w < CT; ++w) {
+            mx[w] = fmaxf(mx[w], __shfl_xor(mx[w], 16, 64));
+            mx[w] = fmaxf(mx[w], __shfl_xor(mx[w], 32, 64));
+            if (c == 0) s_max[wave][w * 16 + r] = mx[w];
         }
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
-        if (c == 0) s_sum[wave][r] = l;
+        lds_barrier();
+        float m[CT];   // (finite where a column sees nothing: its probabilities are exp2(-inf) = 0)
+#pragma unroll
+        for (int w = 0; w < CT; ++w) {
+            if (w > 0 && !wide) continue;
+            m[w] = -3e38f;
+#pragma unroll
+            for (int i = 0; i < FEW_WAVES; ++i) m[w] = fmaxf(m[w], s_max[i][w * 16 + r]);
+            float l = 0.f;
+#pragma unroll
+            for (int tt = 0; tt < 4; ++tt) {
+                bf16x4 pv[NP];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = exp2_fast(sv[w][tt][e] - m[w]);
+                    l += p;
+                    bf16 part[NP];
+                    split_bf16<NP>(p, part);
+#pragma unroll
+                    for (int u = 0; u < NP; ++u) pv[u][e] = part[u];
+                }
+#pragma unroll
+                for (int u = 0; u < NP; ++u) *reinterpret_cast<bf16x4*>(&ps[u][(w * 16 + r) * FEW_PLD + wave * 64 + tt * 16 + 4 * c]) = pv[u];
+            }
+            l += __shfl_xor(l, 16, 64);
+            l += __shfl_xor(l, 32, 64);
+            if (c == 0) s_sum[wave][w * 16 + r] = l;
+        }
         lds_barrier();
 
         // ---- O^T = V^T P^T: HD / 4 elements per wavefront over all rows of the chunk -----------------
-        floatx4 oacc[RT];
+        floatx4 oacc[CT][RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) oacc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < CT; ++w)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) oacc[w][i] = floatx4{0.f, 0.f, 0.f, 0.f};
         if (n_keys < FEW_CHUNK) {   // whatever lies behind the cached rows must not reach the MFMA
 #pragma unroll
             for (int j = 0; j < VS; ++j)
@@ -361,31 +400,39 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(NP)) void attn_paged_f
 #pragma unroll
                 for (int i = 0; i < RT; ++i) vb[i] = codes8_to_bf16(vf[i][j][2 * h], vf[i][j][2 * h + 1], sc);
 #pragma unroll
-                for (int u = 0; u < NP; ++u) {
-                    const bf16x8 pb = *reinterpret_cast<const bf16x8*>(&ps[u][r * FEW_PLD + 64 * j + 16 * c + 8 * h]);
+                for (int w = 0; w < CT; ++w) {
+                    if (w > 0 && !wide) continue;
 #pragma unroll
-                    for (int i = 0; i < RT; ++i) oacc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb[i], pb, oacc[i], 0, 0, 0);
+                    for (int u = 0; u < NP; ++u) {
+                        const bf16x8 pb = *reinterpret_cast<const bf16x8*>(&ps[u][(w * 16 + r) * FEW_PLD + 64 * j + 16 * c + 8 * h]);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) oacc[w][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb[i], pb, oacc[w][i], 0, 0, 0);
+                    }
                 }
             }
         }
-        float lt = s_sum[0][r];
+        // lane (r, c): columns w * 16 + r, elements (wave * RT + i) * 16 + 4c .. + 3
 #pragma unroll
-        for (int i = 1; i < FEW_WAVES; ++i) lt += s_sum[i][r];
-        // lane (r, c): column r, elements (wave * RT + i) * 16 + 4c .. + 3
-        if (cur.pieces == 1) {
-            if (r < cols) {
-                const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-                T* op = (T*)a.o + ((size_t)(cur.row0 + r_row) * a.Hq + cur.kvh * G + r_head) * HD + 4 * c;
+        for (int w = 0; w < CT; ++w) {
+            const int col = w * 16 + r;
+            float lt = s_sum[0][col];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) put4(op + (wave * RT + i) * 16, oacc[i][0] * inv, oacc[i][1] * inv, oacc[i][2] * inv, oacc[i][3] * inv);
+            for (int i = 1; i < FEW_WAVES; ++i) lt += s_sum[i][col];
+            if (cur.pieces == 1) {
+                if (col < cols) {
+                    const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+                    T* op = (T*)a.o + ((size_t)(cur.row0 + r_row[w]) * a.Hq + cur.kvh * G + r_head[w]) * HD + 4 * c;
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) put4(op + (wave * RT + i) * 16, oacc[w][i][0] * inv, oacc[w][i][1] * inv, oacc[w][i][2] * inv, oacc[w][i][3] * inv);
+                }
+            } else if (col < cols) {
+                float* slot = recbuf + (size_t)n_held * slot_cols * RLD + col * RLD;
+#pragma unroll
+                for (int i = 0; i < RT; ++i) *reinterpret_cast<floatx4*>(slot + (wave * RT + i) * 16 + 4 * c) = oacc[w][i];
+                if (wave == 0 && c == 0) *reinterpret_cast<float2*>(slot + HD) = make_float2(m[w], lt);
             }
-        } else {
-            float* slot = recbuf + (size_t)n_held * slot_cols * RLD + r * RLD;
-            if (r < cols) {
-#pragma unroll
-                for (int i = 0; i < RT; ++i) *reinterpret_cast<floatx4*>(slot + (wave * RT + i) * 16 + 4 * c) = oacc[i];
-                if (wave == 0 && c == 0) *reinterpret_cast<float2*>(slot + HD) = make_float2(m, lt);
-            }
+        }
+        if (cur.pieces > 1) {
             if (t == 0) {
                 held_rec[n_held] = (int64_t)cur.req * a.rec_stride * a.Hq + (int64_t)cur.kvh * G * cur.pieces + cur.ch;
                 held_pieces[n_held] = cur.pieces;
@@ -486,6 +533,14 @@ __device__ __forceinline__ void merge_pair(const PagedAttnArgs& a, const PagedRe
     }
 }
 
+// pieces of a request's keys
+__device__ __forceinline__ int pieces_of(const PagedReq& rq, int G) {
+    return is_few(rq.n, G) ? few_pieces(rq.kv) : tile_pieces(n_tiles(rq.n, G), rq.kv);
+}
+template <int HD>
+__device__ __forceinline__ bool wave_each(int pieces) { return pieces <= MERGE_FLIGHT * (256 / HD); }
+
+// A workgroup per row and heads_per_wg query heads.
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnArgs a, int rows_per_req, int heads_per_wg) {
     __shared__ floatx4 part[HD];
@@ -495,12 +550,63 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnAr
     const int row = id % rows_per_req, req = id / rows_per_req;
     const PagedReq rq = paged_req(a, req);
     if (row >= rq.n) return;
-    const int pieces = is_few(rq.n, G) ? few_pieces(rq.kv) : tile_pieces(n_tiles(rq.n, G), rq.kv);
+    const int pieces = pieces_of(rq, G);
     if (pieces == 1) return;   // written by the kernel before
-    if (pieces <= MERGE_FLIGHT * (256 / HD)) {
+    if (wave_each<HD>(pieces)) {
         for (int head = h_lo + wave_index(); head < h_end; head += 4) merge_pair<HD, 1, T>(a, rq, req, row, head, pieces, part);
     } else {
         for (int head = h_lo; head < h_end; ++head) merge_pair<HD, 4, T>(a, rq, req, row, head, pieces, part);
+    }
+}
+
+// The same where a call has prompts, hardly any of whose rows are split: a fixed number of workgroups shares out the pairs
+// (four at a time where a wavefront joins one) that the requests' lengths give (64 single rows behind 2048 in a call for up to
+// 64 rows each: 79 us instead of 102).
+template <int HD, typename T>
+__global__ __launch_bounds__(256) void attn_paged_merge_share_kernel(const PagedAttnArgs a) {
+    __shared__ floatx4 part[HD];
+    const int N = a.kv.n_requests, G = a.Hq / a.Hkv, lane = threadIdx.x & 63, fours = (a.Hq + 3) / 4;
+    auto items_of = [&](const PagedReq& rq, int& pieces) {
+        pieces = rq.n > 0 ? pieces_of(rq, G) : 1;
+        return pieces == 1 ? 0 : rq.n * (wave_each<HD>(pieces) ? fours : a.Hq);
+    };
+    int upto = 0, n_items = 0, pieces;
+    auto scan = [&](int i0) {
+        n_items = items_of(paged_req(a, min(i0 + lane, N - 1)), pieces);
+        if (i0 + lane >= N) n_items = 0;
+        upto = wave_prefix(n_items);
+    };
+    int total = 0;
+    for (int i0 = 0; i0 < N; i0 += 64) {
+        scan(i0);
+        total += __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int w = (int)((int64_t)blockIdx.x * total / gridDim.x);
+    int left = (int)((int64_t)(blockIdx.x + 1) * total / gridDim.x) - w;
+    if (left <= 0) return;
+    int first = 0, before = 0;
+    uint64_t past = 0;
+    for (;; first += 64) {
+        if (N > 64) scan(first);
+        past = __ballot(before + upto > w);
+        if (past) break;
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int at = __builtin_ctzll(past);
+    int req = first + at, item = w - before - __builtin_amdgcn_readlane(upto - n_items, at);
+    for (;; ++req, item = 0) {   // (ends: the requests' items add up to the share)
+        const PagedReq rq = paged_req(a, req);
+        const int end = min(items_of(rq, pieces), item + left);
+        left -= max(end - item, 0);
+        for (; item < end; ++item) {
+            if (wave_each<HD>(pieces)) {
+                const int head = item % fours * 4 + wave_index();
+                if (head < a.Hq) merge_pair<HD, 1, T>(a, rq, req, item / fours, head, pieces, part);
+            } else {
+                merge_pair<HD, 4, T>(a, rq, req, item / a.Hq, item % a.Hq, pieces, part);
+            }
+        }
+        if (left <= 0) return;
     }
 }
 
@@ -558,10 +664,11 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     if (most > INT32_MAX) return set_err(ctx, COMPACT_ESHAPE, "n_requests * max_kv_len beyond what one call indexes");
     {
         ProfileScope ps(ctx, COMPACT_K_ATTN_DECODE, s);
-        auto few = tiles ? attn_paged_few_kernel<HD, NP, T, true> : attn_paged_few_kernel<HD, NP, T, false>;
+        const int ct = (int64_t)a.max_new * G > 16 ? 2 : 1;
+        auto few = tiles ? attn_paged_few_kernel<HD, NP, T, true, 2> : ct == 2 ? attn_paged_few_kernel<HD, NP, T, false, 2> : attn_paged_few_kernel<HD, NP, T, false, 1>;
         const int slot_cols = std::min(a.max_new, FEW_COLS / G) * G, slot_bytes = slot_cols * (HD + 4) * (int)sizeof(float);
         const int slots = std::max(1, std::min(FEW_REC_SLOTS, (16 << 10) / slot_bytes));
-        few<<<(unsigned)std::min<int64_t>(most, few_resident(NP) * n_cus), FEW_WAVES * 64, slots * slot_bytes, s>>>(a, slot_cols, slots);
+        few<<<(unsigned)std::min<int64_t>(most, few_resident(HD, NP, ct) * n_cus), FEW_WAVES * 64, slots * slot_bytes, s>>>(a, slot_cols, slots);
     }
     LAUNCH_CHECK(ctx);
     if (tiles) TRY_RC(launch_attn_paged_tiles(ctx, a, s));
@@ -569,13 +676,17 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     // rows of a request whose keys may be split: 512 t * 2 <= max_kv for its t tiles
     const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * (a.max_kv / TILE_SPLIT / 2) / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
-    // query heads per workgroup: one while that gives no more than some thousand workgroups, else four and more (those of rows
-    // that are not split leave at once)
-    int heads = 1;
-    while (heads < c.n_q_heads && rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads) > 4096) heads = std::max(4, 2 * heads);
-    const int64_t wgs = rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads);
-    if (wgs >= INT32_MAX / 256) return set_err(ctx, COMPACT_ESHAPE, "too many rows of split requests for one call");
-    attn_paged_merge_kernel<HD, T><<<(unsigned)wgs, 256, 0, s>>>(a, (int)rows, heads);
+    if (tiles) {
+        const int64_t pairs = rows * a.kv.n_requests * c.n_q_heads;
+        if (pairs > INT32_MAX) return set_err(ctx, COMPACT_ESHAPE, "too many rows of split requests for one call");
+        attn_paged_merge_share_kernel<HD, T><<<(unsigned)std::min<int64_t>(pairs, 4 * n_cus), 256, 0, s>>>(a);
+    } else {
+        // query heads per workgroup: one while that gives no more than some thousand workgroups, else four and more
+        int heads = 1;
+        while (heads < c.n_q_heads && rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads) > 4096) heads = std::max(4, 2 * heads);
+        const int64_t wgs = rows * a.kv.n_requests * ((c.n_q_heads + heads - 1) / heads);   // (at most 32 rows of 4096 requests)
+        attn_paged_merge_kernel<HD, T><<<(unsigned)wgs, 256, 0, s>>>(a, (int)rows, heads);
+    }
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }

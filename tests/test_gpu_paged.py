@@ -484,6 +484,44 @@ def test_a_request_does_not_depend_on_the_others(lc):
     assert torch.equal(torch.cat(torch.split(got, n_new[::-1])[::-1]), both)
 
 
+@pytest.mark.parametrize("lc", [layer(32, 8, 128), layer(16, 1, 128), layer(64, 8, 64), layer(9, 3, 64), layer(4, 2, 64, "fp32"), layer(6, 1, 128, "fp32")], ids=IDS)
+@pytest.mark.parametrize("P", [16, 64])
+def test_a_few_rows_behind_a_cache(lc, P):
+    """Requests of one column to a few more than 32, by themselves (no prompt in the call: other kernels) and beside a prompt
+    whose keys are split too; a call with none but few rows, and one with single rows among them."""
+    G = lc.n_q_heads // lc.n_kv_heads
+    n_new = sorted({1, 2, 15 // G + 1, 16 // G, 16 // G + 1, 31 // G + 1, 32 // G, 32 // G + 1} - {0}) + [40, 1]
+    lens = [[3, 300, 513, 1500, 256, 257, 17, 700, 40, 2100][i % 10] for i in range(len(n_new))]
+    lens[-2], lens[-1] = 2100, 900
+    lens = [max(n, L) for n, L in zip(n_new, lens)]
+    kv, ref, table = random_cache(lc, lens, P, P + G)
+    q, lay = queries(lc, sum(n_new), P), handle(lc)
+    both = run_attn(lay, kv, q, n_new, lens)
+    check_attn(lc, q, both, n_new, lens, ref, table)
+    rows, want = torch.split(q, n_new), torch.split(both, n_new)
+    for least, most in ((1, 16 // G), (1, 32 // G), (2, 32 // G)):
+        some = [i for i, n in enumerate(n_new) if least <= n <= most]
+        if not some:
+            continue
+        sub = B.PagedKV(lc, kv.k, kv.v, kv.k_scale, kv.v_scale, kv.table[some].contiguous())
+        got = run_attn(lay, sub, torch.cat([rows[i] for i in some]), [n_new[i] for i in some], [lens[i] for i in some])
+        assert torch.equal(got, torch.cat([want[i] for i in some])), (least, most)
+
+
+@pytest.mark.parametrize("N", [65, 300])
+def test_many_requests_beside_a_prompt(N):
+    """More requests than a wavefront looks at side by side, most of them single rows of split caches, some resting."""
+    lc = layer(4, 2, 64)
+    rng = np.random.default_rng(N)
+    n_new = rng.choice([0, 1, 1, 1, 2, 20], N).tolist()
+    lens = [max(n, int(L)) for n, L in zip(n_new, rng.integers(1, 700, N))]
+    n_new[N // 2], lens[N // 2] = 90, 1100
+    kv, ref, table = random_cache(lc, lens, 32, N)
+    q, lay = queries(lc, sum(n_new), N), handle(lc)
+    o = run_attn(lay, kv, q, n_new, [L if n else 0 for n, L in zip(n_new, lens)])
+    check_attn(lc, q, o, n_new, lens, ref, table)
+
+
 def test_strided_queries_and_rows_of_nobody():
     lc = layer(8, 2, 64)
     n_new, lens = [2, 30], [50, 400]
