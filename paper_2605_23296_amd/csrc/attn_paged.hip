@@ -44,6 +44,11 @@ __device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
 // than it needs (it counts outstanding loads), every load of the loop is issued unconditionally, with an address that is
 // read anyway where there is no next item, and the stores stand right before the V loads.  Records are held back in LDS until the
 // buffer is full or the share is done: a store in the load stream stalls it out of proportion.
+// Bound: the codes' way from HBM (64 caches of 2048 rows, 8 KV heads of 128: 268 MB in 56 us, 4.8 TB/s of the 6.2 that a sum reaches;
+// one cache of 32768 rows, 67 MB, 16 us: three loads one behind the other (lengths, page number, codes) before the first
+// item, and the last workgroups' items).  256 rows per item: 512 leave no registers for the next item's loads.  Requests of
+// 17 to 32 columns pay records of half the columns' bytes (8 x 8 rows behind 16384: 93 us; as tiles of 128 columns 106); with four column
+// tiles, for up to 64, those and the registers cost more than they save (16 rows behind 32768: 55 us, as tiles 36).
 // NP: bf16 parts of a query and of a probability (3 for fp32 storage: all 24 bits).  CT: tiles of 16 columns, two where a call may
 // have requests of more than 16; a column's sums are the same either way.
 // ---------------------------------------------------------------------------
@@ -469,7 +474,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(HD, NP, CT)) void attn
 
 // ---------------------------------------------------------------------------
 // Joins the pieces of the (row, query head) pairs of split requests.  HD / 4 lanes span a record; a lane sends for up to
-// MERGE_FLIGHT records before it uses one.  A request whose records one wavefront can send for at once has a wavefront per pair
+// MERGE_FLIGHT records before it uses one.  With m = max m_i: o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i.  Bound by the launch
+// and two loads one behind the other (4 to 5 us for 64 x 8 and for 128 pieces; a call that merges nothing 3.8).  A request whose records one wavefront can send for at once has a wavefront per pair
 // (32 pieces of head_dim 64: 4.0 us instead of 7.2), one with more of them all four wavefronts of the workgroup.
 // ---------------------------------------------------------------------------
 #define MERGE_FLIGHT 8

@@ -44,6 +44,9 @@ int paged_view(compact_ctx* ctx, const compact_paged_kv* kv, bool with_pages, Pa
 // columns that are read lie below a request's length, those written above it; stack entries that are read lie below
 // n_free, those written above; lengths and counters come in pairs.  Page numbers are copied, never followed, so whatever the
 // device arrays hold, nothing outside them is touched.
+// Bound: up to some thousand rows by the launch and the chain of loads and scans (64 decode steps 5 us, 1024 of them 12); beyond
+// that by the angles, which are formed in 64 bits, a row's from the row before by a turn, and by the writes of 8 + 4 hd bytes
+// a row (8 x 4096 rows, 17 MB: 10 us; 512 requests with 36000 rows 14).
 // ---------------------------------------------------------------------------
 #define PLAN_NT 256
 
@@ -301,7 +304,8 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
 // Further workgroups rotate q.
 // Bound by HBM from some thousand rows on: every row is read once, q and the codes are written once (8 x 4096 rows of 32 + 16
 // heads of 128: 755 MB in 146 us, 5.2 TB/s, where a copy reaches 4.9 and a sum 6.2); by the launch and one chain of
-// dependent loads (slot, scale, row) below: 24 decode rows 6.3 us.
+// dependent loads (slot, scale, row) below: 24 decode rows 4.5 us.  A single row's V touches hd lines for a
+// byte each, which 1000 such rows feel (28 us, 130 MB of lines read and written for 2 MB of codes).
 // ---------------------------------------------------------------------------
 #define WR_NT 256
 #define WR_QHEADS 8   // most query heads per wavefront of the q part
@@ -315,7 +319,8 @@ struct WriteArgs {
     PagedView kv;
     int n_rows, Hq, Hkv;
     int chunk;            // rows whose segments one workgroup goes through
-    uint64_t kv_share;    // share of the workgroups that do K and V, times 2^32 (rounded up)
+    int n_kv_wgs;         // workgroups of the K / V part
+    uint64_t kv_share;    // 2^32 times their share of the workgroups in order, until there are none left
     int q_heads;          // query heads per wavefront of the q part
 };
 
@@ -565,6 +570,10 @@ __device__ __forceinline__ void write_v(const WriteArgs<T>& a, const Segment& sg
     if (lane + 64 * half == 0) a.kv.vs[sg.ph] = (uint8_t)byte;
 }
 
+// workgroups per CU
+template <typename T>
+__host__ __device__ constexpr int write_resident() { return sizeof(T) == 2 ? 4 : 3; }
+
 // One row that is a segment by itself (a decode step), K and V, by HD / 8 lanes.  Nothing is read that the row does not need: its V
 // codes are stored byte by byte, and earlier rows are touched only where a scale grows.
 template <int HD, typename T>
@@ -645,16 +654,17 @@ __device__ __forceinline__ void write_single(const WriteArgs<T>& a, int row, int
 }
 
 template <int HD, typename T>
-__global__ __launch_bounds__(WR_NT, sizeof(T) == 2 ? 4 : 3) void paged_write_kernel(const WriteArgs<T> a) {
+__global__ __launch_bounds__(WR_NT, write_resident<T>()) void paged_write_kernel(const WriteArgs<T> a) {
     constexpr int HALF = HD / 2, LPT = HALF / 8, TPW = 64 / LPT;
     const int lane = threadIdx.x & 63, wave = wave_index();
     const int Hkv = a.Hkv;
 
     using Eight = Raw<T, 8>;
     // the workgroups of the K / V part, which wait more than they move (and of which those in the middle of a segment leave at once),
-    // lie evenly among those of the q part
-    const int kv_wg = (int)(blockIdx.x * a.kv_share >> 32);   // how many of them come before this workgroup
-    if ((int)((blockIdx.x + 1ull) * a.kv_share >> 32) == kv_wg) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
+    // lie evenly among those of the q part, or before them
+    auto kv_before = [&](uint64_t wg) { return min((int)(wg * a.kv_share >> 32), a.n_kv_wgs); };
+    const int kv_wg = kv_before(blockIdx.x);
+    if (kv_before(blockIdx.x + 1ull) == kv_wg) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
         const int task = ((int)blockIdx.x - kv_wg) * (WR_NT / 64) + wave;
         const int per_row = (a.Hq + a.q_heads - 1) / a.q_heads;
         const int row = task / per_row * TPW + lane / LPT, h0 = task % per_row * a.q_heads, d = lane % LPT * 8;
@@ -746,7 +756,7 @@ static int launch_write(compact_ctx* ctx, int n_rows, const void* qkv, const Pag
                         hipStream_t s) {
     const int Hq = ctx->cfg.n_q_heads, Hkv = ctx->cfg.n_kv_heads;
     constexpr int TPW = 64 / (HD / 16);
-    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 1};
+    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 0, 1};
     // rows per workgroup of the K / V part: its segments of several rows follow each other, those of one row go side by side, and
     // a prompt leaves all but the first workgroup of a segment idle.  us, 32 + 8 heads of 128, pages of 64: 64 x 4 rows 11.2 by 4, 14.4 by 8,
     // 61.5 by 64; 1024 rows of a prompt 14.3, 11.8, 11.5; 2 x 4096 52.5, 45.8, 41.3; 4 x 4096 97, 83, 78 (pages of 16: 84 by 16, 100 by 64)
@@ -756,7 +766,11 @@ static int launch_write(compact_ctx* ctx, int n_rows, const void* qkv, const Pag
     const int64_t tasks = groups * ((Hq + a.q_heads - 1) / a.q_heads);
     const int64_t kv_wgs = chunks * Hkv, wgs = kv_wgs + (tasks + WR_NT / 64 - 1) / (WR_NT / 64);
     if (wgs >= INT32_MAX / WR_NT) return set_err(ctx, COMPACT_ESHAPE, "too many rows for one call");
-    a.kv_share = (((uint64_t)kv_wgs << 32) + wgs - 1) / wgs;
+    // K and V first where all run at once (1950 rows of fp32 storage, 4 + 2 heads of 64: 6.9 us instead of 7.8), else evenly (see there)
+    int n_cus = 0;
+    TRY_RC(device_cu_count(ctx, &n_cus));
+    a.n_kv_wgs = (int)kv_wgs;
+    a.kv_share = wgs <= write_resident<T>() * n_cus ? 1ull << 32 : (((uint64_t)kv_wgs << 32) + wgs - 1) / wgs;
     paged_write_kernel<HD, T><<<(unsigned)wgs, WR_NT, 0, s>>>(a);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
