@@ -303,7 +303,7 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
 // (decode steps) go four and more side by side in a wavefront, without a barrier (200 of them: 13.7 -> 8.3 us).
 // Further workgroups rotate q.
 // Bound by HBM from some thousand rows on: every row is read once, q and the codes are written once (8 x 4096 rows of 32 + 16
-// heads of 128: 755 MB in 146 us, 5.2 TB/s, where a copy reaches 4.9 and a sum 6.2); by the launch and one chain of
+// heads of 128: 755 MB in 143 us, 5.3 TB/s, where a copy reaches 4.9 and a sum 6.2); by the launch and one chain of
 // dependent loads (slot, scale, row) below: 24 decode rows 4.5 us.  A single row's V touches hd lines for a
 // byte each, which 1000 such rows feel (28 us, 130 MB of lines read and written for 2 MB of codes).
 // ---------------------------------------------------------------------------
@@ -319,8 +319,8 @@ struct WriteArgs {
     PagedView kv;
     int n_rows, Hq, Hkv;
     int chunk;            // rows whose segments one workgroup goes through
-    int n_kv_wgs;         // workgroups of the K / V part
-    uint64_t kv_share;    // 2^32 times their share of the workgroups in order, until there are none left
+    int unit;             // rows of a unit, one or more chunks (all of a call's, or 16 and more)
+    int kv_wgs, q_wgs;    // workgroups of a unit
     int q_heads;          // query heads per wavefront of the q part
 };
 
@@ -660,15 +660,26 @@ __global__ __launch_bounds__(WR_NT, write_resident<T>()) void paged_write_kernel
     const int Hkv = a.Hkv;
 
     using Eight = Raw<T, 8>;
-    // the workgroups of the K / V part, which wait more than they move (and of which those in the middle of a segment leave at once),
-    // lie evenly among those of the q part, or before them
-    auto kv_before = [&](uint64_t wg) { return min((int)(wg * a.kv_share >> 32), a.n_kv_wgs); };
-    const int kv_wg = kv_before(blockIdx.x);
-    if (kv_before(blockIdx.x + 1ull) == kv_wg) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
-        const int task = ((int)blockIdx.x - kv_wg) * (WR_NT / 64) + wave;
+    // A unit's workgroups are on one XCD, whose L2 they share the rotations through (workgroups go to the XCDs in turn, the
+    // units of a round one place further on each time: a page's segments begin every so many units).  Those of K and V,
+    // which wait more than they move (and of which those in the middle of a segment leave at once), lie evenly among the unit's others.
+    // A call whose workgroups all run at once is one unit over all XCDs, K and V first.
+    int at = blockIdx.x, kv_at = at < a.kv_wgs ? at : -1, unit_row = 0;   // kv_at: which of the unit's workgroups for K and V
+    if (a.n_rows > a.unit) {
+        const int per_unit = a.kv_wgs + a.q_wgs, round = (at >> 3) / per_unit;
+        unit_row = (round * 8 + ((at + round) & 7)) * a.unit;
+        at = (at >> 3) % per_unit;
+        const int before = at * a.kv_wgs / per_unit;
+        kv_at = (at + 1) * a.kv_wgs / per_unit > before ? before : -1;
+        at -= before;
+    } else {
+        at -= a.kv_wgs;
+    }
+    if (kv_at < 0) {   // ---- q: TPW rows of q_heads heads per wavefront, four heads at a time
+        const int task = at * (WR_NT / 64) + wave;
         const int per_row = (a.Hq + a.q_heads - 1) / a.q_heads;
-        const int row = task / per_row * TPW + lane / LPT, h0 = task % per_row * a.q_heads, d = lane % LPT * 8;
-        if (row >= a.n_rows) return;
+        const int in_rows = task / per_row * TPW + lane / LPT, row = unit_row + in_rows, h0 = task % per_row * a.q_heads, d = lane % LPT * 8;
+        if (in_rows >= a.unit || row >= a.n_rows) return;
         float2 cs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) cs[j] = a.rot[(size_t)row * HALF + d + j];
@@ -698,8 +709,8 @@ __global__ __launch_bounds__(WR_NT, write_resident<T>()) void paged_write_kernel
 
     // ---- K and V: the segments that begin in this workgroup's rows
     __shared__ WriteShared sh;
-    const int kvh = kv_wg % Hkv, shift = a.kv.page_shift, P = 1 << shift;
-    const int row_lo = kv_wg / Hkv * a.chunk;
+    const int kvh = kv_at % Hkv, shift = a.kv.page_shift, P = 1 << shift;
+    const int row_lo = unit_row + kv_at / Hkv * a.chunk;
     const int64_t n_slots = (int64_t)a.kv.n_pages << shift;
     auto slot_of = [&](int row) { return row >= 0 && row < a.n_rows ? a.slot[row] : (int64_t)-1; };
     // the slots of 64 rows from row_lo on: `cuts` marks those that do not continue the row before them in its page
@@ -756,21 +767,27 @@ static int launch_write(compact_ctx* ctx, int n_rows, const void* qkv, const Pag
                         hipStream_t s) {
     const int Hq = ctx->cfg.n_q_heads, Hkv = ctx->cfg.n_kv_heads;
     constexpr int TPW = 64 / (HD / 16);
-    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 0, 0, 1};
+    WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 1, 1, 1, 1};
     // rows per workgroup of the K / V part: its segments of several rows follow each other, those of one row go side by side, and
     // a prompt leaves all but the first workgroup of a segment idle.  us, 32 + 8 heads of 128, pages of 64: 64 x 4 rows 11.2 by 4, 14.4 by 8,
-    // 61.5 by 64; 1024 rows of a prompt 14.3, 11.8, 11.5; 2 x 4096 52.5, 45.8, 41.3; 4 x 4096 97, 83, 78 (pages of 16: 84 by 16, 100 by 64)
+    // 61.5 by 64; 1024 rows of a prompt 14.3, 11.8, 11.5; 2 x 4096 52.5, 45.8, 41.3; 4 x 4096 97, 83, 78 (pages of 16: 84 by 16, 100 by 64); units of XCDs have since taken off 2 to 20 %
     a.chunk = n_rows <= 512 ? 4 : n_rows <= 8192 ? 8 : std::min(1 << kv.page_shift, 64);
-    const int64_t chunks = (n_rows + a.chunk - 1) / a.chunk, groups = (n_rows + TPW - 1) / TPW;
+    const int64_t groups = (n_rows + TPW - 1) / TPW;
     a.q_heads = (int)std::min<int64_t>(WR_QHEADS, std::max<int64_t>(1, groups * Hq / 4096));
-    const int64_t tasks = groups * ((Hq + a.q_heads - 1) / a.q_heads);
-    const int64_t kv_wgs = chunks * Hkv, wgs = kv_wgs + (tasks + WR_NT / 64 - 1) / (WR_NT / 64);
-    if (wgs >= INT32_MAX / WR_NT) return set_err(ctx, COMPACT_ESHAPE, "too many rows for one call");
-    // K and V first where all run at once (1950 rows of fp32 storage, 4 + 2 heads of 64: 6.9 us instead of 7.8), else evenly (see there)
+    auto workgroups = [&](int64_t unit) {   // with units of so many rows
+        const int64_t kv_wgs = (unit + a.chunk - 1) / a.chunk * Hkv, tasks = (unit + TPW - 1) / TPW * ((Hq + a.q_heads - 1) / a.q_heads);
+        const int64_t q_wgs = (tasks + WR_NT / 64 - 1) / (WR_NT / 64);
+        a.unit = (int)unit;
+        a.kv_wgs = (int)kv_wgs;
+        a.q_wgs = (int)q_wgs;
+        return (kv_wgs + q_wgs) * (unit < n_rows ? ((n_rows + unit - 1) / unit + 7) / 8 * 8 : 1);
+    };
+    // one unit where all run at once (1950 rows of fp32 storage, 4 + 2 heads of 64: 6.9 us instead of 7.5)
     int n_cus = 0;
     TRY_RC(device_cu_count(ctx, &n_cus));
-    a.n_kv_wgs = (int)kv_wgs;
-    a.kv_share = wgs <= write_resident<T>() * n_cus ? 1ull << 32 : (((uint64_t)kv_wgs << 32) + wgs - 1) / wgs;
+    int64_t wgs = workgroups(n_rows);
+    if (wgs > write_resident<T>() * n_cus) wgs = workgroups(std::max(a.chunk, 16));
+    if (wgs >= INT32_MAX / WR_NT) return set_err(ctx, COMPACT_ESHAPE, "too many rows for one call");
     paged_write_kernel<HD, T><<<(unsigned)wgs, WR_NT, 0, s>>>(a);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
