@@ -46,7 +46,7 @@ int paged_view(compact_ctx* ctx, const compact_paged_kv* kv, bool with_pages, Pa
 // device arrays hold, nothing outside them is touched.
 // Bound: up to some thousand rows by the launch and the chain of loads and scans (64 decode steps 5 us, 1024 of them 12); beyond
 // that by the angles, which are formed in 64 bits, a row's from the row before by a turn, and by the writes of 8 + 4 hd bytes
-// a row (8 x 4096 rows, 17 MB: 10 us; 512 requests with 36000 rows 14).
+// a row (8 x 4096 rows, 17 MB: 10 us; 512 requests with 37000 rows 14).
 // ---------------------------------------------------------------------------
 #define PLAN_NT 256
 
