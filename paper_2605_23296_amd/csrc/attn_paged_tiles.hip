@@ -61,9 +61,10 @@ __device__ __forceinline__ int next_place(const PagedAttnArgs& a, int mine, int 
     mine = __builtin_amdgcn_readfirstlane(*s_place);
     return mine < n ? mine : -1;
 }
-__device__ __forceinline__ Unit unit_at(const PagedAttnArgs& a, int mine, int units, int xcd_heads) {
+// `wave`: which 32 columns of the tile the wavefront owns
+__device__ __forceinline__ Unit unit_at(const PagedAttnArgs& a, int mine, int units, int xcd_heads, int wave) {
     Unit un;
-    const int r = threadIdx.x & 31, lane = threadIdx.x & 63, wave = wave_index(), x = blockIdx.x & 7;
+    const int r = threadIdx.x & 31, lane = threadIdx.x & 63, x = blockIdx.x & 7;
     const int G = a.Hq / a.Hkv, N = a.sched[SCHED_LISTED];
     const int32_t* before = a.sched + SCHED_UNITS;
     const int at = mine * (8 / xcd_heads) + x / xcd_heads;
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(256, 1) void attn_paged_tile_f32_kernel(const Paged
 
     const int n_mine = units_of_xcd(blockIdx.x & 7, units, Hkv, xcd_heads);
     for (int mine = -1; (mine = next_place(a, mine, n_mine, &s_place)) >= 0;) {
-        const Unit un = unit_at(a, mine, units, xcd_heads);
+        const Unit un = unit_at(a, mine, units, xcd_heads, wave_index());
         __syncthreads();   // (the tiles of the unit before have been read)
         const PagedReq& rq = un.rq;
         const int req = un.req, kvh = un.kvh, k_lo = un.k_lo, n_steps = un.n_steps;
@@ -327,6 +328,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedAttn
     const int units = a.sched[SCHED_UNITS + a.sched[SCHED_LISTED]];
     const int pi_r = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
     const float scale_log2 = a.scale_log2;
+    // (the other way round in the CU's second workgroup: tiles of up to 64 columns then load all four SIMDs)
+    const int columns = blockIdx.x < gridDim.x / 2 ? wave : 3 - wave;
 
     // LDS byte offsets of the fragments of a tile: K row pi_r (the second half 32 rows on, same swizzle), V^T row r
     int kfo[KK], vfo[4];
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedAttn
 
     const int n_mine = units_of_xcd(blockIdx.x & 7, units, Hkv, xcd_heads);
     for (int mine = -1; (mine = next_place(a, mine, n_mine, &s_place)) >= 0;) {
-        const Unit un = unit_at(a, mine, units, xcd_heads);
+        const Unit un = unit_at(a, mine, units, xcd_heads, columns);
         __syncthreads();   // (the tiles of the unit before have been read)
         const int kv = un.rq.kv, k_lo = un.k_lo, n_tiles = un.n_steps;
         floatx16 oacc[DT];
@@ -424,6 +427,43 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedAttn
 #pragma unroll
                     for (int wd = 0; wd < 4; ++wd) vreg[i][wd] &= low_bytes(live - v_gran * PAGED_GRAN - 4 * wd);
             };
+
+            // a wavefront without columns only stages
+            if (columns * 32 >= un.cols) {
+                int pid_k = in_range(load_pid(0)), pid_v = pid_k, pid_n = load_pid(1);
+                auto request = [&](int J) __attribute__((always_inline)) {   // K of tile J, V^T of tile J - 1
+                    ksb = k_ready(J, pid_k);
+                    vsb = v_ready(J - 1, pid_v);
+#pragma unroll
+                    for (int i = 0; i < NLD; ++i) {
+                        k_load(i);
+                        v_load(i);
+                    }
+                    pid_v = pid_k;
+                    pid_k = in_range(pid_n);
+                    pid_n = load_pid(J + 2);
+                };
+                ksb = k_ready(0, pid_k);
+#pragma unroll
+                for (int i = 0; i < NLD; ++i) k_load(i);
+                pid_k = in_range(pid_n);
+                pid_n = load_pid(2);
+#pragma unroll
+                for (int i = 0; i < NLD; ++i) k_put(0, i);
+                request(1);
+                tile_barrier();
+                for (int J = 1; J <= n_tiles; ++J) {
+                    v_trim(J - 1);
+#pragma unroll
+                    for (int i = 0; i < NLD; ++i) {
+                        k_put(J & 1, i);
+                        v_put((J - 1) & 1, i);
+                    }
+                    request(J + 1);
+                    tile_barrier();
+                }
+                continue;
+            }
 
             floatx16 se, so;      // S^T of two halves of 32 keys: column r, key 32 n + (e / 8) * 16 + h * 8 + e % 8
             uintx4 pe[2], po[2];  // their P^T
