@@ -13,10 +13,14 @@
 #define SCHED_ORDER (8 * SCHED_PITCH)                      // [listed] those requests
 #define SCHED_UNITS (SCHED_ORDER + PAGED_MAX_REQUESTS)     // [listed + 1] units before each of them
 #define SCHED_BYTES (sizeof(int32_t) * (SCHED_UNITS + PAGED_MAX_REQUESTS + 1))
-// A request of t tiles has its keys cut into pieces of 512 t to 1024 t rows: a chunk of few rows behind a long cache becomes enough
-// units for the card, one of many rows is not cut.  Finer pieces (as many as give 512 units) cost more in records than they
-// gain: 32 mixed requests 277 -> 589 us.
+// A request of t tiles has its keys cut into pieces of 512 t to 1024 t rows, and of 2048 to 4096 as long as that gives no more than
+// 64 units per KV head, which fill the card: a chunk of a prompt behind a long cache mostly comes alone or with single rows (256 rows behind
+// 8192, 32 + 8 heads of 128: 86 -> 61 us; 7 requests of up to 118 behind up to 12149 124 -> 101).  Where many come at once, the records of what
+// need not have been cut cost up to an eighth (32 x 250 rows behind 4000 to 8000: 843 -> 952), which a request may not know; with 1024 to 2048
+// rows it is a quarter, and with as many pieces as give 512 units in any case twice the time of 32 mixed requests.
 #define TILE_SPLIT 512
+#define TILE_LONG 2048
+#define TILE_FILL 64
 
 struct PagedAttnArgs {
     PagedView kv;
@@ -48,7 +52,7 @@ __device__ __forceinline__ bool is_few(int n, int group) { return n <= FEW_COLS 
 // pieces of a request's keys (at least one, so that a request without keys has somebody to write its zeros)
 __device__ __forceinline__ int few_pieces(int kv) { return max((kv + FEW_CHUNK - 1) / FEW_CHUNK, 1); }
 __device__ __forceinline__ int n_tiles(int n, int group) { return (int)(((int64_t)n * group + TILE_COLS - 1) / TILE_COLS); }
-__device__ __forceinline__ int tile_pieces(int tiles, int kv) { return max(kv / TILE_SPLIT / tiles, 1); }
+__device__ __forceinline__ int tile_pieces(int tiles, int kv) { return max(max(kv / TILE_SPLIT / tiles, min(kv / TILE_LONG, TILE_FILL / tiles)), 1); }
 // rows of a piece: the last piece may hold fewer
 __device__ __forceinline__ int tile_piece_rows(int pieces, int kv) {
     return ((kv + pieces - 1) / pieces + TILE_KEYS - 1) / TILE_KEYS * TILE_KEYS;

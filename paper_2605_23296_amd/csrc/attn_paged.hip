@@ -633,8 +633,8 @@ static int64_t record_stride(const compact_layer_cfg& c, int max_new, int max_kv
     int64_t few = 0, tiles = 0;
     const int chunks = (max_kv - 1) / FEW_CHUNK + 1;
     if (chunks > 1) few = (int64_t)std::min(max_new, FEW_COLS / G) * chunks;
-    // n rows in t = ceil(n G / 128) tiles, p = floor(kv / 512 t) >= 2 pieces: n p <= (128 t / G) (kv / 512 t)
-    if (has_tiles(c, max_new) && max_kv >= 2 * TILE_SPLIT) tiles = (int64_t)TILE_COLS * (max_kv / TILE_SPLIT + 1) / G + 1;
+    // n rows in t = ceil(n G / 128) tiles, t p <= max(kv / 512, 64) for p >= 2 pieces: n p <= (128 / G) max(kv / 512, 64)
+    if (has_tiles(c, max_new) && max_kv >= 2 * TILE_SPLIT) tiles = (int64_t)TILE_COLS * (std::max(max_kv / TILE_SPLIT, TILE_FILL) + 1) / G + 1;
     return std::max(few, tiles);
 }
 
@@ -679,8 +679,8 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     LAUNCH_CHECK(ctx);
     if (tiles) TRY_RC(launch_attn_paged_tiles(ctx, a, s));
     if (a.rec_stride == 0) return COMPACT_OK;
-    // rows of a request whose keys may be split: 512 t * 2 <= max_kv for its t tiles
-    const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * (a.max_kv / TILE_SPLIT / 2) / G + 1;
+    // rows of a request whose keys may be split: 2 t <= max(kv / 512, 64) for its t tiles
+    const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * std::max(a.max_kv / TILE_SPLIT, TILE_FILL) / 2 / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
     if (tiles) {
         const int64_t pairs = rows * a.kv.n_requests * c.n_q_heads;

@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedAttn
                     for (int wd = 0; wd < 4; ++wd) vreg[i][wd] &= low_bytes(live - v_gran * PAGED_GRAN - 4 * wd);
             };
 
-            // a wavefront without columns only stages
+            // a wavefront without columns only stages (80 requests of up to 60 rows behind up to 3000: 158 -> 149 us)
             if (columns * 32 >= un.cols) {
                 int pid_k = in_range(load_pid(0)), pid_v = pid_k, pid_n = load_pid(1);
                 auto request = [&](int J) __attribute__((always_inline)) {   // K of tile J, V^T of tile J - 1
