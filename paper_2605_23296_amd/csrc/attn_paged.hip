@@ -627,14 +627,17 @@ __global__ __launch_bounds__(256) void attn_paged_merge_share_kernel(const Paged
 
 static bool has_tiles(const compact_layer_cfg& c, int max_new) { return (int64_t)max_new * (c.n_q_heads / c.n_kv_heads) > FEW_COLS; }
 
+// t tiles in p >= 2 pieces: t p is at most this
+static int most_split(int max_kv) { return std::max(max_kv / TILE_SPLIT, max_kv >= 2 * TILE_LONG ? TILE_FILL : 0); }
+
 // row-pieces of a request that records are kept for; 0: no request of the call is split
 static int64_t record_stride(const compact_layer_cfg& c, int max_new, int max_kv) {
     const int G = c.n_q_heads / c.n_kv_heads;
     int64_t few = 0, tiles = 0;
     const int chunks = (max_kv - 1) / FEW_CHUNK + 1;
     if (chunks > 1) few = (int64_t)std::min(max_new, FEW_COLS / G) * chunks;
-    // n rows in t = ceil(n G / 128) tiles, t p <= max(kv / 512, 64) for p >= 2 pieces: n p <= (128 / G) max(kv / 512, 64)
-    if (has_tiles(c, max_new) && max_kv >= 2 * TILE_SPLIT) tiles = (int64_t)TILE_COLS * (std::max(max_kv / TILE_SPLIT, TILE_FILL) + 1) / G + 1;
+    // n rows in t = ceil(n G / 128) tiles: n p <= (128 / G) t p
+    if (has_tiles(c, max_new) && max_kv >= 2 * TILE_SPLIT) tiles = (int64_t)TILE_COLS * (most_split(max_kv) + 1) / G + 1;
     return std::max(few, tiles);
 }
 
@@ -679,8 +682,8 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     LAUNCH_CHECK(ctx);
     if (tiles) TRY_RC(launch_attn_paged_tiles(ctx, a, s));
     if (a.rec_stride == 0) return COMPACT_OK;
-    // rows of a request whose keys may be split: 2 t <= max(kv / 512, 64) for its t tiles
-    const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * std::max(a.max_kv / TILE_SPLIT, TILE_FILL) / 2 / G + 1;
+    // rows of a request whose keys may be split: 2 t <= t p for its t tiles
+    const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * most_split(a.max_kv) / 2 / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
     if (tiles) {
         const int64_t pairs = rows * a.kv.n_requests * c.n_q_heads;

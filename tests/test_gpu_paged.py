@@ -419,6 +419,21 @@ def test_long_caches(lc):
     check_attn(lc, q, run_attn(lay, kv, q, n_new, lens), n_new, lens, ref, table)
 
 
+@pytest.mark.parametrize("lc", [layer(2, 2, 64), layer(2, 2, 128), layer(2, 2, 64, "fp32"), layer(8, 1, 64)], ids=IDS)
+def test_long_chunks_in_pieces(lc):
+    """Chunks of many rows whose keys are cut: rows that see nothing of a later piece, lengths around the cut, beside one that is not cut."""
+    if lc.n_kv_heads == 2:
+        n_new, lens = [2000, 4090, 300, 300, 1, 60], [4100, 4096, 4095, 4096, 4200, 1000]
+    else:
+        n_new, lens = [300, 40, 3], [6500, 4500, 4097]
+    kv, ref, table = random_cache(lc, lens, 64, 16)
+    q, lay = queries(lc, sum(n_new), 16), handle(lc)
+    o = run_attn(lay, kv, q, n_new, lens)
+    check_attn(lc, q, o, n_new, lens, ref, table)
+    one = B.PagedKV(lc, kv.k, kv.v, kv.k_scale, kv.v_scale, kv.table[:1].contiguous())
+    assert torch.equal(run_attn(lay, one, q[:n_new[0]], n_new[:1], lens[:1]), o[:n_new[0]])
+
+
 @pytest.mark.parametrize("lc", [layer(8, 2, 128), layer(8, 2, 64), layer(4, 2, 64, "fp32")], ids=IDS)
 def test_large_scores_and_growing_maxima(lc):
     """Scores in the hundreds that grow along the keys: the running maximum moves at nearly every step."""
