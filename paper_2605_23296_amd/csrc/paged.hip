@@ -79,15 +79,18 @@ __device__ __forceinline__ int lane_before(int v) {
     return (threadIdx.x & 63) ? u : 0;
 }
 
-// the last i in 0 .. n - 1 with a[i] <= x (a[0] = 0 <= x, a does not decrease)
+// the last i in 0 .. n - 1 with a[i] <= x (a[0] = 0 <= x, a does not decrease), three places looked at side by side
 __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a[mid] <= x)
-            lo = mid;
-        else
-            hi = mid;
+        const int q = (hi - lo + 3) >> 2, m1 = lo + q, m2 = min(m1 + q, hi - 1), m3 = min(m2 + q, hi - 1);
+        const bool b1 = a[m1] <= x, b2 = a[m2] <= x, b3 = a[m3] <= x;
+        if (b3) {
+            lo = m3;
+        } else {
+            hi = b2 ? m3 : b1 ? m2 : m1;
+            lo = b2 ? m2 : b1 ? m1 : lo;
+        }
     }
     return lo;
 }
