@@ -8,14 +8,16 @@
 #define FEW_WAVES 4
 #define FEW_PLD (FEW_CHUNK + 8)   // bf16 per column of the probability tile (padded against bank conflicts)
 
-// inclusive sum over the wavefront's lanes
+// inclusive sum over the wavefront's lanes: inside rows of 16 lanes, then across them
 __device__ __forceinline__ int wave_prefix(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int ofs = 1; ofs < 64; ofs <<= 1) {
-        const int u = __shfl_up(v, ofs, 64);
-        if (lane >= ofs) v += u;
-    }
+#if defined(__HIP_DEVICE_COMPILE__)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast:31 to rows 2 and 3
+#endif
     return v;
 }
 // inclusive sum over the workgroup's threads; `red`: one int per wavefront
