@@ -388,7 +388,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(HD, NP, CT)) void attn
         for (int w = 0; w < CT; ++w)
 #pragma unroll
             for (int i = 0; i < RT; ++i) oacc[w][i] = floatx4{0.f, 0.f, 0.f, 0.f};
-        if (n_keys < FEW_CHUNK) {   // whatever lies behind the cached rows must not reach the MFMA
+        if (n_keys < FEW_CHUNK) {   // whatever lies behind the cached rows must not reach the MFMA, scales of pages that are nobody's included
+            if (r * PAGED_GRAN >= n_keys) vsb = 127;
 #pragma unroll
             for (int j = 0; j < VS; ++j)
 #pragma unroll
