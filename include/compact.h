@@ -317,7 +317,8 @@ int compact_prefix_stack_forward(compact_ctx* ctx, int32_t n_layers, const compa
  * Codes are E4M3 (OCP 8-bit floating point: no infinities, 0x7F / 0xFF = NaN), scales E8M0: a code c of a page and
  * KV head stands for c * 2^(scale - 127).  The scale of a page and head is the least power of two (>= 2^-126) that brings the
  * largest finite value written to it to at most 448; where a later row raises it, the page's codes are rounded to the new
- * scale once more.  The first row of a page starts it anew, whatever the page held before.
+ * scale once more.  The first row of a page starts it anew, whatever the page held before.  Values of more than 240 * 2^120 in
+ * size are cached as that: the next code stands for 2^128, which is no bf16 or fp32 number.
  * Page sizes: page_rows in {16, 32, 64, 128}.  Both storage types; d_k and d_v must be 16-byte aligned.                    */
 typedef struct compact_paged_kv {
     void*    d_k;          /* uint8 [n_pages][Hkv][page_rows][hd], after rotary embedding */
@@ -369,6 +370,7 @@ int compact_rope_paged_write(compact_ctx* ctx, int32_t n_rows, const void* d_qkv
  * where that is none.  One row per request is a decode step, more a prompt or a chunk of one; both may share a call.
  * max_new and max_kv_len bound n and d_kv_len (rows of requests with more are not computed rightly; nothing outside the
  * buffers is touched).  q rows are q_stride elements apart (>= Dq, a multiple of 8), o is [n_rows, Dq]; both 16-byte aligned.
+ * Sums are fp32: V values near the top of the range may come out as infinities in rows that see them, and in no other.
  * Rows that belong to no request are left as they are.  How a request's keys are split depends on its own lengths
  * alone: its results do not depend on the other requests.  The workspace must hold compact_paged_workspace_bytes(...). */
 int compact_paged_workspace_bytes(const compact_ctx* ctx, int32_t n_requests, int32_t n_rows, int32_t max_new,

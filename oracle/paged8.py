@@ -8,7 +8,8 @@ Element (8 bits, E4M3 of the OCP 8-bit floating point format: S EEEE MMM, expone
     E = 0         : (-1)^S * M * 2^-9
     E = 1..15     : (-1)^S * (1 + M/8) * 2^(E - 7), except E = 15, M = 7: NaN; no infinities; the largest value is 448
 Scale (8 bits, E8M0): 2^(e - 127), one per page and KV head for K and for V.  Of the values written to a page so far that
-are finite, the largest in size is at most 448 scales, and e (>= 1) is the least for which that holds."""
+are finite, the largest in size is at most 448 scales, and e (>= 1) is the least for which that holds.  Finite sizes above TOP are
+written as TOP, since the next value, 2^128, is none of bf16 or fp32."""
 import numpy as np
 
 from oracle.layer import gqa_attention
@@ -23,6 +24,7 @@ def e4m3_value(code):
 
 
 VALUES = np.array([e4m3_value(c) for c in range(256)])
+TOP = 240.0 * 2.0 ** 120
 _SIZES = VALUES[:127]      # the sizes there are, ascending
 
 
@@ -119,7 +121,7 @@ class Pages:
                         y = np.where(bad[rows, h][:, None], np.nan, y)
                     else:
                         y = np.where(np.isfinite(y), y, 0.0)
-                    c[at] = to_e4m3(y / 2.0 ** float(new - 127))
+                    c[at] = to_e4m3(np.clip(y, -TOP, TOP) / 2.0 ** float(new - 127))
 
     def rows(self, name, table_row, n):
         """The first n cached rows of a request, [n, heads, hd]."""

@@ -54,6 +54,11 @@ __device__ __forceinline__ unsigned recode4(unsigned w, float down) {
 // a mask of the first n bytes of a word (none for n <= 0, all for n >= 4)
 __device__ __forceinline__ unsigned low_bytes(int n) { return n >= 4 ? 0xFFFFFFFFu : (1u << 8 * max(n, 0)) - 1u; }
 
+// The largest size that is cached, 240 * 2^120: the next code at that scale, 256, is 2^128, which neither bf16 nor fp32 has.  The bits
+// of a float (and, in the upper half, of a bf16).
+#define TOP_BITS 0x7F700000u
+#define TOP_BYTE 247   // its scale
+
 // E8M0 byte of the least 2^e with amax <= 448 * 2^e = 1.75 * 2^(e + 8), at least 1; amax is finite and not negative
 __device__ __forceinline__ int scale_byte(float amax) {
     const unsigned u = __builtin_bit_cast(unsigned, amax);

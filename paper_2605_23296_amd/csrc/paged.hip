@@ -350,6 +350,13 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Raw {
         else
             w[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
     }
+    // the same sign, the size of the given bits (which the type has)
+    __device__ __forceinline__ void set_size(int i, unsigned size) {
+        if constexpr (sizeof(T) == 4)
+            w[i] = (w[i] & 0x80000000u) | size;
+        else
+            w[i >> 1] = i & 1 ? (w[i >> 1] & 0x8000FFFFu) | size : (w[i >> 1] & 0xFFFF8000u) | size >> 16;
+    }
     __device__ __forceinline__ void as_they_are() {
 #pragma unroll
         for (unsigned i = 0; i < sizeof(T) * N / 4; ++i) w[i] = (unsigned)here((int)w[i]);
@@ -367,6 +374,15 @@ __device__ __forceinline__ void rotate_closely(float lo, float hi, float c, floa
 // Sizes as the bits of a float without its sign: they order like the values, and what is not finite lies at INF_BITS and above.
 #define INF_BITS 0x7F800000u
 __device__ __forceinline__ unsigned size_bits(float x) { return __builtin_bit_cast(unsigned, x) & 0x7FFFFFFFu; }
+// a finite value within the sizes that are cached
+__device__ __forceinline__ float below_top(float x) {
+    const float top = __builtin_bit_cast(float, TOP_BITS);
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_fmed3f(x, -top, top);
+#else
+    return x;
+#endif
+}
 __device__ __forceinline__ unsigned wave_max_bits(unsigned v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o, 64));
@@ -466,6 +482,10 @@ __device__ __forceinline__ void write_k(const WriteArgs<T>& a, const Segment& sg
             if (j < sg.n) {
                 float lo[8], hi[8];
                 rotated(g, j, lo, hi);
+                if (__builtin_amdgcn_readfirstlane(byte) >= TOP_BYTE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) lo[e] = below_top(lo[e]), hi[e] = below_top(hi[e]);
+                }
                 uintx2 wl = {to_codes4(lo[0] * up, lo[1] * up, lo[2] * up, lo[3] * up), to_codes4(lo[4] * up, lo[5] * up, lo[6] * up, lo[7] * up)};
                 uintx2 wh = {to_codes4(hi[0] * up, hi[1] * up, hi[2] * up, hi[3] * up), to_codes4(hi[4] * up, hi[5] * up, hi[6] * up, hi[7] * up)};
                 if (is_bad(sh, j)) wl = wh = uintx2{0x7F7F7F7Fu, 0x7F7F7F7Fu};
@@ -493,7 +513,7 @@ __device__ __forceinline__ void write_v(const WriteArgs<T>& a, const Segment& sg
     uint8_t* vp = a.kv.v + (sg.ph << shift) * HD;
     const int g_lo = sg.o / PAGED_GRAN, g_end = (sg.o + sg.n + PAGED_GRAN - 1) / PAGED_GRAN;
     auto place = [&](int g, int e) { return reinterpret_cast<uintx4*>(vp + (((unsigned)(d + e) << shift) + g * PAGED_GRAN)); };
-    Four x[PAGED_GRAN];   // the rows of a granule (in place of those that are not in the segment: the nearest one); 0 for what is not finite
+    Four x[PAGED_GRAN];   // the rows of a granule (in place of those that are not in the segment: the nearest one); 0 for what is not finite, no more than the top
     // returns the lane's largest finite size
     auto load = [&](int g) {
         unsigned mine = 0;
@@ -505,8 +525,8 @@ __device__ __forceinline__ void write_v(const WriteArgs<T>& a, const Segment& sg
 #pragma unroll
                 for (int e = 0; e < 4; ++e) mine = max(mine, size_bits(x[u].at(e)));
         }
-        if (__any(mine >= INF_BITS)) {
-            if (mine >= INF_BITS) {
+        if (__any(mine > TOP_BITS)) {
+            if (mine > TOP_BITS) {
                 mine = 0;
 #pragma unroll
                 for (int u = 0; u < PAGED_GRAN; ++u)
@@ -518,6 +538,7 @@ __device__ __forceinline__ void write_v(const WriteArgs<T>& a, const Segment& sg
                             atomicOr(&sh.bad[j >> 5], 1u << (j & 31));
                             x[u].clear(e);
                         } else {
+                            if (size > TOP_BITS) x[u].set_size(e, TOP_BITS);
                             mine = max(mine, size);
                         }
                     }
@@ -596,13 +617,13 @@ __device__ __forceinline__ void write_single(const WriteArgs<T>& a, int row, int
         const unsigned size = size_bits(f);
         bad |= size >= INF_BITS;
         top = max(top, size < INF_BITS ? size : 0u);
-        return size < INF_BITS ? f : 0.f;
+        return size < INF_BITS ? below_top(f) : 0.f;
     };
 #pragma unroll
     for (int e = 0; e < 4; ++e) rotate_closely(x.at(e), y.at(e), cs.at(2 * e), cs.at(2 * e + 1), k[e], k[4 + e]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        see(k[e], k_top);
+        k[e] = see(k[e], k_top);
         val[e] = see(v.at(e), v_top);
     }
 #pragma unroll

@@ -1,9 +1,10 @@
-"""Paged cache in 8 bits at the edges of what its calls accept: requests without cached rows beside pages that hold anything."""
+"""Paged cache in 8 bits at the edges of what its calls accept: requests without cached rows beside pages that hold anything, and
+values at the top of the range."""
 import pytest
 import torch
 
 from paper_2605_23296_amd import binding as B
-from tests.test_gpu_paged import ATTN_LAYERS, IDS, check_attn, handle, queries, random_cache, run_attn
+from tests.test_gpu_paged import ATTN_LAYERS, DEV, IDS, check_attn, handle, ints, layer, queries, random_cache, run_attn, tdtype
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +34,49 @@ def test_requests_without_cached_rows_give_zeros(lc, n_new, lens, entry):
     check_attn(lc, q, o, n_new, lens, ref, table)
     for rows, L in zip(torch.split(o, n_new), lens):
         assert L > 0 or (rows == 0).all()
+
+
+@pytest.mark.parametrize("lc", [layer(8, 2, 128), layer(8, 2, 64), layer(4, 2, 64, "fp32"), layer(4, 2, 128, "fp32")], ids=IDS)
+@pytest.mark.parametrize("T,n,at", [(290, 1, None), (290, 3, 288), (66, 4, 64), (200, 200, 96), (700, 130, 640)])
+@pytest.mark.parametrize("name", ["k", "v"])
+def test_the_largest_finite_values_leave_rows_that_do_not_see_them_alone(lc, T, n, at, name):
+    """A cached row (the first one of a page) with the storage type's largest values in one KV head: what is read back is finite and within
+    a code's rounding, and the rows before it have the bits that they have beside an ordinary row."""
+    H, Hq, hd, P, dt = lc.n_kv_heads, lc.n_q_heads, lc.head_dim, 32, tdtype(lc)
+    big, lay = torch.finfo(dt).max, handle(lc)
+    g = torch.Generator().manual_seed(22)
+    plain = torch.randn((T, Hq + 2 * H, hd), generator=g).to(dt)
+    at = T - 1 if at is None else at
+    large = plain.clone()
+    if name == "k":      # (its rotation stays within the type: the other half is 0)
+        large[at, Hq + 1] = 0.0
+        large[at, Hq + 1, :2] = torch.tensor([big, -big])
+    else:
+        large[at, Hq + H + 1, :4] = torch.tensor([big, -big, big / 2, 248 * 2.0 ** 120])
+    out = []
+    for x in (plain, large):
+        kv = B.PagedKV.allocate(lc, 1, -(-T // P), -(-T // P), P, DEV)
+        for t in (kv.k, kv.v, kv.k_scale, kv.v_scale):
+            t.fill_(0x7F)
+        st = B.PagedStep(lc, 1, T, DEV, n_pages=kv.n_pages, n_new=ints([T]))
+        lay.compact_paged_plan(kv, st)
+        q = torch.empty((T, Hq * hd), dtype=dt, device=DEV)
+        # (a single row is written by itself: T = 290 and n = 1 is a decode step behind 289 rows)
+        cut = T - 1 if n == 1 else T
+        for lo, hi in ((0, cut), (cut, T)):
+            if lo < hi:
+                lay.compact_rope_paged_write(x[lo:hi].reshape(hi - lo, -1).to(DEV), kv, st.slot[lo:hi], st.rot[lo:hi], q[lo:hi])
+        cached = kv.rows(0, T)
+        assert torch.isfinite(cached[0]).all() and torch.isfinite(cached[1]).all()
+        out.append(run_attn(lay, kv, q[T - n:], [n], [T]))
+    got = cached[name == "v"][at, 1].cpu()
+    if name == "v":
+        # half a step of E4M3 is 2^-4 of the value; the top of the range is cut off at 240 * 2^120, less than 2^-4 (1/16) below the largest
+        assert ((got[:4] - large[at, Hq + H + 1, :4].float()).abs() <= 2.0 ** -4 * large[at, Hq + H + 1, :4].float().abs()).all()
+    before = max(at - (T - n), 0)
+    assert torch.equal(out[1][:before], out[0][:before]) and torch.isfinite(out[0]).all()
+    if n > 1:
+        assert before > 0
+    # the other KV head never sees it
+    half = Hq // H * hd
+    assert torch.equal(out[1][:, :half], out[0][:, :half])
