@@ -346,7 +346,7 @@ typedef struct compact_paged_step {
     int32_t*       d_cu;         /* [N + 1] first packed row of every request (2^31 - 1 where it is more) */
     int64_t*       d_slot;       /* [max_rows] page * page_rows + row in the page; -1 = nowhere */
     float*         d_rot;        /* [max_rows][hd / 2][2] cos and sin of the row's rotary angles */
-    int32_t        max_rows;     /* rows of the packed batch; those past d_cu[N] get slot -1 and position 0 */
+    int32_t        max_rows;     /* rows of the packed batch, at most 2^26; those past d_cu[N] get slot -1 and position 0 */
 } compact_paged_step;
 
 /* Plans one step: block table, slot map and rotary table from the lengths, in one launch.  Finished requests (d_n_new < 0)
@@ -354,7 +354,7 @@ typedef struct compact_paged_step {
  * adds rows takes what it lacks, in the order of requests, the first missing page from the top of the stack.  A request is
  * refused as a whole -- its length stays, its rows get slot -1, its d_kv_len is 0 -- when its rows end beyond max_rows or max_pages, or
  * when its pages and those of the requests before it (granted or not) are more than there are.  Table columns that the step does not fill
- * and stack entries above the old and the new top are left as they are.  COMPACT_ESHAPE beyond 4096 requests. */
+ * and stack entries above the old and the new top are left as they are.  COMPACT_ESHAPE beyond 4096 requests or 2^26 rows. */
 int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, const compact_paged_step* step, void* hip_stream);
 
 /* Rows of a packed qkv [n_rows, Dq + 2 Dkv]: q rotated to d_q [n_rows, Dq], k rotated and v into the pages at d_slot (slots

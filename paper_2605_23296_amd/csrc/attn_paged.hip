@@ -653,7 +653,7 @@ static int check_bounds(compact_ctx* ctx, int n_requests, int n_rows, int max_ne
     if (n_requests < 1 || n_rows < 0 || max_new < 1 || max_kv_len < 1)
         return set_err(ctx, COMPACT_EINVAL, "n_requests >= 1, n_rows >= 0, max_new >= 1, max_kv_len >= 1 required");
     if (n_requests > PAGED_MAX_REQUESTS) return set_err(ctx, COMPACT_ESHAPE, "more than 4096 requests");
-    if (n_rows > 1 << 26) return set_err(ctx, COMPACT_ESHAPE, "n_rows must be at most 2^26");
+    if (n_rows > PAGED_MAX_ROWS) return set_err(ctx, COMPACT_ESHAPE, "n_rows must be at most 2^26");
     return COMPACT_OK;
 }
 

@@ -2,7 +2,8 @@
 #pragma once
 #include "common.h"
 
-#define PAGED_MAX_REQUESTS 4096   // the plan keeps three numbers per request in LDS
+#define PAGED_MAX_REQUESTS 4096   // the plan keeps four numbers per request in LDS
+#define PAGED_MAX_ROWS (1 << 26)  // rows of a step: a plan's threads and the units of an attention are counted in 32 bits
 #define PAGED_GRAN 16             // rows of a granule: a 16-byte piece of a V row, never across pages
 
 struct PagedView {

@@ -216,9 +216,9 @@ __global__ __launch_bounds__(PLAN_NT) void paged_plan_kernel(const PlanArgs a) {
             st.d_n_refused[0] = s_refused;
         }
     }
-    const int gt = blockIdx.x * PLAN_NT + t, all = gridDim.x * PLAN_NT;
-    for (int v = n_free + gt; v < left; v += all) st.d_free[v] = stack(v);
-    for (int k = gt; k < taken; k += all) {   // the k-th page from the top of the stack
+    const unsigned gt = blockIdx.x * PLAN_NT + t, all = gridDim.x * PLAN_NT;   // (at most 2^28: the sums below stay inside 32 bits)
+    for (unsigned v = n_free + gt; v < (unsigned)left; v += all) st.d_free[v] = stack(v);
+    for (unsigned k = gt; k < (unsigned)taken; k += all) {   // the k-th page from the top of the stack
         const int i = last_at_most(want, N + 1, k);
         a.kv.table[(size_t)i * width + pages(len[i]) + (k - want[i])] = stack(total - 1 - k);
     }
@@ -275,7 +275,7 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
         !step->d_len_out || !step->d_kv_len || !step->d_cu || !step->d_slot || !step->d_rot)
         return set_err(ctx, COMPACT_EINVAL, "null array in the step");
     if (step->max_rows < 1) return set_err(ctx, COMPACT_EINVAL, "max_rows must be >= 1");
-    if (step->max_rows > 1 << 30) return set_err(ctx, COMPACT_ESHAPE, "max_rows must be at most 2^30");
+    if (step->max_rows > PAGED_MAX_ROWS) return set_err(ctx, COMPACT_ESHAPE, "max_rows must be at most 2^26");
     if (step->d_len == step->d_len_out || step->d_len == step->d_kv_len || step->d_n_new == step->d_len_out || step->d_n_new == step->d_kv_len ||
         step->d_n_free == step->d_n_free_out || step->d_n_free == step->d_n_refused || step->d_len_out == step->d_kv_len ||
         step->d_n_free_out == step->d_n_refused)

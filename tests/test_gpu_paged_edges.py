@@ -1,5 +1,5 @@
-"""Paged cache in 8 bits at the edges of what its calls accept: requests without cached rows beside pages that hold anything, and
-values at the top of the range."""
+"""Paged cache in 8 bits at the edges of what its calls accept: requests without cached rows beside pages that hold anything,
+values at the top of the range, stacks of as many pages as there are numbers."""
 import pytest
 import torch
 
@@ -80,3 +80,24 @@ def test_the_largest_finite_values_leave_rows_that_do_not_see_them_alone(lc, T, 
     # the other KV head never sees it
     half = Hq // H * hd
     assert torch.equal(out[1][:, :half], out[0][:, :half])
+
+
+@pytest.mark.parametrize("used", [0, 1, 5])
+def test_a_stack_of_2_to_the_31_pages(used):
+    """Places on the stack of free pages up to the largest int: pages are taken from its top, and a finished request's are pushed there."""
+    lc, n_pages = layer(4, 2, 64), 2 ** 31 - 1
+    lay, empty = handle(lc), torch.empty(0, dtype=torch.uint8, device=DEV)
+    free = torch.empty(n_pages, dtype=torch.int32, device=DEV)
+    n_free = n_pages - used
+    free[n_free - 8:] = torch.arange(n_free - 8, n_pages, dtype=torch.int64, device=DEV).int()
+    table = ints([[-1] * 8, list(range(100, 100 + used)) + [-1] * (8 - used), [-1] * 8])
+    kv = B.PagedKV(lc, empty, empty, empty, empty, table, n_pages=n_pages, page_rows=16)
+    st = B.PagedStep(lc, 3, 64, DEV, n_new=ints([33, -1, 0]), len=ints([0, 16 * used, 0]), free=free, n_free=ints([n_free]))
+    lay.compact_paged_plan(kv, st)
+    stack = list(range(n_free - 8, n_free)) + list(range(100, 100 + used))     # the top of it
+    assert kv.table[0].tolist() == stack[:-4:-1] + [-1] * 5
+    assert st.n_free_out.item() == n_pages - 3 and st.n_refused.item() == 0 and st.len_out.tolist() == [33, 0, 0]
+    # (entries above the new top are not written)
+    assert free[n_free - 8:n_pages - 3].tolist() == stack[:-3]
+    assert free[n_pages - 3:].tolist() == list(range(n_pages - 3, n_pages))
+    assert st.slot[:33].tolist() == [stack[-1 - r // 16] * 16 + r % 16 for r in range(33)] and (st.slot[33:] == -1).all()
