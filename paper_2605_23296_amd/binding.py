@@ -138,14 +138,23 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _addr(t):
-    assert t.is_contiguous()
+def _refuse(detail):
+    raise CompactError(1, detail)
+
+
+def _array(t, dtype, n, device, name):
+    """Address of an array of at least n elements that a kernel on `device` may use as they lie there."""
+    if t.dtype is not dtype or t.numel() < n or t.get_device() != device or not t.is_contiguous():
+        _refuse("%s: %s %s on %s%s; contiguous %s, at least %d elements, on the current GPU needed"
+                % (name, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous", dtype, n))
     return t.data_ptr()
 
 
-def _raw_stream():
-    # (0.3 us; torch.cuda.current_stream().cuda_stream takes 2.7, half of a small call)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+def _raw_stream(device):
+    try:      # (0.1 us; the public way takes 2.7, half of a small call)
+        return torch._C._cuda_getCurrentRawStream(device)
+    except AttributeError:
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def _i32arr(vals):
@@ -209,10 +218,14 @@ class PagedKV:
         self.n_requests, self.max_pages = table.shape
         if k.numel():
             pages, rows = (self.n_pages, layer.n_kv_heads), (self.page_rows, layer.head_dim)
-            assert tuple(k.shape) == pages + rows and tuple(v.shape) == pages + rows[::-1], (k.shape, v.shape)
-            assert tuple(k_scale.shape) == pages and tuple(v_scale.shape) == pages, (k_scale.shape, v_scale.shape)
-        assert all(x.dtype == torch.uint8 and x.is_contiguous() for x in (k, v, k_scale, v_scale))
-        assert table.dtype == torch.int32 and table.is_contiguous()
+            for name, shape in (("k", pages + rows), ("v", pages + rows[::-1]), ("k_scale", pages), ("v_scale", pages)):
+                if tuple(getattr(self, name).shape) != shape:
+                    _refuse("pages: %s is %s, %s needed" % (name, tuple(getattr(self, name).shape), shape))
+        self.device = table.get_device()
+        for name in ("k", "v", "k_scale", "v_scale"):
+            _array(getattr(self, name), torch.uint8, 0, self.device, "pages: " + name)
+        _array(table, torch.int32, 0, self.device, "block table")
+        self.heads = (layer.n_kv_heads, layer.head_dim)
         self.c = PagedKVStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), self.n_pages,
                                self.page_rows, self.max_pages, self.n_requests)
         self.ref = C.byref(self.c)
@@ -250,7 +263,7 @@ class PagedStep:
         self.len_out, self.kv_len, self.cu = ints(n_requests), ints(n_requests), ints(n_requests + 1)
         self.slot = torch.empty(max_rows, dtype=torch.int64, device=device)
         self.rot = torch.empty((max_rows, layer.head_dim // 2, 2), dtype=torch.float32, device=device)
-        self.n_requests, self.max_rows = n_requests, max_rows
+        self.n_requests, self.max_rows, self.head_dim = n_requests, max_rows, layer.head_dim
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
@@ -258,11 +271,15 @@ class PagedStep:
 
     def struct(self):
         if self._c is None:
-            arrays = (self.n_new, self.len, self.n_free, self.free, self.n_free_out, self.n_refused, self.len_out, self.kv_len, self.cu,
-                      self.slot, self.rot)
-            assert self.n_new.numel() == self.n_requests and self.len.numel() == self.n_requests
-            assert all(x.is_contiguous() and x.dtype == d for x, d in zip(arrays, [torch.int32] * 9 + [torch.int64, torch.float32]))
-            object.__setattr__(self, "_c", PagedStepStruct(*[x.data_ptr() for x in arrays], self.max_rows))
+            N, i32, device = self.n_requests, torch.int32, self.n_new.get_device()
+            if self.n_new.numel() != N or self.len.numel() != N:
+                _refuse("step: %d requests, n_new of %d, len of %d" % (N, self.n_new.numel(), self.len.numel()))
+            arrays = (("n_new", i32, N), ("len", i32, N), ("n_free", i32, 1), ("free", i32, 0), ("n_free_out", i32, 1), ("n_refused", i32, 1),
+                      ("len_out", i32, N), ("kv_len", i32, N), ("cu", i32, N + 1), ("slot", torch.int64, self.max_rows),
+                      ("rot", torch.float32, self.max_rows * self.head_dim))
+            c = PagedStepStruct(*[_array(getattr(self, name), dtype, n, device, "step: " + name) for name, dtype, n in arrays], self.max_rows)
+            for name, value in (("device", device), ("n_stack", self.free.numel()), ("_c", c)):
+                object.__setattr__(self, name, value)
         return self._c
 
     def advance(self):
@@ -289,6 +306,8 @@ class Layer:
             setattr(self.w, name, t.data_ptr() if t is not None else None)
         self.ws = None
         self.torch_dtype = torch.bfloat16 if layer.dtype == "bf16" else torch.float32
+        self.kv_heads = (layer.n_kv_heads, layer.head_dim)
+        self.q_cols, self.qkv_cols = layer.n_q_heads * layer.head_dim, (layer.n_q_heads + 2 * layer.n_kv_heads) * layer.head_dim
 
     def close(self):
         if self.ctx:
@@ -425,13 +444,40 @@ class Layer:
                                                      C.byref(tails.c), _ptr(o), wsp, wsn, _stream()))
 
     # -- paged cache in 8 bits ------------------------------------------------------
+    # The kernels go by the sizes they are told, so every array is held against them here.  The comparisons are written out: with a
+    # function call per array they cost 1.0 us a call instead of 0.7, of the 7 to 8 that a small one takes.
+    def _fits(self, kv, device):
+        if kv.heads != self.kv_heads or kv.device != device:
+            _refuse("pages for %s KV heads x head_dim on device %d; the layer has %s, the current device is %d" % (kv.heads, kv.device, self.kv_heads, device))
+
     def compact_paged_plan(self, kv, step):
-        assert step.n_requests == kv.n_requests and step.free.numel() >= kv.n_pages
-        self.check(self.L.compact_paged_plan(self.ctx, kv.ref, C.byref(step.struct()), _raw_stream()))
+        device, st = torch.cuda.current_device(), step.struct()
+        if step.n_requests != kv.n_requests or step.n_stack < kv.n_pages or step.head_dim != self.kv_heads[1] or kv.device != device or step.device != device:
+            _refuse("step of %d requests, a stack of %d pages and head_dim %d on device %d; the cache has %d, %d, %d on device %d, the current device is %d"
+                    % (step.n_requests, step.n_stack, step.head_dim, step.device, kv.n_requests, kv.n_pages, self.kv_heads[1], kv.device, device))
+        rc = self.L.compact_paged_plan(self.ctx, kv.ref, C.byref(st), _raw_stream(device))
+        if rc:
+            self.check(rc)
 
     def compact_rope_paged_write(self, qkv, kv, slot, rot, q):
-        """qkv [rows, Dq + 2 Dkv] -> q [rows, Dq] (rotated), k and v into kv's pages at slot [rows]."""
-        self.check(self.L.compact_rope_paged_write(self.ctx, qkv.shape[0], _addr(qkv), kv.ref, _addr(slot), _addr(rot), _addr(q), _raw_stream()))
+        """qkv [rows, Dq + 2 Dkv] -> q [rows, Dq] (rotated), k and v into kv's pages at slot [rows]; rot [rows, hd / 2, 2].  slot, rot and
+        q may have more rows."""
+        device, dt, shape = torch.cuda.current_device(), self.torch_dtype, qkv.shape
+        rows = shape[0]
+        if (len(shape) != 2 or shape[1] != self.qkv_cols or kv.heads != self.kv_heads or kv.device != device
+                or qkv.dtype is not dt or qkv.get_device() != device or not qkv.is_contiguous()
+                or slot.dtype is not torch.int64 or slot.numel() < rows or slot.get_device() != device or not slot.is_contiguous()
+                or rot.dtype is not torch.float32 or rot.numel() < rows * self.kv_heads[1] or rot.get_device() != device or not rot.is_contiguous()
+                or q.dtype is not dt or q.numel() < rows * self.q_cols or q.get_device() != device or not q.is_contiguous()):
+            self._fits(kv, device)
+            _array(qkv, dt, 0, device, "qkv")
+            _array(slot, torch.int64, rows, device, "slot")
+            _array(rot, torch.float32, rows * self.kv_heads[1], device, "rot")
+            _array(q, dt, rows * self.q_cols, device, "q")
+            _refuse("qkv: %s, [rows, %d] needed" % (tuple(qkv.shape), self.qkv_cols))
+        rc = self.L.compact_rope_paged_write(self.ctx, rows, qkv.data_ptr(), kv.ref, slot.data_ptr(), rot.data_ptr(), q.data_ptr(), _raw_stream(device))
+        if rc:
+            self.check(rc)
 
     def paged_workspace_bytes(self, n_requests, n_rows, max_new, max_kv_len):
         n = C.c_size_t()
@@ -445,12 +491,25 @@ class Layer:
         return self.ws
 
     def compact_attn_paged(self, q, kv, cu, kv_len, max_new, max_kv_len, o):
-        """q [rows, >= Dq] (its rows may be apart), o [rows, Dq]."""
-        rows, stride = q.shape[0], q.stride()
-        assert stride[1] == 1
-        ws = self.ws
-        self.check(self.L.compact_attn_paged(self.ctx, kv.ref, rows, _addr(cu), _addr(kv_len), max_new, max_kv_len, q.data_ptr(), stride[0],
-                                             _addr(o), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream()))
+        """q [rows, >= Dq] (its rows may be apart), o [rows, Dq], cu [n_requests + 1], kv_len [n_requests].  The workspace is self.ws."""
+        device, dt, shape, apart, ws, N = torch.cuda.current_device(), self.torch_dtype, q.shape, q.stride(), self.ws, kv.n_requests
+        rows = shape[0]
+        if (len(shape) != 2 or shape[1] < self.q_cols or apart[1] != 1 or kv.heads != self.kv_heads or kv.device != device
+                or q.dtype is not dt or q.get_device() != device
+                or cu.dtype is not torch.int32 or cu.numel() <= N or cu.get_device() != device or not cu.is_contiguous()
+                or kv_len.dtype is not torch.int32 or kv_len.numel() < N or kv_len.get_device() != device or not kv_len.is_contiguous()
+                or o.dtype is not dt or o.numel() < rows * self.q_cols or o.get_device() != device or not o.is_contiguous()
+                or ws is not None and ws.get_device() != device):
+            self._fits(kv, device)
+            _array(cu, torch.int32, N + 1, device, "cu")
+            _array(kv_len, torch.int32, N, device, "kv_len")
+            _array(o, dt, rows * self.q_cols, device, "o")
+            _refuse("q: %s %s with strides %s on %s, workspace on %s; [rows, %d] of %s on the current GPU needed"
+                    % (q.dtype, tuple(q.shape), q.stride(), q.device, ws if ws is None else ws.device, self.q_cols, dt))
+        rc = self.L.compact_attn_paged(self.ctx, kv.ref, rows, cu.data_ptr(), kv_len.data_ptr(), max_new, max_kv_len, q.data_ptr(), apart[0],
+                                       o.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream(device))
+        if rc:
+            self.check(rc)
 
     # -- profiling --------------------------------------------------------------
     def compact_profile_select(self, klass):

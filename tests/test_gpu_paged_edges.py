@@ -1,5 +1,5 @@
 """Paged cache in 8 bits at the edges of what its calls accept: requests without cached rows beside pages that hold anything,
-values at the top of the range, stacks of as many pages as there are numbers."""
+values at the top of the range, stacks of as many pages as there are numbers, arrays that are not on the GPU."""
 import pytest
 import torch
 
@@ -101,3 +101,34 @@ def test_a_stack_of_2_to_the_31_pages(used):
     assert free[n_free - 8:n_pages - 3].tolist() == stack[:-3]
     assert free[n_pages - 3:].tolist() == list(range(n_pages - 3, n_pages))
     assert st.slot[:33].tolist() == [stack[-1 - r // 16] * 16 + r % 16 for r in range(33)] and (st.slot[33:] == -1).all()
+
+
+def test_arrays_on_the_host_are_refused():
+    """One array of a call on the CPU, the others where they belong: nothing is launched."""
+    lc = layer(8, 2, 64)
+    lay, kv, st = handle(lc), B.PagedKV.allocate(lc, 3, 4, 12, 16, DEV), B.PagedStep(lc, 3, 5, DEV, n_pages=12)
+    lay.ensure_paged_workspace(3, 5, 2, 64, DEV)
+    qkv, q, o = (torch.zeros((5, n), dtype=torch.bfloat16, device=DEV) for n in (768, 512, 512))
+
+    def calls(qkv=qkv, slot=st.slot, rot=st.rot, q=q, cu=st.cu, kv_len=st.kv_len, o=o, kv=kv):
+        lay.compact_rope_paged_write(qkv, kv, slot, rot, q)
+        lay.compact_attn_paged(q, kv, cu, kv_len, 2, 64, o)
+    lay.compact_paged_plan(kv, st)
+    calls()
+    for name, t in dict(qkv=qkv, slot=st.slot, rot=st.rot, q=q, cu=st.cu, kv_len=st.kv_len, o=o).items():
+        with pytest.raises(B.CompactError) as e:
+            calls(**{name: t.cpu()})
+        assert e.value.code == 1, name
+    for name in ("n_new", "len", "n_free", "free", "n_free_out", "n_refused", "len_out", "kv_len", "cu", "slot", "rot"):
+        bad = B.PagedStep(lc, 3, 5, DEV, n_pages=12)
+        setattr(bad, name, getattr(bad, name).cpu())
+        with pytest.raises(B.CompactError):
+            lay.compact_paged_plan(kv, bad)
+    for name in ("k", "v", "k_scale", "v_scale", "table"):
+        with pytest.raises(B.CompactError):
+            B.PagedKV(lc, **{n: getattr(kv, n).cpu() if n == name else getattr(kv, n) for n in ("k", "v", "k_scale", "v_scale", "table")})
+    with pytest.raises(B.CompactError):
+        calls(kv=B.PagedKV.allocate(lc, 3, 4, 12, 16, "cpu"))
+    lay.ws = lay.ws.cpu()
+    with pytest.raises(B.CompactError):
+        calls()

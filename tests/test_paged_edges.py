@@ -7,7 +7,7 @@ import torch
 
 from oracle import paged8 as P8
 from paper_2605_23296_amd import binding as B
-from paper_2605_23296_amd.workloads import WORKLOADS
+from paper_2605_23296_amd.workloads import WORKLOADS, LayerConfig
 from tests.test_paged import _kv, _step
 
 
@@ -32,3 +32,132 @@ def test_a_plan_takes_no_more_rows_than_its_threads_can_count():
     lay = B.Layer(WORKLOADS["dense_8x4096"].layer, None)
     for rows in (1 << 30, 1 << 29, (1 << 26) + 1):
         assert lay.L.compact_paged_plan(lay.ctx, C.byref(_kv()), C.byref(_step(max_rows=rows)), None) == 2, rows
+
+
+class Calls:
+    """Stands in for the library: counts the calls that reach it."""
+
+    def __init__(self):
+        self.n = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.n += 1
+            return 0
+        return call
+
+
+@pytest.fixture
+def on_the_host(monkeypatch):
+    """A layer whose calls end before the library, and what they take, on the CPU (whose device number is -1)."""
+    lc = LayerConfig(d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=64, ffn_dim=256, dtype="bf16")
+    lay = B.Layer(lc, None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    real, lay.L = lay.L, Calls()
+    yield lay, B.PagedKV.allocate(lc, 3, 4, 12, 16, "cpu")
+    lay.L = real
+
+
+def test_calls_refuse_arrays_that_are_not_on_the_current_gpu(on_the_host, monkeypatch):
+    lay, kv = on_the_host
+    lay.ws, st, bf = torch.zeros(1 << 20, dtype=torch.uint8), B.PagedStep(lay.layer, 3, 5, "cpu", n_pages=12), torch.bfloat16
+    calls = (lambda: lay.compact_paged_plan(kv, st), lambda: lay.compact_rope_paged_write(torch.zeros((5, 768), dtype=bf), kv, st.slot, st.rot, torch.zeros((5, 512), dtype=bf)),
+             lambda: lay.compact_attn_paged(torch.zeros((5, 512), dtype=bf), kv, st.cu, st.kv_len, 2, 64, torch.zeros((5, 512), dtype=bf)))
+    for call in calls:
+        call()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call in calls:
+        assert refused(call)
+    assert lay.L.n == 3
+
+
+def refused(call):
+    with pytest.raises(B.CompactError) as e:
+        call()
+    return e.value.code == 1
+
+
+WRONG = [lambda t: t.float() if t.dtype is not torch.float32 else t.double(),           # another type
+         lambda t: t.reshape(-1)[:-1],                                                  # one element short
+         lambda t: t.reshape(-1).repeat_interleave(2)[::2].reshape(t.shape)]            # elements apart
+
+
+def test_write_refuses_arrays_that_do_not_fit(on_the_host):
+    lay, kv = on_the_host
+    bf = torch.bfloat16
+    good = dict(qkv=torch.zeros((5, 12 * 64), dtype=bf), slot=torch.zeros(5, dtype=torch.int64), rot=torch.zeros((5, 32, 2)), q=torch.zeros((5, 512), dtype=bf))
+
+    def write(kv=kv, **over):
+        a = dict(good, **over)
+        lay.compact_rope_paged_write(a["qkv"], kv, a["slot"], a["rot"], a["q"])
+    write()
+    write(slot=torch.zeros(9, dtype=torch.int64), rot=torch.zeros((9, 32, 2)), q=torch.zeros((9, 512), dtype=bf))   # more rows are no harm
+    write(qkv=torch.zeros((0, 12 * 64), dtype=bf))
+    assert lay.L.n == 3
+    for name in good:
+        for wrong in WRONG:
+            assert refused(lambda: write(**{name: wrong(good[name])})), name
+    assert refused(lambda: write(slot=good["slot"].int()))
+    assert refused(lambda: write(qkv=good["qkv"][:, :-64].contiguous()))
+    other = LayerConfig(d_model=512, n_q_heads=8, n_kv_heads=4, head_dim=64, ffn_dim=256, dtype="bf16")
+    assert refused(lambda: write(kv=B.PagedKV.allocate(other, 3, 4, 12, 16, "cpu")))
+    assert lay.L.n == 3
+
+
+def test_attention_refuses_arrays_that_do_not_fit(on_the_host):
+    lay, kv = on_the_host
+    bf = torch.bfloat16
+    lay.ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    good = dict(q=torch.zeros((5, 512), dtype=bf), cu=torch.zeros(4, dtype=torch.int32), kv_len=torch.zeros(3, dtype=torch.int32), o=torch.zeros((5, 512), dtype=bf))
+
+    def attn(kv=kv, **over):
+        a = dict(good, **over)
+        lay.compact_attn_paged(a["q"], kv, a["cu"], a["kv_len"], 2, 64, a["o"])
+    attn()
+    attn(q=torch.zeros((5, 768), dtype=bf)[:, :512])       # rows may be apart
+    attn(cu=torch.zeros(9, dtype=torch.int32), o=torch.zeros((9, 512), dtype=bf))
+    assert lay.L.n == 3
+    for name in ("cu", "kv_len", "o"):
+        for wrong in WRONG:
+            assert refused(lambda: attn(**{name: wrong(good[name])})), name
+    assert refused(lambda: attn(q=good["q"].reshape(-1)))
+    assert refused(lambda: attn(q=good["q"].float())) and refused(lambda: attn(q=good["q"][:, :-8])) and refused(lambda: attn(q=torch.zeros((512, 5), dtype=bf).T))
+    other = LayerConfig(d_model=512, n_q_heads=8, n_kv_heads=1, head_dim=128, ffn_dim=256, dtype="bf16")
+    assert refused(lambda: attn(kv=B.PagedKV.allocate(other, 3, 4, 12, 16, "cpu")))
+    assert lay.L.n == 3
+
+
+def test_plan_refuses_arrays_that_do_not_fit(on_the_host):
+    lay, kv = on_the_host
+
+    def step(**over):
+        st = B.PagedStep(lay.layer, 3, 40, "cpu", n_pages=12)
+        for name, value in over.items():
+            setattr(st, name, value)
+        lay.compact_paged_plan(kv, st)
+    step()
+    assert lay.L.n == 1
+    st = B.PagedStep(lay.layer, 3, 40, "cpu", n_pages=12)
+    for name in ("n_new", "len", "n_free", "free", "n_free_out", "n_refused", "len_out", "kv_len", "cu", "slot", "rot"):
+        for wrong in WRONG:
+            t = wrong(getattr(st, name))
+            if t.numel() > 1 or t.is_contiguous() and (t.dtype is not getattr(st, name).dtype or t.numel() == 0):   # (one element is never apart)
+                assert refused(lambda: step(**{name: t})), name
+    assert refused(lambda: lay.compact_paged_plan(kv, B.PagedStep(lay.layer, 2, 40, "cpu", n_pages=12)))
+    assert refused(lambda: lay.compact_paged_plan(kv, B.PagedStep(lay.layer, 3, 40, "cpu", n_pages=11)))
+    wide = LayerConfig(d_model=512, n_q_heads=4, n_kv_heads=2, head_dim=128, ffn_dim=256, dtype="bf16")
+    assert refused(lambda: lay.compact_paged_plan(kv, B.PagedStep(wide, 3, 40, "cpu", n_pages=12)))     # its rows of `rot` are not the layer's
+    assert lay.L.n == 1
+
+
+def test_a_cache_refuses_pages_of_other_shapes():
+    lc = LayerConfig(d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=64, ffn_dim=256, dtype="bf16")
+    kv = B.PagedKV.allocate(lc, 3, 4, 12, 16, "cpu")
+    good = dict(k=kv.k, v=kv.v, k_scale=kv.k_scale, v_scale=kv.v_scale, table=kv.table)
+    B.PagedKV(lc, **good)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        for bad in (good[name][:-1], good[name].float(), good[name].transpose(0, 1).contiguous().transpose(0, 1)):
+            assert refused(lambda: B.PagedKV(lc, **dict(good, **{name: bad}))), name
+    for bad in (kv.table.long(), kv.table.t().contiguous().t()):
+        assert refused(lambda: B.PagedKV(lc, **dict(good, table=bad)))
