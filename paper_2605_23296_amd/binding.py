@@ -209,26 +209,39 @@ class KVCache:
 class PagedKV:
     """Pages in 8 bits and their block table (compact_paged_kv): k uint8 [n_pages, Hkv, page_rows, hd], v uint8 [n_pages, Hkv,
     hd, page_rows], k_scale and v_scale uint8 [n_pages, Hkv], table int32 [n_requests, max_pages].  n_pages and page_rows
-    are taken from k unless given (a plan needs the table alone)."""
+    are taken from k unless given (a plan needs the table alone).  The arrays may be replaced (a larger pool: k, v, both scales and
+    n_pages); the next call uses the new ones."""
 
     def __init__(self, layer, k, v, k_scale, v_scale, table, n_pages=None, page_rows=None):
         self.layer, self.k, self.v, self.k_scale, self.v_scale, self.table = layer, k, v, k_scale, v_scale, table
         self.n_pages = k.shape[0] if n_pages is None else n_pages
         self.page_rows = k.shape[2] if page_rows is None else page_rows
-        self.n_requests, self.max_pages = table.shape
-        if k.numel():
-            pages, rows = (self.n_pages, layer.n_kv_heads), (self.page_rows, layer.head_dim)
-            for name, shape in (("k", pages + rows), ("v", pages + rows[::-1]), ("k_scale", pages), ("v_scale", pages)):
-                if tuple(getattr(self, name).shape) != shape:
-                    _refuse("pages: %s is %s, %s needed" % (name, tuple(getattr(self, name).shape), shape))
-        self.device = table.get_device()
-        for name in ("k", "v", "k_scale", "v_scale"):
-            _array(getattr(self, name), torch.uint8, 0, self.device, "pages: " + name)
-        _array(table, torch.int32, 0, self.device, "block table")
-        self.heads = (layer.n_kv_heads, layer.head_dim)
-        self.c = PagedKVStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), self.n_pages,
-                               self.page_rows, self.max_pages, self.n_requests)
-        self.ref = C.byref(self.c)
+        self.struct()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_ref", None)   # (made again by the next call)
+
+    def struct(self):
+        """Reference to the compact_paged_kv of the arrays as they are."""
+        if self._ref is None:
+            layer, table, names = self.layer, self.table, ("k", "v", "k_scale", "v_scale")
+            arrays = [getattr(self, name) for name in names]
+            if self.k.numel():
+                pages, rows = (self.n_pages, layer.n_kv_heads), (self.page_rows, layer.head_dim)
+                for name, x, shape in zip(names, arrays, (pages + rows, pages + rows[::-1], pages, pages)):
+                    if tuple(x.shape) != shape:
+                        _refuse("pages: %s is %s, %s needed" % (name, tuple(x.shape), shape))
+            device = table.get_device()
+            for name, x in zip(names, arrays):
+                _array(x, torch.uint8, 0, device, "pages: " + name)
+            _array(table, torch.int32, 0, device, "block table")
+            n_requests, max_pages = table.shape
+            c = PagedKVStruct(*[x.data_ptr() for x in arrays], table.data_ptr(), self.n_pages, self.page_rows, max_pages, n_requests)
+            for name, value in (("n_requests", n_requests), ("max_pages", max_pages), ("device", device),
+                                ("heads", (layer.n_kv_heads, layer.head_dim)), ("c", c), ("_ref", C.byref(c))):
+                object.__setattr__(self, name, value)
+        return self._ref
 
     @classmethod
     def allocate(cls, layer, n_requests, max_pages, n_pages, page_rows, device):
@@ -451,18 +464,18 @@ class Layer:
             _refuse("pages for %s KV heads x head_dim on device %d; the layer has %s, the current device is %d" % (kv.heads, kv.device, self.kv_heads, device))
 
     def compact_paged_plan(self, kv, step):
-        device, st = torch.cuda.current_device(), step.struct()
+        device, ref, st = torch.cuda.current_device(), kv._ref or kv.struct(), step.struct()
         if step.n_requests != kv.n_requests or step.n_stack < kv.n_pages or step.head_dim != self.kv_heads[1] or kv.device != device or step.device != device:
             _refuse("step of %d requests, a stack of %d pages and head_dim %d on device %d; the cache has %d, %d, %d on device %d, the current device is %d"
                     % (step.n_requests, step.n_stack, step.head_dim, step.device, kv.n_requests, kv.n_pages, self.kv_heads[1], kv.device, device))
-        rc = self.L.compact_paged_plan(self.ctx, kv.ref, C.byref(st), _raw_stream(device))
+        rc = self.L.compact_paged_plan(self.ctx, ref, C.byref(st), _raw_stream(device))
         if rc:
             self.check(rc)
 
     def compact_rope_paged_write(self, qkv, kv, slot, rot, q):
         """qkv [rows, Dq + 2 Dkv] -> q [rows, Dq] (rotated), k and v into kv's pages at slot [rows]; rot [rows, hd / 2, 2].  slot, rot and
         q may have more rows."""
-        device, dt, shape = torch.cuda.current_device(), self.torch_dtype, qkv.shape
+        device, ref, dt, shape = torch.cuda.current_device(), kv._ref or kv.struct(), self.torch_dtype, qkv.shape
         rows = shape[0]
         if (len(shape) != 2 or shape[1] != self.qkv_cols or kv.heads != self.kv_heads or kv.device != device
                 or qkv.dtype is not dt or qkv.get_device() != device or not qkv.is_contiguous()
@@ -475,7 +488,7 @@ class Layer:
             _array(rot, torch.float32, rows * self.kv_heads[1], device, "rot")
             _array(q, dt, rows * self.q_cols, device, "q")
             _refuse("qkv: %s, [rows, %d] needed" % (tuple(qkv.shape), self.qkv_cols))
-        rc = self.L.compact_rope_paged_write(self.ctx, rows, qkv.data_ptr(), kv.ref, slot.data_ptr(), rot.data_ptr(), q.data_ptr(), _raw_stream(device))
+        rc = self.L.compact_rope_paged_write(self.ctx, rows, qkv.data_ptr(), ref, slot.data_ptr(), rot.data_ptr(), q.data_ptr(), _raw_stream(device))
         if rc:
             self.check(rc)
 
@@ -492,8 +505,8 @@ class Layer:
 
     def compact_attn_paged(self, q, kv, cu, kv_len, max_new, max_kv_len, o):
         """q [rows, >= Dq] (its rows may be apart), o [rows, Dq], cu [n_requests + 1], kv_len [n_requests].  The workspace is self.ws."""
-        device, dt, shape, apart, ws, N = torch.cuda.current_device(), self.torch_dtype, q.shape, q.stride(), self.ws, kv.n_requests
-        rows = shape[0]
+        device, ref, dt, shape, apart, ws = torch.cuda.current_device(), kv._ref or kv.struct(), self.torch_dtype, q.shape, q.stride(), self.ws
+        rows, N = shape[0], kv.n_requests
         if (len(shape) != 2 or shape[1] < self.q_cols or apart[1] != 1 or kv.heads != self.kv_heads or kv.device != device
                 or q.dtype is not dt or q.get_device() != device
                 or cu.dtype is not torch.int32 or cu.numel() <= N or cu.get_device() != device or not cu.is_contiguous()
@@ -506,7 +519,7 @@ class Layer:
             _array(o, dt, rows * self.q_cols, device, "o")
             _refuse("q: %s %s with strides %s on %s, workspace on %s; [rows, %d] of %s on the current GPU needed"
                     % (q.dtype, tuple(q.shape), q.stride(), q.device, ws if ws is None else ws.device, self.q_cols, dt))
-        rc = self.L.compact_attn_paged(self.ctx, kv.ref, rows, cu.data_ptr(), kv_len.data_ptr(), max_new, max_kv_len, q.data_ptr(), apart[0],
+        rc = self.L.compact_attn_paged(self.ctx, ref, rows, cu.data_ptr(), kv_len.data_ptr(), max_new, max_kv_len, q.data_ptr(), apart[0],
                                        o.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream(device))
         if rc:
             self.check(rc)

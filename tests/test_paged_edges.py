@@ -161,3 +161,24 @@ def test_a_cache_refuses_pages_of_other_shapes():
             assert refused(lambda: B.PagedKV(lc, **dict(good, **{name: bad}))), name
     for bad in (kv.table.long(), kv.table.t().contiguous().t()):
         assert refused(lambda: B.PagedKV(lc, **dict(good, table=bad)))
+
+
+def test_a_cache_whose_arrays_are_replaced_uses_the_new_ones(on_the_host):
+    lay, kv = on_the_host
+    st, seen = B.PagedStep(lay.layer, 3, 5, "cpu", n_pages=20), []
+
+    def plan():
+        lay.L.compact_paged_plan = lambda ctx, ref, step, stream: seen.append(ref._obj) or 0
+        lay.compact_paged_plan(kv, st)
+        return seen[-1]
+    assert (plan().d_table, plan().d_k, plan().n_pages) == (kv.table.data_ptr(), kv.k.data_ptr(), 12)
+    kv.table = torch.full((3, 6), -1, dtype=torch.int32)
+    assert (plan().d_table, plan().max_pages, kv.max_pages) == (kv.table.data_ptr(), 6, 6)
+    big = B.PagedKV.allocate(lay.layer, 3, 6, 20, 16, "cpu")       # a larger pool, array by array
+    kv.k, kv.v, kv.k_scale, kv.v_scale = big.k, big.v, big.k_scale, big.v_scale
+    assert refused(plan)                                             # the number of pages is still the old one
+    kv.n_pages = 20
+    c = plan()
+    assert (c.d_k, c.d_v, c.d_k_scale, c.d_v_scale, c.n_pages) == (big.k.data_ptr(), big.v.data_ptr(), big.k_scale.data_ptr(), big.v_scale.data_ptr(), 20)
+    kv.table = torch.full((2, 6), -1, dtype=torch.int32)
+    assert refused(plan)                                             # the step has three requests
