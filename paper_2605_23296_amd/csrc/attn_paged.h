@@ -31,9 +31,9 @@ struct PagedAttnArgs {
     int64_t q_stride;
     int Hq, Hkv;
     float scale_log2;
-    // records of requests whose keys are split: [request][row][query head][piece], HD values each, and behind all of them (max, sum)
+    // records of requests whose keys are split: [row][query head][piece] of a request, HD values each, and behind all of them (max, sum)
     float* rec;
-    int64_t rec_stride;       // row-pieces of a request
+    int rec_req, rec_row;     // a request's place among them, in row-pieces: so many per request and packed row before it
     int64_t n_rec;            // records in all
     int32_t* sched;           // the tile kernel's schedule: units taken per XCD (SCHED_PITCH apart), requests, units before them
 };
@@ -56,6 +56,11 @@ __device__ __forceinline__ int tile_pieces(int tiles, int kv) { return max(max(k
 // rows of a piece: the last piece may hold fewer
 __device__ __forceinline__ int tile_piece_rows(int pieces, int kv) {
     return ((kv + pieces - 1) / pieces + TILE_KEYS - 1) / TILE_KEYS * TILE_KEYS;
+}
+
+// the first record of a request's row and query head
+__device__ __forceinline__ int64_t first_record(const PagedAttnArgs& a, int req, int row0, int row, int head, int pieces) {
+    return ((int64_t)req * a.rec_req + (int64_t)row0 * a.rec_row + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces;
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -442,7 +442,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(HD, NP, CT)) void attn
         }
         if (cur.pieces > 1) {
             if (t == 0) {
-                held_rec[n_held] = (int64_t)cur.req * a.rec_stride * a.Hq + (int64_t)cur.kvh * G * cur.pieces + cur.ch;
+                held_rec[n_held] = first_record(a, cur.req, cur.row0, 0, cur.kvh * G, cur.pieces) + cur.ch;
                 held_pieces[n_held] = cur.pieces;
                 held_cols[n_held] = cols;
             }
@@ -489,7 +489,7 @@ __device__ __forceinline__ void merge_pair(const PagedAttnArgs& a, const PagedRe
     constexpr int TPR = HD / 4, NS = 64 / TPR, STEP = NS * WAVES;   // lanes per record, records side by side
     const int lane = threadIdx.x & 63, wave = wave_index();
     const int sub = WAVES == 1 ? lane / TPR : wave * NS + lane / TPR, e4 = lane % TPR;
-    const int64_t rec = ((int64_t)req * a.rec_stride + (int64_t)row * pieces) * a.Hq + (int64_t)head * pieces;
+    const int64_t rec = first_record(a, req, rq.row0, row, head, pieces);
     const floatx4* val = reinterpret_cast<const floatx4*>(a.rec + rec * HD) + e4;
     const float2* ml = reinterpret_cast<const float2*>(a.rec + a.n_rec * HD) + rec;
     floatx4 v[MERGE_FLIGHT];
@@ -633,19 +633,31 @@ static bool has_tiles(const compact_layer_cfg& c, int max_new) { return (int64_t
 // t tiles in p >= 2 pieces: t p is at most this
 static int most_split(int max_kv) { return std::max(max_kv / TILE_SPLIT, max_kv >= 2 * TILE_LONG ? TILE_FILL : 0); }
 
-// row-pieces of a request that records are kept for; 0: no request of the call is split
-static int64_t record_stride(const compact_layer_cfg& c, int max_new, int max_kv) {
-    const int G = c.n_q_heads / c.n_kv_heads;
-    int64_t few = 0, tiles = 0;
-    const int chunks = (max_kv - 1) / FEW_CHUNK + 1;
-    if (chunks > 1) few = (int64_t)std::min(max_new, FEW_COLS / G) * chunks;
-    // n rows in t = ceil(n G / 128) tiles: n p <= (128 / G) t p
-    if (has_tiles(c, max_new) && max_kv >= 2 * TILE_SPLIT) tiles = (int64_t)TILE_COLS * (most_split(max_kv) + 1) / G + 1;
-    return std::max(few, tiles);
+// Where the records lie: a request's row-pieces begin at req * per_req + row0 * per_row.  Three ways to hold all of them, each
+// with room for the most that a request's n rows in p >= 2 pieces can be; the smallest is taken.
+struct RecordLayout {
+    int64_t per_req, per_row, total;   // in row-pieces; total 0: no request of the call is split
+};
+static RecordLayout record_layout(const compact_layer_cfg& c, int n_requests, int n_rows, int max_new, int max_kv) {
+    const int G = c.n_q_heads / c.n_kv_heads, chunks = (max_kv - 1) / FEW_CHUNK + 1;
+    if (chunks == 1) return {0, 0, 0};
+    const int64_t few = (int64_t)std::min(max_new, FEW_COLS / G) * chunks;
+    const bool tiles = has_tiles(c, max_new) && max_kv >= 2 * TILE_SPLIT;
+    // by request: n rows in t = ceil(n G / 128) tiles: n p <= (128 / G) t p
+    RecordLayout best = {tiles ? std::max(few, (int64_t)TILE_COLS * (most_split(max_kv) + 1) / G + 1) : few, 0, 0};
+    best.total = best.per_req * n_requests;
+    auto consider = [&](int64_t per_req, int64_t per_row) {
+        const int64_t total = per_req * n_requests + per_row * n_rows;
+        if (total < best.total) best = {per_req, per_row, total};
+    };
+    consider(0, chunks);   // by row: p <= chunks
+    // by both: a few rows as above, t p <= kv / 512 whatever the rows, or p <= kv / 2048
+    if (tiles) consider(std::max(few, (int64_t)TILE_COLS * (max_kv / TILE_SPLIT) / G), max_kv >= 2 * TILE_LONG ? max_kv / TILE_LONG : 0);
+    return best;
 }
 
-static size_t paged_workspace(const compact_layer_cfg& c, int n_requests, int max_new, int max_kv) {
-    const size_t rec = (size_t)n_requests * record_stride(c, max_new, max_kv) * c.n_q_heads;
+static size_t paged_workspace(const compact_layer_cfg& c, int n_requests, int n_rows, int max_new, int max_kv) {
+    const size_t rec = (size_t)record_layout(c, n_requests, n_rows, max_new, max_kv).total * c.n_q_heads;
     return align_up(SCHED_BYTES, 256) + rec * (c.head_dim + 2) * 4;
 }
 
@@ -661,7 +673,8 @@ extern "C" int compact_paged_workspace_bytes(const compact_ctx* ctx, int32_t n_r
                                              int32_t max_kv_len, size_t* bytes) {
     if (!ctx || !bytes) return COMPACT_EINVAL;
     TRY_RC(check_bounds(const_cast<compact_ctx*>(ctx), n_requests, n_rows, max_new, max_kv_len));
-    *bytes = paged_workspace(ctx->cfg, n_requests, std::max(std::min(max_new, n_rows), 1), max_kv_len);
+    n_rows = std::max(n_rows, 1);
+    *bytes = paged_workspace(ctx->cfg, n_requests, n_rows, std::min(max_new, n_rows), max_kv_len);
     return COMPACT_OK;
 }
 
@@ -684,7 +697,7 @@ static int launch_attn_paged(compact_ctx* ctx, const PagedAttnArgs& a, hipStream
     }
     LAUNCH_CHECK(ctx);
     if (tiles) TRY_RC(launch_attn_paged_tiles(ctx, a, s));
-    if (a.rec_stride == 0) return COMPACT_OK;
+    if (a.n_rec == 0) return COMPACT_OK;
     // rows of a request whose keys may be split: 2 t <= t p for its t tiles
     const int64_t few_rows = std::min(a.max_new, FEW_COLS / G), tile_rows = (int64_t)TILE_COLS * most_split(a.max_kv) / 2 / G + 1;
     const int64_t rows = tiles ? std::min<int64_t>(a.max_new, std::max(few_rows, tile_rows)) : few_rows;
@@ -719,7 +732,7 @@ extern "C" int compact_attn_paged(compact_ctx* ctx, const compact_paged_kv* kv, 
         return set_err(ctx, COMPACT_EINVAL, "q_stride must be at least n_q_heads * head_dim and a multiple of 8");
     if (((uintptr_t)d_q | (uintptr_t)d_o) & 15) return set_err(ctx, COMPACT_EINVAL, "q and o must be 16-byte aligned");
     max_new = std::min(max_new, n_rows);
-    if (!d_workspace || ((uintptr_t)d_workspace & 15) || ws_bytes < paged_workspace(c, kv->n_requests, max_new, max_kv_len))
+    if (!d_workspace || ((uintptr_t)d_workspace & 15) || ws_bytes < paged_workspace(c, kv->n_requests, n_rows, max_new, max_kv_len))
         return set_err(ctx, COMPACT_EWORKSPACE, "workspace missing, not 16-byte aligned or too small for the paged attention");
     a.cu = d_cu;
     a.kv_len = d_kv_len;
@@ -732,8 +745,10 @@ extern "C" int compact_attn_paged(compact_ctx* ctx, const compact_paged_kv* kv, 
     a.Hq = c.n_q_heads;
     a.Hkv = c.n_kv_heads;
     a.scale_log2 = LOG2E / sqrtf((float)c.head_dim);
-    a.rec_stride = record_stride(c, max_new, a.max_kv);
-    a.n_rec = (int64_t)kv->n_requests * a.rec_stride * c.n_q_heads;
+    const RecordLayout records = record_layout(c, kv->n_requests, n_rows, max_new, a.max_kv);
+    a.rec_req = (int)records.per_req;   // (at most 128 * (2^22 + 1))
+    a.rec_row = (int)records.per_row;
+    a.n_rec = records.total * c.n_q_heads;
     a.sched = (int32_t*)d_workspace;
     a.rec = (float*)((char*)d_workspace + align_up(SCHED_BYTES, 256));
     const bool b = c.dtype == COMPACT_BF16;

@@ -112,7 +112,7 @@ __device__ __forceinline__ void put_unit(const PagedAttnArgs& a, const Unit& un,
 #pragma unroll
             for (int g = 0; g < 4; ++g) put4(op + d * 32 + g * 8, oacc[d][4 * g] * inv, oacc[d][4 * g + 1] * inv, oacc[d][4 * g + 2] * inv, oacc[d][4 * g + 3] * inv);
     } else {
-        const int64_t rec = ((int64_t)un.req * a.rec_stride + (int64_t)un.row * un.pieces) * a.Hq + (int64_t)un.head * un.pieces + un.piece;
+        const int64_t rec = first_record(a, un.req, un.rq.row0, un.row, un.head, un.pieces) + un.piece;
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d)
 #pragma unroll

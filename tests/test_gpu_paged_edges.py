@@ -1,5 +1,6 @@
 """Paged cache in 8 bits at the edges of what its calls accept: requests without cached rows beside pages that hold anything,
-values at the top of the range, stacks of as many pages as there are numbers, arrays that are not on the GPU."""
+values at the top of the range, stacks of as many pages as there are numbers, arrays that are not on the GPU,
+workspaces of exactly the size that is asked for."""
 import pytest
 import torch
 
@@ -132,3 +133,28 @@ def test_arrays_on_the_host_are_refused():
     lay.ws = lay.ws.cpu()
     with pytest.raises(B.CompactError):
         calls()
+
+
+@pytest.mark.parametrize("lc", [layer(4, 1, 128), layer(2, 1, 64, "fp32")], ids=IDS)
+@pytest.mark.parametrize("n_new,lens", [([4000, 1], [5000, 4999]),                                               # by request
+                                        ([1, 2, 50] + [1, 0, 3] * 12, [1100, 257, 1090] + [600, 1000, 300] * 12),    # by row
+                                        ([1, 1, 1200, 40, 3, 32, 500, 9], [8200, 300, 6000, 8200, 8200, 4100, 7000, 513])],   # by both
+                         ids=["by_request", "by_row", "by_both"])
+def test_records_stay_inside_the_workspace_that_was_asked_for(lc, n_new, lens):
+    """Every way to lay out the records of split keys, in a workspace of that size: right, the bits of the requests by themselves, and
+    what lies behind it is untouched."""
+    kv, ref, table = random_cache(lc, lens, 64, 23)
+    q, lay = queries(lc, sum(n_new), 23), handle(lc)
+    said = [L if n else 0 for n, L in zip(n_new, lens)]
+    need = lay.paged_workspace_bytes(len(lens), sum(n_new), max(n_new), max(lens))
+    room = torch.full((need + (1 << 20),), 0xA5, dtype=torch.uint8, device=DEV)
+    lay.ws = room[:need]
+    o = run_attn(lay, kv, q, n_new, said)
+    assert lay.ws.data_ptr() == room.data_ptr() and (room[need:] == 0xA5).all()
+    check_attn(lc, q, o, n_new, said, ref, table)
+    lay.ws, row = None, 0
+    for i, (n, L) in enumerate(zip(n_new, said)):
+        if n:
+            one = B.PagedKV(lc, kv.k, kv.v, kv.k_scale, kv.v_scale, kv.table[i:i + 1].contiguous())
+            assert torch.equal(run_attn(lay, one, q[row:row + n], [n], [L]), o[row:row + n]), i
+        row += n

@@ -182,3 +182,42 @@ def test_a_cache_whose_arrays_are_replaced_uses_the_new_ones(on_the_host):
     assert (c.d_k, c.d_v, c.d_k_scale, c.d_v_scale, c.n_pages) == (big.k.data_ptr(), big.v.data_ptr(), big.k_scale.data_ptr(), big.v_scale.data_ptr(), 20)
     kv.table = torch.full((2, 6), -1, dtype=torch.int32)
     assert refused(plan)                                             # the step has three requests
+
+
+def pieces(n, kv, G):
+    """Into how many pieces a request's keys are cut (n rows of G query heads each per KV head)."""
+    if n <= 32 and n * G <= 32:
+        return max(-(-kv // 256), 1)
+    tiles = -(-n * G // 128)
+    return max(kv // 512 // tiles, min(kv // 2048, 64 // tiles), 1)
+
+
+def wide(G):
+    return B.Layer(LayerConfig(d_model=4096, n_q_heads=8 * G, n_kv_heads=8, head_dim=128, ffn_dim=4096, dtype="bf16"), None)
+
+
+@pytest.mark.parametrize("n_requests,max_kv,mib", [(24, 8192, 340), (512, 8192, 1050), (512, 32768, 4200), (1, 8192, 40), (4096, 2048, 270)])
+def test_workspace_goes_by_the_rows_of_a_call(n_requests, max_kv, mib):
+    """2048 rows a step, all of which one request may bring: no slot has room for all of them by itself."""
+    lay = wide(4)
+    assert lay.paged_workspace_bytes(n_requests, 2048, 2048, max_kv) <= mib << 20
+    # never more than a record for every row, query head and 256 keys, nor than the requests' own by themselves
+    base = lay.paged_workspace_bytes(1, 1, 1, 1)
+    assert lay.paged_workspace_bytes(n_requests, 2048, 2048, max_kv) - base <= 2048 * -(-max_kv // 256) * 32 * 130 * 4
+    assert lay.paged_workspace_bytes(n_requests, 2048, 2048, max_kv) - base <= n_requests * (lay.paged_workspace_bytes(1, 1 << 20, 2048, max_kv) - base)
+
+
+@pytest.mark.parametrize("G", [1, 3, 4, 16])
+def test_workspace_holds_every_batch_and_grows_with_each_bound(G):
+    lay, rng = wide(G), np.random.default_rng(G)
+    base = lay.paged_workspace_bytes(1, 1, 1, 1)
+    for _ in range(500):
+        N, most, max_kv = int(rng.integers(1, 40)), int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 17))
+        few = min(most, 32 // G)
+        n = [int(rng.choice([1, few, min(few + 1, most), most, rng.integers(0, most + 1)])) for _ in range(N)]
+        kv = [int(rng.choice([max_kv, rng.integers(0, max_kv + 1)])) for _ in range(N)]
+        rows, need = max(sum(n), 1), sum(a * pieces(a, b, G) for a, b in zip(n, kv) if pieces(a, b, G) > 1)
+        have = lay.paged_workspace_bytes(N, rows, most, max_kv)
+        assert have - base >= need * 8 * G * 130 * 4, (n, kv)
+        for more in ((N + 1, rows, most, max_kv), (N, rows + 9, most, max_kv), (N, rows, most + 5, max_kv), (N, rows, most, max_kv + 300)):
+            assert lay.paged_workspace_bytes(*more) >= have, (more, n)
