@@ -297,8 +297,12 @@ class PagedStep:
 
     def advance(self):
         """After a step: its lengths and its stack are the next one's."""
+        c = self._c
         self.len, self.len_out = self.len_out, self.len
         self.n_free, self.n_free_out = self.n_free_out, self.n_free
+        if c is not None:      # (the arrays are the same ones, and have been looked at)
+            c.d_len, c.d_len_out, c.d_n_free, c.d_n_free_out = c.d_len_out, c.d_len, c.d_n_free_out, c.d_n_free
+            object.__setattr__(self, "_c", c)
 
 
 class Layer:

@@ -221,3 +221,17 @@ def test_workspace_holds_every_batch_and_grows_with_each_bound(G):
         assert have - base >= need * 8 * G * 130 * 4, (n, kv)
         for more in ((N + 1, rows, most, max_kv), (N, rows + 9, most, max_kv), (N, rows, most + 5, max_kv), (N, rows, most, max_kv + 300)):
             assert lay.paged_workspace_bytes(*more) >= have, (more, n)
+
+
+def test_a_step_that_advances_swaps_its_arrays():
+    lc = LayerConfig(d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=64, ffn_dim=256, dtype="bf16")
+    st = B.PagedStep(lc, 3, 5, "cpu", n_pages=12)
+    st.advance()                              # before its first call as well
+    for _ in range(3):
+        before = st.struct() and (st.len, st.n_free)
+        st.advance()
+        assert st.len_out is before[0] and st.n_free_out is before[1]
+        names = [n for n, _ in B.PagedStepStruct._fields_[:-1]]
+        assert [getattr(st.struct(), n) for n in names] == [getattr(st, n[2:]).data_ptr() for n in names]
+    st.len = torch.zeros(4, dtype=torch.int32)
+    assert refused(st.struct)
