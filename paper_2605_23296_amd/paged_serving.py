@@ -42,7 +42,9 @@ class PagedServer:
         self.free = n_pages            # pages not promised to a request
 
     def submit(self, request):
-        """Takes the request if there is a slot, and pages for all of its rows."""
+        """Takes the request if there is a slot, and pages for all of its rows.  One without rows is done at once."""
+        if request.rows.shape[0] == 0:
+            return True
         pages = -(-request.rows.shape[0] // self.kv.page_rows)
         free = [i for i, r in enumerate(self.slots) if r is None and i not in self.leaving]
         if request.rows.shape[0] > self.max_len or not free or pages > self.free:
