@@ -353,7 +353,7 @@ typedef struct compact_paged_step {
  * give their pages back first, pushed on the stack in the order of requests and table columns; then every request that
  * adds rows takes what it lacks, in the order of requests, the first missing page from the top of the stack.  A request is
  * refused as a whole -- its length stays, its rows get slot -1, its d_kv_len is 0 -- when its rows end beyond max_rows or max_pages, or
- * when its pages and those of the requests before it (granted or not) are more than there are.  Table columns that the step does not fill
+ * when it lacks pages and these and those of the requests before it (granted or not) are more than there are.  Table columns that the step does not fill
  * and stack entries above the old and the new top are left as they are.  COMPACT_ESHAPE beyond 4096 requests or 2^26 rows. */
 int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, const compact_paged_step* step, void* hip_stream);
 
@@ -370,7 +370,9 @@ int compact_rope_paged_write(compact_ctx* ctx, int32_t n_rows, const void* d_qkv
  * where that is none.  One row per request is a decode step, more a prompt or a chunk of one; both may share a call.
  * max_new and max_kv_len bound n and d_kv_len (rows of requests with more are not computed rightly; nothing outside the
  * buffers is touched).  q rows are q_stride elements apart (>= Dq, a multiple of 8), o is [n_rows, Dq]; both 16-byte aligned.
- * Sums are fp32: V values near the top of the range may come out as infinities in rows that see them, and in no other.
+ * Scores, softmax and sums are fp32; with bf16 storage a probability is rounded to bf16 before it is multiplied with V (as
+ * in the slab path), with fp32 storage it keeps 24 bits.  V values near the top of the range may come out as infinities in rows
+ * that see them, and in no other.
  * Rows that belong to no request are left as they are.  How a request's keys are split depends on its own lengths
  * alone: its results do not depend on the other requests.  The workspace must hold compact_paged_workspace_bytes(...). */
 int compact_paged_workspace_bytes(const compact_ctx* ctx, int32_t n_requests, int32_t n_rows, int32_t max_new,

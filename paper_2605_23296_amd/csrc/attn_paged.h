@@ -15,7 +15,7 @@
 #define SCHED_BYTES (sizeof(int32_t) * (SCHED_UNITS + PAGED_MAX_REQUESTS + 1))
 // A request of t tiles has its keys cut into pieces of 512 t to 1024 t rows, and of 2048 to 4096 as long as that gives no more than
 // 64 units per KV head, which fill the card: a chunk of a prompt behind a long cache mostly comes alone or with single rows (256 rows behind
-// 8192, 32 + 8 heads of 128: 86 -> 61 us; 7 requests of up to 118 behind up to 12149 124 -> 101).  Where many come at once, the records of what
+// 8192, 32 + 8 heads of 128: 86 -> 62 us; 7 requests of up to 118 behind up to 12149 124 -> 99).  Where many come at once, the records of what
 // need not have been cut cost up to an eighth (32 x 250 rows behind 4000 to 8000: 843 -> 952), which a request may not know; with 1024 to 2048
 // rows it is a quarter, and with as many pieces as give 512 units in any case twice the time of 32 mixed requests.
 #define TILE_SPLIT 512

@@ -46,12 +46,14 @@ __device__ __forceinline__ int block_prefix(int v, int* red, int& total) {
 // than it needs (it counts outstanding loads), every load of the loop is issued unconditionally, with an address that is
 // read anyway where there is no next item, and the stores stand right before the V loads.  Records are held back in LDS until the
 // buffer is full or the share is done: a store in the load stream stalls it out of proportion.
-// Bound: the codes' way from HBM (64 caches of 2048 rows, 8 KV heads of 128: 268 MB in 56 us, 4.8 TB/s of the 6.2 that a sum reaches;
-// one cache of 32768 rows, 67 MB, 16 us: three loads one behind the other (lengths, page number, codes) before the first
+// Bound: the codes' way from HBM (64 caches of 2048 rows, 8 KV heads of 128: 268 MB in 57 us, 4.7 TB/s of the 6.2 that a sum reaches;
+// one cache of 32768 rows, 67 MB, 16.5 us: three loads one behind the other (lengths, page number, codes) before the first
 // item, and the last workgroups' items).  256 rows per item: 512 leave no registers for the next item's loads.  Requests of
-// 17 to 32 columns pay records of half the columns' bytes (8 x 8 rows behind 16384: 93 us; as tiles of 128 columns 106); with four column
-// tiles, for up to 64, those and the registers cost more than they save (16 rows behind 32768: 55 us, as tiles 36).
-// NP: bf16 parts of a query and of a probability (3 for fp32 storage: all 24 bits).  CT: tiles of 16 columns, two where a call may
+// 17 to 32 columns pay records of a quarter of the codes' bytes, written and read again (8 x 8 rows behind 16384: 268 MB of codes, 72 of
+// records, 94 us with the merge; as tiles of 128 columns 106); with four column tiles, for up to 64, those and the registers cost more than they save (16 rows behind 32768: 55 us, as tiles 36).
+// NP: bf16 parts of a query and of a probability (3 for fp32 storage: all 24 bits).  bf16 storage rounds a probability to bf16 for the
+// second product, as the slab kernels do: one matrix instruction in place of two or three, for a relative error of 0.0016 to 0.0018 against
+// 64 bits where rounding the output alone has 0.0015 to 0.0017 (prompts 0.002); their sum is of the values before the rounding.  CT: tiles of 16 columns, two where a call may
 // have requests of more than 16; a column's sums are the same either way.
 // ---------------------------------------------------------------------------
 #define FEW_REC_SLOTS 8
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, few_resident(HD, NP, CT)) void attn
 // ---------------------------------------------------------------------------
 // Joins the pieces of the (row, query head) pairs of split requests.  HD / 4 lanes span a record; a lane sends for up to
 // MERGE_FLIGHT records before it uses one.  With m = max m_i: o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i.  Bound by the launch
-// and two loads one behind the other (4 to 5 us for 64 x 8 and for 128 pieces; a call that merges nothing 3.8).  A request whose records one wavefront can send for at once has a wavefront per pair
+// and two loads one behind the other (5.2 us for 64 x 8 and for 128 pieces, traced; a call that merges nothing 4.5).  A request whose records one wavefront can send for at once has a wavefront per pair
 // (32 pieces of head_dim 64: 4.0 us instead of 7.2), one with more of them all four wavefronts of the workgroup.
 // ---------------------------------------------------------------------------
 #define MERGE_FLIGHT 8
@@ -570,7 +572,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedAttnAr
 
 // The same where a call has prompts, hardly any of whose rows are split: a fixed number of workgroups shares out the pairs
 // (four at a time where a wavefront joins one) that the requests' lengths give (64 single rows behind 2048 in a call for up to
-// 64 rows each: 79 us instead of 102).
+// 64 rows each: 75 us in all, 98 with a workgroup per row that there may be).
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void attn_paged_merge_share_kernel(const PagedAttnArgs a) {
     __shared__ floatx4 part[HD];

@@ -124,7 +124,7 @@ __device__ __forceinline__ void put_unit(const PagedAttnArgs& a, const Unit& un,
 // fp32 storage: queries and probabilities as three bf16 parts each (all 24 bits), the codes exact in bf16.  Steps of 64 keys: the
 // codes of the next one are in flight in registers while this one is computed, are expanded once per workgroup and go to LDS.
 // Bound by its own order (scores, softmax, output one behind the other in a wavefront, one wavefront per SIMD): 8 prompts of
-// 1024 rows, 4 + 2 heads of 64, 51 us, 0.25 PFLOP/s of bf16 products.  This storage is for checking.
+// 1024 rows, 4 + 2 heads of 64, 47 us, 0.27 PFLOP/s of bf16 products.  This storage is for checking.
 template <int HD>
 __global__ __launch_bounds__(256, 1) void attn_paged_tile_f32_kernel(const PagedAttnArgs a, int xcd_heads) {
     constexpr int NP = 3;
@@ -309,7 +309,9 @@ __device__ __forceinline__ unsigned pack_bf16x2(float a, float b) {
 // an order that is written out, as the slab path's prefill attention does it.  What the pages add: the codes of a K tile are
 // requested two steps before their use and those of a V tile as well, into registers; a step later they are expanded to bf16 (exact), once
 // per workgroup, and go to LDS between the matrix instructions, a piece of 16 codes every four of them.
-// Bound (8 prompts of 4096 rows, 32 + 8 heads of 128: 1.10 TFLOP in 1074 us, 1.02 PFLOP/s where a large product reaches 1.27): no pipe
+// A probability is rounded to bf16 for the second product (a part more would cost half of the matrix time again: the error against 64 bits
+// is 0.002, of the output's rounding alone 0.0017); the sums are of the values before the rounding.
+// Bound (8 prompts of 4096 rows, 32 + 8 heads of 128: 1.10 TFLOP in 1076 us, 1.02 PFLOP/s where a large product reaches 1.27): no pipe
 // alone.  The matrix pipes are busy 54 % of the cycles, the vector ALU issues in 55 %, the LDS works in 41 %, at 1.9 GHz of 2.4; without
 // the exponentials 1044 us, with half of the fragments' reads 1056, without the staging 982.  64 columns per wavefront would halve
 // the reads, but the scores then go through the accumulator registers: 1309.

@@ -44,9 +44,9 @@ int paged_view(compact_ctx* ctx, const compact_paged_kv* kv, bool with_pages, Pa
 // columns that are read lie below a request's length, those written above it; stack entries that are read lie below
 // n_free, those written above; lengths and counters come in pairs.  Page numbers are copied, never followed, so whatever the
 // device arrays hold, nothing outside them is touched.
-// Bound: up to some thousand rows by the launch and the chain of loads and scans (64 decode steps 5 us, 1024 of them 12); beyond
+// Bound: up to some thousand rows by the launch and the chain of loads and scans (64 decode steps 5.2 us, 1024 of them 7.8, traced); beyond
 // that by the angles, which are formed in 64 bits, a row's from the row before by a turn, and by the writes of 8 + 4 hd bytes
-// a row (8 x 4096 rows, 17 MB: 9.4 us; 512 requests with 37000 rows 13).
+// a row (8 x 4096 rows, 17 MB: 9.5 us; 512 requests with 37000 rows 13.6).
 // ---------------------------------------------------------------------------
 #define PLAN_NT 256
 
@@ -306,9 +306,9 @@ extern "C" int compact_paged_plan(compact_ctx* ctx, const compact_paged_kv* kv, 
 // (decode steps) go four and more side by side in a wavefront, without a barrier (200 of them: 13.7 -> 8.3 us).
 // Further workgroups rotate q.
 // Bound by HBM from some thousand rows on: every row is read once, q and the codes are written once (8 x 4096 rows of 32 + 16
-// heads of 128: 755 MB in 143 us, 5.3 TB/s, where a copy reaches 4.9 and a sum 6.2); by the launch and one chain of
-// dependent loads (slot, scale, row) below: 24 decode rows 4.5 us.  A single row's V touches hd lines for a
-// byte each, which 1000 such rows feel (28 us, 130 MB of lines read and written for 2 MB of codes).
+// heads of 128: 755 MB in 145 us, 5.2 TB/s, where a copy reaches 4.9 and a sum 6.2); by the launch and one chain of
+// dependent loads (slot, scale, row) below: 24 decode rows 4.2 us (traced).  A single row's V touches hd lines for a
+// byte each, which 1000 such rows feel (23 us, 43 MB written for 8 MB of q and 2 MB of codes).
 // ---------------------------------------------------------------------------
 #define WR_NT 256
 #define WR_QHEADS 8   // most query heads per wavefront of the q part
@@ -794,7 +794,8 @@ static int launch_write(compact_ctx* ctx, int n_rows, const void* qkv, const Pag
     WriteArgs<T> a{(const T*)qkv, (T*)q, slot, (const float2*)rot, kv, n_rows, Hq, Hkv, 1, 1, 1, 1, 1};
     // rows per workgroup of the K / V part: its segments of several rows follow each other, those of one row go side by side, and
     // a prompt leaves all but the first workgroup of a segment idle.  us, 32 + 8 heads of 128, pages of 64: 64 x 4 rows 11.2 by 4, 14.4 by 8,
-    // 61.5 by 64; 1024 rows of a prompt 14.3, 11.8, 11.5; 2 x 4096 52.5, 45.8, 41.3; 4 x 4096 97, 83, 78 (pages of 16: 84 by 16, 100 by 64); units of XCDs have since taken off 2 to 20 %
+    // 61.5 by 64; 1024 rows of a prompt 14.3, 11.8, 11.5; 2 x 4096 52.5, 45.8, 41.3; 4 x 4096 97, 83, 78 (pages of 16: 84 by 16,
+    // 100 by 64), all before the units of XCDs below
     a.chunk = n_rows <= 512 ? 4 : n_rows <= 8192 ? 8 : std::min(1 << kv.page_shift, 64);
     const int64_t groups = (n_rows + TPW - 1) / TPW;
     a.q_heads = (int)std::min<int64_t>(WR_QHEADS, std::max<int64_t>(1, groups * Hq / 4096));
