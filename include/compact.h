@@ -381,6 +381,78 @@ int compact_attn_paged(compact_ctx* ctx, const compact_paged_kv* kv, int32_t n_r
                        const int32_t* d_kv_len, int32_t max_new, int32_t max_kv_len, const void* d_q, int64_t q_stride,
                        void* d_o, void* d_workspace, size_t ws_bytes, void* hip_stream);
 
+/* ---- 8-bit integer weights ---------------------------------------------------
+ * What a server that keeps its projections as 8-bit integers with a scale per output channel runs around them: the codes of
+ * rows (activations, once per token; weights, once), the product of two matrices of codes, the norms around a block that hand
+ * their rows on as codes, and for routed layers the choice of the experts and their products.  No call below allocates, uploads or
+ * reads a device value on the host, so all of them may be captured in a HIP graph; results do not depend on the
+ * other rows of a call, nor on the workspace: sums of codes are integers, which add up the same in any order.
+ *
+ * Codes of a row x with amax = max |x_i|: q_i = 127 x_i / amax rounded to the nearest integer, ties to even (of that quotient itself,
+ * not of a rounded one), int8 in -127 .. 127; scale = amax / 127, fp32.  A row of zeros has scale 0.  A row that holds an infinity or
+ * NaN has scale NaN and codes 0, so whatever is computed from it is NaN, and nothing else is.                          */
+
+/* rows x cols of d_x (storage type, rows x_stride elements apart, x_stride >= cols) -> codes d_q int8 [rows, cols], d_scale [rows]. */
+int compact_quant_i8(compact_ctx* ctx, const void* d_x, int64_t x_stride, int64_t rows, int32_t cols, void* d_q, float* d_scale,
+                     void* hip_stream);
+
+/* C[m, n] = a_scale[m] b_scale[n] sum_k A[m, k] B[n, k] (+ R[m, n] if d_r != NULL): codes A int8 [M, K], B int8 [N, K] (any int8 value,
+ * -128 among them), the sum in 32-bit integers, C and R in the storage type.  Epilogue 1 treats B as [2N, K] (b_scale [2N]) stacked gate/up and stores
+ * silu(gate) * up.  d_r may be d_c.  K a multiple of 16, at most 131056; d_a and d_b 16-byte aligned, any M and N.  With a
+ * workspace of compact_gemm_i8_workspace_bytes few rows are faster; a smaller one, or none, changes no bit. */
+int compact_gemm_i8_workspace_bytes(const compact_ctx* ctx, int64_t M, int32_t N, int32_t K, int32_t epilogue, size_t* bytes);
+int compact_gemm_i8(compact_ctx* ctx, const void* d_a, const float* d_a_scale, const void* d_b, const float* d_b_scale, const void* d_r,
+                    void* d_c, int64_t M, int32_t N, int32_t K, int32_t epilogue, void* d_workspace, size_t ws_bytes,
+                    void* hip_stream);
+
+/* The norms around a block, rows of d_model elements in the storage type T:
+ *   h = T(x + alpha * gate * p),  p = RMSNorm(b; g_post), or b itself if d_g_post is NULL;   h = x if d_b is NULL
+ *   n = T(RMSNorm(h; g_pre)), and the codes of n.
+ * d_b: the block's output rows; d_gate (nullable = 1): one row for all (gate_stride 0) or a row each (gate_stride >= d_model,
+ * a multiple of 8); d_h, d_n, and the pair d_q (int8) / d_q_scale: each NULL where it is not wanted, one at least is.  d_g_pre is needed for d_n
+ * and d_q, d_b for d_h.  d_h and d_n may be d_x or d_b themselves (in place).  Arithmetic is fp32; n comes from the rounded h, as if
+ * the two norms were calls of their own.  Row arrays and gains 16-byte aligned (d_q 8). */
+int compact_block_norm(compact_ctx* ctx, const void* d_x, const void* d_b, const void* d_g_post, const void* d_gate, int64_t gate_stride,
+                       float alpha, void* d_h, const void* d_g_pre, void* d_n, void* d_q, float* d_q_scale, int64_t rows,
+                       void* hip_stream);
+
+/* How compact_route chooses top_k of n_experts (the layer's):
+ *   s = softmax or sigmoid of the row's logits;  c = s + bias;  the experts are n_groups groups of neighbours, a group counts as the
+ *   sum of its group_top largest c; eligible are the experts of the topk_groups best groups; the top_k eligible ones with the largest c are chosen,
+ *   in descending order; weight = s * factor, divided first by the sum of the chosen s if renorm.  Ties go to the lower index.
+ * Scores are compared to 44 bits.  An expert whose logit is -inf or NaN, or whose c is -inf or NaN, is chosen only where fewer than top_k
+ * others are eligible (weight 0 for the logit's sake), does not count in its group, and a group of such experts is the last choice; a row without
+ * a finite logit has weights 0.  Logits of +inf share the softmax among them.  Indices are always distinct and valid. */
+enum { COMPACT_SCORE_SOFTMAX = 0, COMPACT_SCORE_SIGMOID = 1 };
+typedef struct compact_route_rule {
+    int32_t score;         /* COMPACT_SCORE_* */
+    int32_t n_groups;      /* divides n_experts; 1 = no groups; at most 64 */
+    int32_t topk_groups;   /* 1 .. n_groups, with top_k experts at least in them */
+    int32_t group_top;     /* 1 or 2 */
+    int32_t renorm;
+    float   factor;
+} compact_route_rule;
+/* d_logits [rows, n_experts] fp32: given, or, where d_m [rows, d_model] and d_w_router [n_experts, d_model] (storage type) are,
+ * written as their product in fp32 (by the kernel that compact_moe_route uses, with its bits).  d_bias [n_experts] fp32 or NULL.
+ * d_expert_idx, d_weight [rows, top_k]. */
+int compact_route(compact_ctx* ctx, const compact_route_rule* rule, const void* d_m, const void* d_w_router, float* d_logits,
+                  const float* d_bias, int64_t rows, int32_t* d_expert_idx, float* d_weight, void* hip_stream);
+
+/* Expert weights as codes with a scale per output channel. */
+typedef struct compact_experts_i8 {
+    const void*  d_gate_up;         /* int8 [E, 2F, d], rows 0..F-1 gate, F..2F-1 up */
+    const float* d_gate_up_scale;   /* [E, 2F] */
+    const void*  d_down;            /* int8 [E, d, F] */
+    const float* d_down_scale;      /* [E, d] */
+} compact_experts_i8;
+/* y = h + sum_k weight_k FFN_{idx_k}(m), rows m as codes (d_m int8 [rows, d], d_m_scale [rows]), routing given, as compact_moe_ffn; silu(gate) * up is
+ * rounded to the storage type and then to codes, a row for each of its experts.  Indices outside 0 .. n_experts - 1 choose no
+ * expert.  d_y may be d_h.  bf16 storage only; at most 2^26 / top_k rows. */
+int compact_moe_ffn_i8_workspace_bytes(const compact_ctx* ctx, int64_t rows, size_t* bytes);
+int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const void* d_m, const float* d_m_scale, const void* d_h,
+                       const int32_t* d_expert_idx, const float* d_weight, int64_t rows, void* d_y, void* d_workspace,
+                       size_t ws_bytes, void* hip_stream);
+
 /* ---- per-kernel timing ----------------------------------------------------
  * When enabled, every launch of the selected kernel class is bracketed by HIP
  * events on the launch stream.  compact_profile_read synchronises those

@@ -29,6 +29,8 @@ EXPORTS = [
     "compact_mixed_workspace_bytes", "compact_mixed_forward",
     "compact_prefix_stack_workspace_bytes", "compact_prefix_stack_forward",
     "compact_paged_plan", "compact_rope_paged_write", "compact_paged_workspace_bytes", "compact_attn_paged",
+    "compact_quant_i8", "compact_gemm_i8_workspace_bytes", "compact_gemm_i8", "compact_block_norm", "compact_route",
+    "compact_moe_ffn_i8_workspace_bytes", "compact_moe_ffn_i8",
 ]
 
 
@@ -63,6 +65,15 @@ class PagedKVStruct(C.Structure):
 class PagedStepStruct(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("d_n_new", "d_len", "d_n_free", "d_free", "d_n_free_out", "d_n_refused", "d_len_out",
                                           "d_kv_len", "d_cu", "d_slot", "d_rot")] + [("max_rows", C.c_int32)]
+
+
+class RouteRuleStruct(C.Structure):
+    _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("topk_groups", C.c_int32), ("group_top", C.c_int32), ("renorm", C.c_int32),
+                ("factor", C.c_float)]
+
+
+class ExpertsI8Struct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_gate_up", "d_gate_up_scale", "d_down", "d_down_scale")]
 
 
 class CompactError(RuntimeError):
@@ -119,6 +130,13 @@ def lib():
     L.compact_rope_paged_write.argtypes = [vp, i32, vp, P(PagedKVStruct), vp, vp, vp, vp]
     L.compact_paged_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, P(sz)]
     L.compact_attn_paged.argtypes = [vp, P(PagedKVStruct), i32, vp, vp, i32, i32, vp, i64, vp, vp, sz, vp]
+    L.compact_quant_i8.argtypes = [vp, vp, i64, i64, i32, vp, vp, vp]
+    L.compact_gemm_i8_workspace_bytes.argtypes = [vp, i64, i32, i32, i32, P(sz)]
+    L.compact_gemm_i8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, sz, vp]
+    L.compact_block_norm.argtypes = [vp, vp, vp, vp, vp, i64, C.c_float, vp, vp, vp, vp, vp, i64, vp]
+    L.compact_route.argtypes = [vp, P(RouteRuleStruct), vp, vp, vp, vp, i64, vp, vp, vp]
+    L.compact_moe_ffn_i8_workspace_bytes.argtypes = [vp, i64, P(sz)]
+    L.compact_moe_ffn_i8.argtypes = [vp, P(ExpertsI8Struct), vp, vp, vp, vp, vp, i64, vp, vp, sz, vp]
     for name in EXPORTS:
         fn = getattr(L, name)
         if name not in ("compact_destroy", "compact_last_error"):
@@ -303,6 +321,24 @@ class PagedStep:
         if c is not None:      # (the arrays are the same ones, and have been looked at)
             c.d_len, c.d_len_out, c.d_n_free, c.d_n_free_out = c.d_len_out, c.d_len, c.d_n_free_out, c.d_n_free
             object.__setattr__(self, "_c", c)
+
+
+class RouteRule:
+    """How compact_route chooses (compact_route_rule): score "softmax" or "sigmoid"; n_groups groups of experts of which topk_groups (None: all)
+    are eligible, ranked by the sum of their group_top best; renorm divides the weights by their sum, factor multiplies them."""
+
+    def __init__(self, score="softmax", n_groups=1, topk_groups=None, group_top=1, renorm=True, factor=1.0):
+        if score not in ("softmax", "sigmoid"):
+            _refuse("route: score %r; softmax or sigmoid needed" % (score,))
+        self.c = RouteRuleStruct(int(score == "sigmoid"), n_groups, n_groups if topk_groups is None else topk_groups, group_top, bool(renorm), factor)
+        self.ref = C.byref(self.c)
+
+
+class ExpertsI8:
+    """Expert weights as codes (compact_experts_i8): gate_up int8 [E, 2F, d], gate_up_scale fp32 [E, 2F], down int8 [E, d, F], down_scale [E, d]."""
+
+    def __init__(self, gate_up, gate_up_scale, down, down_scale):
+        self.gate_up, self.gate_up_scale, self.down, self.down_scale = gate_up, gate_up_scale, down, down_scale
 
 
 class Layer:
@@ -525,6 +561,138 @@ class Layer:
                     % (q.dtype, tuple(q.shape), q.stride(), q.device, ws if ws is None else ws.device, self.q_cols, dt))
         rc = self.L.compact_attn_paged(self.ctx, ref, rows, cu.data_ptr(), kv_len.data_ptr(), max_new, max_kv_len, q.data_ptr(), apart[0],
                                        o.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream(device))
+        if rc:
+            self.check(rc)
+
+    # -- 8-bit integer weights ------------------------------------------------------
+    # (every array is held against the sizes that the kernels go by; the comparisons are written out, as above)
+    def compact_quant_i8(self, x, q, scale):
+        """x [rows, cols] (its rows may be apart) -> codes q int8 [rows, cols], scale fp32 [rows]."""
+        device, shape = torch.cuda.current_device(), x.shape
+        if len(shape) != 2:
+            _refuse("x: %s, [rows, cols] needed" % (tuple(shape),))
+        rows, cols = shape
+        apart, step = x.stride()
+        if rows <= 1:
+            apart = cols
+        if (x.dtype is not self.torch_dtype or x.get_device() != device or step != 1 and cols > 1
+                or q.dtype is not torch.int8 or q.shape != shape or q.get_device() != device or not q.is_contiguous()
+                or scale.dtype is not torch.float32 or scale.numel() < rows or scale.get_device() != device or not scale.is_contiguous()):
+            _array(q, torch.int8, rows * cols, device, "codes")
+            _array(scale, torch.float32, rows, device, "scale")
+            _refuse("x: %s %s with strides %s on %s, codes %s; [rows, cols] of %s with whole rows on the current GPU, codes of its shape needed"
+                    % (x.dtype, tuple(shape), x.stride(), x.device, tuple(q.shape), self.torch_dtype))
+        rc = self.L.compact_quant_i8(self.ctx, x.data_ptr(), apart, rows, cols, q.data_ptr(), scale.data_ptr(), _raw_stream(device))
+        if rc:
+            self.check(rc)
+
+    def gemm_i8_workspace_bytes(self, M, N, K, epilogue=0):
+        n = C.c_size_t()
+        self.check(self.L.compact_gemm_i8_workspace_bytes(self.ctx, M, N, K, epilogue, C.byref(n)))
+        return n.value
+
+    def compact_gemm_i8(self, a, a_scale, b, b_scale, r, c, epilogue=0):
+        """a int8 [M, K], b int8 [N, K] (epilogue 1: [2N, K]), their scales fp32, r and c [M, N].  The workspace is self.ws, if there is one."""
+        device, dt, ws = torch.cuda.current_device(), self.torch_dtype, self.ws
+        if len(a.shape) != 2 or len(b.shape) != 2 or len(c.shape) != 2:
+            _refuse("product: a %s, b %s, c %s; [M, K], [N, K] and [M, N] needed" % (tuple(a.shape), tuple(b.shape), tuple(c.shape)))
+        (M, K), (M2, N), (n, K2) = a.shape, c.shape, b.shape
+        if (M2 != M or K2 != K or n != (2 * N if epilogue == 1 else N)
+                or a.dtype is not torch.int8 or a.get_device() != device or not a.is_contiguous()
+                or b.dtype is not torch.int8 or b.get_device() != device or not b.is_contiguous()
+                or a_scale.dtype is not torch.float32 or a_scale.numel() < M or a_scale.get_device() != device or not a_scale.is_contiguous()
+                or b_scale.dtype is not torch.float32 or b_scale.numel() < n or b_scale.get_device() != device or not b_scale.is_contiguous()
+                or c.dtype is not dt or c.get_device() != device or not c.is_contiguous()
+                or r is not None and (r.dtype is not dt or r.shape != c.shape or r.get_device() != device or not r.is_contiguous())
+                or ws is not None and ws.get_device() != device):
+            _array(a, torch.int8, 0, device, "a")
+            _array(b, torch.int8, 0, device, "b")
+            _array(a_scale, torch.float32, M, device, "a_scale")
+            _array(b_scale, torch.float32, n, device, "b_scale")
+            _array(c, dt, 0, device, "c")
+            if r is not None:
+                _array(r, dt, 0, device, "r")
+            _refuse("product: a %s, b %s, r %s, c %s, epilogue %d, workspace on %s do not belong together"
+                    % (tuple(a.shape), tuple(b.shape), None if r is None else tuple(r.shape), tuple(c.shape), epilogue, None if ws is None else ws.device))
+        rc = self.L.compact_gemm_i8(self.ctx, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), None if r is None else r.data_ptr(),
+                                    c.data_ptr(), M, N, K, epilogue, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                    _raw_stream(device))
+        if rc:
+            self.check(rc)
+
+    def compact_block_norm(self, x, b=None, g_post=None, gate=None, alpha=1.0, h=None, g_pre=None, n=None, q=None, q_scale=None):
+        """Rows [rows, d_model]; h, n, q (int8) and q_scale (fp32 [rows]) are written where given.  gate: [d_model], or [rows, d_model] whose rows
+        may be apart."""
+        device, dt, shape, d = torch.cuda.current_device(), self.torch_dtype, x.shape, self.layer.d_model
+        if len(shape) != 2 or shape[1] != d:
+            _refuse("rows: %s, [rows, %d] needed" % (tuple(shape), d))
+        rows, ptr, gate_stride = shape[0], [], 0
+        for t in (x, b, h, n):
+            if t is None:
+                ptr.append(None)
+                continue
+            if t.dtype is not dt or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+                _refuse("rows: %s %s on %s; contiguous %s of %s on the current GPU needed" % (t.dtype, tuple(t.shape), t.device, dt, tuple(shape)))
+            ptr.append(t.data_ptr())
+        for t in (g_post, g_pre):
+            ptr.append(None if t is None else _array(t, dt, d, device, "gain"))
+        if gate is None:
+            ptr.append(None)
+        else:
+            if gate.dtype is not dt or gate.get_device() != device or gate.shape != shape and tuple(gate.shape) != (d,) or gate.stride(-1) != 1:
+                _refuse("gate: %s %s with strides %s on %s; [%d] or %s of %s on the current GPU needed"
+                        % (gate.dtype, tuple(gate.shape), gate.stride(), gate.device, d, tuple(shape), dt))
+            gate_stride = 0 if gate.dim() == 1 or rows <= 1 else gate.stride(0)
+            ptr.append(gate.data_ptr())
+        if q is not None and q.shape != shape:
+            _refuse("codes: %s, %s needed" % (tuple(q.shape), tuple(shape)))
+        rc = self.L.compact_block_norm(self.ctx, ptr[0], ptr[1], ptr[4], ptr[6], gate_stride, alpha, ptr[2], ptr[5], ptr[3],
+                                       None if q is None else _array(q, torch.int8, rows * d, device, "codes"),
+                                       None if q_scale is None else _array(q_scale, torch.float32, rows, device, "scale"), rows, _raw_stream(device))
+        if rc:
+            self.check(rc)
+
+    def compact_route(self, rule, logits, bias, idx, weight, m=None, w_router=None):
+        """logits fp32 [rows, n_experts], given, or written as m w_router^T where these are; bias fp32 [n_experts] or None; idx int32 and weight fp32
+        [rows, top_k]."""
+        device, E, k, shape = torch.cuda.current_device(), self.layer.n_experts, self.layer.top_k, logits.shape
+        if len(shape) != 2 or shape[1] != E:
+            _refuse("logits: %s, [rows, %d] needed" % (tuple(shape), E))
+        rows = shape[0]
+        if m is not None and m.shape != (rows, self.layer.d_model) or w_router is not None and w_router.shape != (E, self.layer.d_model):
+            _refuse("router: rows %s, weights %s; %s and %s needed" % (None if m is None else tuple(m.shape), None if w_router is None else tuple(w_router.shape),
+                                                                      (rows, self.layer.d_model), (E, self.layer.d_model)))
+        rc = self.L.compact_route(self.ctx, rule.ref, None if m is None else _array(m, self.torch_dtype, 0, device, "rows"),
+                                  None if w_router is None else _array(w_router, self.torch_dtype, 0, device, "router weights"),
+                                  _array(logits, torch.float32, 0, device, "logits"),
+                                  None if bias is None else _array(bias, torch.float32, E, device, "bias"), rows,
+                                  _array(idx, torch.int32, rows * k, device, "idx"), _array(weight, torch.float32, rows * k, device, "weight"),
+                                  _raw_stream(device))
+        if rc:
+            self.check(rc)
+
+    def moe_ffn_i8_workspace_bytes(self, rows):
+        n = C.c_size_t()
+        self.check(self.L.compact_moe_ffn_i8_workspace_bytes(self.ctx, rows, C.byref(n)))
+        return n.value
+
+    def compact_moe_ffn_i8(self, experts, m, m_scale, h, idx, weight, y):
+        """experts: ExpertsI8; m int8 [rows, d], m_scale fp32 [rows], h and y [rows, d], idx int32 and weight fp32 [rows, top_k].  The workspace is
+        self.ws."""
+        device, dt, i8, f32, ws = torch.cuda.current_device(), self.torch_dtype, torch.int8, torch.float32, self.ws
+        d, F, E, k, shape = self.layer.d_model, self.layer.ffn_dim, self.layer.n_experts, self.layer.top_k, m.shape
+        if len(shape) != 2 or shape[1] != d or h.shape != shape or y.shape != shape or ws is not None and ws.get_device() != device:
+            _refuse("rows: codes %s, h %s, y %s, workspace on %s; [rows, %d] on the current GPU needed"
+                    % (tuple(shape), tuple(h.shape), tuple(y.shape), None if ws is None else ws.device, d))
+        rows = shape[0]
+        if experts.gate_up.shape != (E, 2 * F, d) or experts.down.shape != (E, d, F):
+            _refuse("experts: gate_up %s, down %s; %s and %s needed" % (tuple(experts.gate_up.shape), tuple(experts.down.shape), (E, 2 * F, d), (E, d, F)))
+        e = ExpertsI8Struct(_array(experts.gate_up, i8, 0, device, "gate_up"), _array(experts.gate_up_scale, f32, E * 2 * F, device, "gate_up_scale"),
+                            _array(experts.down, i8, 0, device, "down"), _array(experts.down_scale, f32, E * d, device, "down_scale"))
+        rc = self.L.compact_moe_ffn_i8(self.ctx, C.byref(e), _array(m, i8, 0, device, "codes"), _array(m_scale, f32, rows, device, "scale"),
+                                       _array(h, dt, 0, device, "h"), _array(idx, torch.int32, rows * k, device, "idx"),
+                                       _array(weight, f32, rows * k, device, "weight"), rows, _array(y, dt, 0, device, "y"),
+                                       None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream(device))
         if rc:
             self.check(rc)
 

@@ -147,18 +147,6 @@ extern "C" const char* compact_last_error(const compact_ctx* ctx) { return ctx ?
 // workspace carving: the same routine sizes the workspace (base == nullptr)
 // and hands out its pieces
 // ---------------------------------------------------------------------------
-struct Carver {
-    char* base;
-    size_t off = 0;
-    explicit Carver(void* b) : base((char*)b) {}
-    void* take(size_t bytes) {
-        off = align_up(off, 256);
-        void* p = base ? base + off : nullptr;
-        off += bytes;
-        return p;
-    }
-};
-
 struct PrefillBufs {
     void *n, *qkv, *o, *h, *act;
     // MoE
@@ -193,7 +181,7 @@ static int moe_min_mtile(const compact_layer_cfg& c) { return c.dtype == COMPACT
 
 // mt = rows per tile of the plan's tile map: the row tile of the prefill-size expert GEMMs, or 16 for the decode
 // steps' per-expert streaming
-static void carve_moe_plan(Carver& cv, const compact_layer_cfg& c, int64_t rows, MoePlan& plan, int mt) {
+void carve_moe_plan(Carver& cv, const compact_layer_cfg& c, int64_t rows, MoePlan& plan, int mt) {
     const int64_t rk = rows * c.top_k;
     plan.max_mtiles = (int32_t)(rk / mt + c.n_experts + 1);
     plan.counts = (int32_t*)cv.take(sizeof(int32_t) * c.n_experts);
@@ -468,12 +456,6 @@ static int gemm_partials(compact_ctx* ctx, const void* A, const void* B, float* 
     ProfileScope ps(ctx, COMPACT_K_GEMM_SKINNY, s);
     return launch_gemm_skinny(ctx, (const bf16*)A, (const bf16*)B, partials, M, N, K, *ks, s);
 }
-
-#define TRY(expr)                      \
-    do {                               \
-        const int _rc = (expr);        \
-        if (_rc != COMPACT_OK) return _rc; \
-    } while (0)
 
 // ---------------------------------------------------------------------------
 // prefill

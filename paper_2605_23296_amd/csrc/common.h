@@ -108,6 +108,11 @@ int device_cu_count(compact_ctx* ctx, int* n_cus);
             return set_err(ctx, COMPACT_EHIP, std::string(#expr) + ": " + hipGetErrorString(_e)); \
     } while (0)
 #define LAUNCH_CHECK(ctx) HIP_TRY(ctx, hipGetLastError())
+#define TRY(expr)                      \
+    do {                               \
+        const int _rc = (expr);        \
+        if (_rc != COMPACT_OK) return _rc; \
+    } while (0)
 
 // The value itself, computed where it stands: keeps what derives from it in a rare branch from being hoisted out of the
 // loop into registers that the loop needs (a spilled register's reload would wait for every load in flight).
@@ -146,6 +151,18 @@ __device__ __forceinline__ void wait_all_memory() {
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline size_t dtype_size(int dtype) { return dtype == COMPACT_BF16 ? 2 : 4; }
+// buffers one after another in a caller's workspace (null base: only counts)
+struct Carver {
+    char* base;
+    size_t off = 0;
+    explicit Carver(void* b) : base((char*)b) {}
+    void* take(size_t bytes) {
+        off = align_up(off, 256);
+        void* p = base ? base + off : nullptr;
+        off += bytes;
+        return p;
+    }
+};
 
 // ---------------------------------------------------------------------------
 // kernel launchers (one translation unit each)
@@ -316,6 +333,8 @@ struct MoePlan {              // device buffers carved from the workspace
     int32_t* tile_rows;
     int32_t max_mtiles;
 };
+// mt: rows per tile of the plan's tile map, which has room for rows * top_k routed rows
+void carve_moe_plan(Carver& cv, const compact_layer_cfg& c, int64_t rows, MoePlan& plan, int mt);
 int launch_moe_route(compact_ctx* ctx, const void* m, const void* w_router, int64_t rows, int32_t* idx,
                      float* gate, float* logits, hipStream_t s,
                      float* partials_ws = nullptr);   // partials_ws: [ks][rows][E] scratch; enables the few-rows path
@@ -332,3 +351,39 @@ int launch_moe_combine_partials(compact_ctx* ctx, const float* partials, int ks,
 // h_is_f32: the residual h is fp32 (decode) instead of the storage type
 int launch_moe_combine(compact_ctx* ctx, const void* expert_out, const void* h, bool h_is_f32,
                        const int32_t* slot_of, int64_t rows, void* y, hipStream_t s);
+
+// int8_rows.hip : rows and their codes
+int launch_quant_i8(compact_ctx* ctx, const void* x, int64_t x_stride, int64_t rows, int cols, int8_t* q, float* scale, hipStream_t s);
+struct BlockNormArgs {
+    const void *x, *b, *g_post, *gate;   // b, g_post, gate: null = none
+    int64_t gate_stride;
+    float alpha;
+    void* h;                             // null: not wanted; the same for n, q and q_scale
+    const void* g_pre;
+    void* n;
+    int8_t* q;
+    float* q_scale;
+    int64_t rows;
+};
+int launch_block_norm(compact_ctx* ctx, const BlockNormArgs& a, hipStream_t s);
+
+// gemm_i8.hip : products of codes
+struct GemmI8Args {
+    const int8_t* a;
+    const float* a_scale;
+    const int8_t* b;
+    const float* b_scale;
+    const void* r;            // storage type; null = none
+    void* c;
+    int64_t M;
+    int N, K, epilogue;
+    const GroupedArgs* grouped;   // experts: row-tile map; b_expert_stride in bytes, b_scale [E][N or 2N]
+};
+size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue);
+int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_bytes, hipStream_t s);
+// row-tile height of the experts' products over `rows` routed rows
+int gemm_i8_group_mtile(int64_t rows, int n_experts);
+
+// route.hip
+int launch_route(compact_ctx* ctx, const compact_route_rule& rule, const float* logits, const float* bias, int64_t rows, int32_t* idx,
+                 float* weight, hipStream_t s);

@@ -149,8 +149,11 @@ __global__ __launch_bounds__(256) void expert_rank_kernel(const int32_t* __restr
     for (int j = 0; j < PER; ++j) {
         e[j] = -1;
         if (i0 + j < n) {
-            e[j] = idx[i0 + j];
-            lr[j] = atomicAdd(&lc[e[j]], 1);
+            const int v = idx[i0 + j];   // (outside 0 .. E - 1: no expert)
+            if (v >= 0 && v < E) {
+                e[j] = v;
+                lr[j] = atomicAdd(&lc[v], 1);
+            }
         }
     }
     __syncthreads();
@@ -198,12 +201,17 @@ __global__ __launch_bounds__(256) void expert_scan_kernel(const int32_t* __restr
 
 __global__ __launch_bounds__(256) void expert_scatter_kernel(const int32_t* __restrict__ idx, const float* __restrict__ gate,
                                                              const int32_t* rank,
-                                                             const int32_t* __restrict__ offsets, int64_t n, int k,
+                                                             const int32_t* __restrict__ offsets, int64_t n, int k, int E,
                                                              int32_t* __restrict__ sorted_token,
                                                              float* __restrict__ sorted_gate, int32_t* slot_of) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
-    const int pos = offsets[idx[i]] + rank[i];
+    const int e = idx[i];
+    if (e < 0 || e >= E) {
+        slot_of[i] = -1;
+        return;
+    }
+    const int pos = offsets[e] + rank[i];
     sorted_token[pos] = (int32_t)(i / k);
     sorted_gate[pos] = gate[i];
     slot_of[i] = pos;
@@ -289,13 +297,16 @@ __device__ __forceinline__ void plan_small(int t, int my, float gate, int n, int
         o.sorted_token[pos] = t / k;
         o.sorted_gate[pos] = gate;
         o.slot_of[t] = pos;
+    } else if (t < n) {
+        o.slot_of[t] = -1;
     }
 }
 
 __global__ __launch_bounds__(256) void moe_plan_small_kernel(const int32_t* __restrict__ idx, const float* __restrict__ gate, int n,
                                                              int k, int E, int mtile, const PlanOut out) {
     const int t = threadIdx.x;
-    plan_small(t, t < n ? idx[t] : -1, t < n ? gate[t] : 0.f, n, k, E, mtile, out);
+    const int e = t < n ? idx[t] : -1;   // (outside 0 .. E - 1: no expert)
+    plan_small(t, e < E ? e : -1, t < n ? gate[t] : 0.f, n, k, E, mtile, out);
 }
 
 // Decode: logits (split-K partials), top-k and plan in one workgroup of 16 wavefronts, a row per wavefront.
@@ -365,7 +376,7 @@ int launch_moe_plan(compact_ctx* ctx, const int32_t* idx, const float* gate, int
     expert_rank_kernel<<<(unsigned)((n + 1023) / 1024), 256, 0, s>>>(idx, n, c.n_experts, plan.counts, plan.slot_of);
     expert_scan_kernel<<<1, 256, 0, s>>>(plan.counts, c.n_experts, mtile, plan.offsets, plan.tile_expert, plan.tile_row0,
                                          plan.tile_rows, plan.max_mtiles);
-    expert_scatter_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(idx, gate, plan.slot_of, plan.offsets, n, c.top_k,
+    expert_scatter_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(idx, gate, plan.slot_of, plan.offsets, n, c.top_k, c.n_experts,
                                                                       plan.sorted_token, plan.sorted_gate, plan.slot_of);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
@@ -383,8 +394,10 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const T* __restrict__ 
         float acc[8];
         load8(hres + row * d + c, acc);
         for (int j = 0; j < k; ++j) {
+            const int64_t slot = slot_of[row * k + j];
+            if (slot < 0) continue;   // an index that is no expert's
             float v[8];
-            load8(expert_out + (int64_t)slot_of[row * k + j] * d + c, v);
+            load8(expert_out + slot * d + c, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] += v[e];
         }
