@@ -167,7 +167,9 @@ extern "C" int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* ex
         return set_err(ctx, COMPACT_EWORKSPACE, "workspace too small for the expert feed-forward");
     hipStream_t s = (hipStream_t)hip_stream;
     const int64_t rk = rows * c.top_k;
-    const int mtile = gemm_i8_group_mtile(rk, c.n_experts);
+    int n_cus = 0;
+    TRY(device_cu_count(ctx, &n_cus));
+    const int mtile = gemm_i8_group_mtile(rk, c.n_experts, c.ffn_dim, c.d_model, n_cus);
     TRY(launch_moe_plan(ctx, d_expert_idx, d_weight, rows, mtile, b.plan, s));
     GroupedArgs g{};
     g.mtile = mtile;

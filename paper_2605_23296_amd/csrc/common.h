@@ -382,7 +382,7 @@ struct GemmI8Args {
 size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue);
 int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_bytes, hipStream_t s);
 // row-tile height of the experts' products over `rows` routed rows
-int gemm_i8_group_mtile(int64_t rows, int n_experts);
+int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus);
 
 // route.hip
 int launch_route(compact_ctx* ctx, const compact_route_rule& rule, const float* logits, const float* bias, int64_t rows, int32_t* idx,

@@ -655,17 +655,6 @@ static int launch_small(compact_ctx* ctx, GemmParams& p, hipStream_t s, int k_sl
     return COMPACT_OK;
 }
 
-// How the 256 x 256 kernel cuts M rows: slots of 256 x 256 (a last row tile of more than 128 rows is one), and 128 x 256
-// tiles of a bottom row tile of at most 128 rows.
-struct LargeTiles {
-    int64_t slots;
-    int64_t bottom;
-};
-static LargeTiles large_tiles(int64_t M, int n_ntiles) {
-    const int64_t rest = M % 256;
-    return {(M / 256 + (rest > 128 ? 1 : 0)) * n_ntiles, rest > 0 && rest <= 128 ? n_ntiles : 0};
-}
-
 // n_full (plain products): slots of 256 x 256 that are whole tiles, see the kernel
 template <int EPI, bool GROUPED>
 static int launch_large(compact_ctx* ctx, GemmParams& p, int64_t n_full, int n_cus, hipStream_t s) {
@@ -722,7 +711,6 @@ struct TileForm {
     int bm, bn;
     double t_idle, t_load, t_tile;
 };
-enum { TILE_256 = 0, TILE_128, TILE_128_128, TILE_128_64, TILE_64_128, TILE_64_64, TILE_FORMS };
 static const TileForm tile_forms[TILE_FORMS] = {{256, 256, 1.00, 0.70, 4.8}, {128, 256, 0.75, 0.24, 2.7}, {128, 128, 0.55, 0.13, 1.7},
                                                 {128, 64, 0.31, 0.03, 2.2},  {64, 128, 0.40, 0.04, 3.3},  {64, 64, 0.25, 0.05, 2.5}};
 
@@ -755,7 +743,7 @@ static double large_cost(int64_t n_full, int64_t halves, int K, int n_cus) {
     return end;
 }
 
-static int pick_tile(int64_t M, int N, int K, int epilogue, int n_cus, int64_t* n_full) {
+int pick_tile(int64_t M, int N, int K, int epilogue, int n_cus, int64_t* n_full) {
     // every slot a whole tile, whole rounds of them and the rest in halves, one round less, or halves only
     const int outn = epilogue == 1 ? 128 : 256, n_ntiles = (N + outn - 1) / outn;
     const LargeTiles lt = large_tiles(M, n_ntiles);

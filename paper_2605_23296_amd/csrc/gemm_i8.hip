@@ -1,6 +1,8 @@
 // Products of 8-bit codes:  C[m, n] = a_scale[m] b_scale[n] sum_k A[m, k] B[n, k], the sum in 32-bit integers.  Integer sums are the
 // same in any order, so every tile form and every split of K gives the same bits.
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "common.h"
 #include "gemm_ring.h"
@@ -21,6 +23,8 @@ struct GemmI8Params {
     int N;    // output columns (F for SwiGLU, whose W has 2N rows)
     int K;
     int n_mtiles, n_ntiles;
+    int n_full;  // 256 x 256 kernel, plain product: workgroups that take a whole tile (the others take halves)
+    int* sums;   // of k-slices
     int f32;  // C and R are fp32 rather than bf16
     GroupedArgs g;
 };
@@ -56,12 +60,30 @@ __device__ __forceinline__ I8Tile i8_tile(const GemmI8Params& p) {
     return t;
 }
 
+// the kernel may use that much LDS, on every device that it runs on (a set bit is a device that knows)
+static int allow_lds(compact_ctx* ctx, const void* kernel, size_t bytes, std::atomic<uint64_t>& known) {
+    int dev = 0;
+    HIP_TRY(ctx, hipGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (known.load(std::memory_order_relaxed) & bit) return COMPACT_OK;
+    HIP_TRY(ctx, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    known.fetch_or(bit, std::memory_order_relaxed);
+    return COMPACT_OK;
+}
+
 // One output from its sums; the same roundings wherever it is computed.
 #pragma clang fp contract(off)
 __device__ __forceinline__ float i8_value(int sum, float xs, float ws) { return (float)sum * xs * ws; }
 __device__ __forceinline__ float i8_glu(float g, float u, bool f32) {
     const float e = f32 ? expf(-g) : __expf(-g);   // (__expf: off by up to 3.4e-6 of the value at g = -80)
     return g / (1.0f + e) * u;
+}
+
+__device__ __forceinline__ void i8_put(const GemmI8Params& p, int64_t o, float v) {
+    if (p.f32)
+        ((float*)p.C)[o] = v + (p.R ? ((const float*)p.R)[o] : 0.f);
+    else
+        ((bf16*)p.C)[o] = (bf16)(v + (p.R ? (float)((const bf16*)p.R)[o] : 0.f));
 }
 
 // Epilogue of one wavefront: TM x TN MFMA tiles, 16 output rows per pass through a slab of its own [16][WOUT + 4].  acc[i][j][e]: output
@@ -136,15 +158,35 @@ __device__ __forceinline__ void i8_store(const GemmI8Params& p, const I8Tile& tp
                     store8((bf16*)p.C + o, v);
                 }
             } else {
-                for (int e = 0; e < 8 && n + e < p.N; ++e) {
-                    if (p.f32)
-                        ((float*)p.C)[o + e] = v[e] + (p.R ? ((const float*)p.R)[o + e] : 0.f);
-                    else
-                        ((bf16*)p.C)[o + e] = (bf16)(v[e] + (p.R ? (float)((const bf16*)p.R)[o + e] : 0.f));
-                }
+                for (int e = 0; e < 8 && n + e < p.N; ++e) i8_put(p, o + e, v[e]);
             }
         }
         __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Sums of a k-slice as they are: [slice][row][N, SwiGLU: 2N].
+template <bool GLU, int TM, int TN>
+__device__ __forceinline__ void i8_store_sums(const GemmI8Params& p, const I8Tile& tp, const intx4 (&acc)[TM][TN], int lane, int wrow,
+                                              int n_first) {
+    constexpr int TJ = GLU ? TN / 2 : TN;
+    const int r = lane & 15, c4 = lane >> 4, cols = GLU ? 2 * p.N : p.N;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int lm = wrow + i * 16 + r;
+        if (lm >= tp.rows_valid) continue;
+        int* row = p.sums + ((int64_t)blockIdx.y * p.M + tp.m0 + lm) * cols;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int n = n_first + (j % TJ) * 16 + c4 * 4, at = j < TJ ? n : p.N + n;
+            if (n + 4 <= p.N && p.N % 4 == 0) {
+                *reinterpret_cast<intx4*>(row + at) = acc[i][j];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < p.N) row[at + e] = acc[i][j][e];
+            }
+        }
     }
 }
 
@@ -189,9 +231,10 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_tile_kernel(const GemmI8P
         wc[u] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
         wsrc[u] = tp.W + (int64_t)n * p.K + wc[u];
     }
-    const int nk = (p.K + BK - 1) / BK;
+    // gridDim.y slices of K (partial sums): this workgroup's k-tiles
+    const int n_k = (p.K + BK - 1) / BK, k_lo = n_k * blockIdx.y / gridDim.y, nk = n_k * (blockIdx.y + 1) / gridDim.y - k_lo;
     auto gload = [&](int kt, int stage) {
-        const int k0 = min(kt, nk - 1) * BK;   // past the end: the last k-tile again, into a stage nobody reads
+        const int k0 = (k_lo + min(kt, nk - 1)) * BK;   // past the end: the last k-tile again, into a stage nobody reads
         char* dst = smem + stage * STAGE;
         if (k0 + BK <= p.K) {
 #pragma unroll
@@ -243,37 +286,396 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_tile_kernel(const GemmI8P
         stage = stage + 1 == S ? 0 : stage + 1;
         fill = fill + 1 == S ? 0 : fill + 1;
     }
+    if (gridDim.y > 1) {
+        i8_store_sums<GLU, TM, TN>(p, tp, acc, lane, wm * WTM, tp.n0 + wn * WOUT);
+        return;
+    }
     ring_barrier<0>();   // the repeated loads must not land in the slabs
     i8_store<GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), lane, wm * WTM, tp.n0 + wn * WOUT);
 }
 
+// Sums of k-slices -> outputs, 4 columns a thread.
+template <bool GLU>
+__global__ __launch_bounds__(256) void gemm_i8_finish_kernel(const GemmI8Params p, int slices) {
+    const int cols = GLU ? 2 * p.N : p.N;
+    const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t m = blockIdx.y;
+    if (n >= p.N) return;
+    const float xs = p.xs[m];
+    int g[4] = {0, 0, 0, 0}, u[4] = {0, 0, 0, 0};
+    for (int s = 0; s < slices; ++s) {
+        const int* row = p.sums + ((int64_t)s * p.M + m) * cols + n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) {
+                g[e] += row[e];
+                if (GLU) u[e] += row[p.N + e];
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < p.N) {
+            float v = i8_value(g[e], xs, p.ws[n + e]);
+            if (GLU) v = i8_glu(v, i8_value(u[e], xs, p.ws[p.N + n + e]), p.f32);
+            i8_put(p, m * p.N + n + e, v);
+        }
+}
+
 template <int BM, int BN, int WM, int WN, int S, bool GLU, bool GROUPED>
-static int launch_tile(compact_ctx* ctx, GemmI8Params& p, hipStream_t s) {
+static int launch_tile(compact_ctx* ctx, GemmI8Params& p, hipStream_t s, int slices = 1) {
     constexpr int OUTN = GLU ? BN / 2 : BN;
     if (!GROUPED) p.n_mtiles = (int)((p.M + BM - 1) / BM);
     p.n_ntiles = (p.N + OUTN - 1) / OUTN;
     constexpr size_t smem = (size_t)S * (BM + BN) * I8_BK;
-    static_assert(smem <= 64 * 1024, "no attribute needed");
+    static std::atomic<uint64_t> lds_set{0};
+    TRY(allow_lds(ctx, (const void*)gemm_i8_tile_kernel<BM, BN, WM, WN, S, GLU, GROUPED>, smem, lds_set));
     const int64_t tiles = (int64_t)p.n_mtiles * p.n_ntiles;
     if (tiles == 0) return COMPACT_OK;
     if (tiles > 0x7fffffff) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
-    gemm_i8_tile_kernel<BM, BN, WM, WN, S, GLU, GROUPED><<<(unsigned)tiles, WM * WN * 64, smem, s>>>(p);
+    gemm_i8_tile_kernel<BM, BN, WM, WN, S, GLU, GROUPED><<<dim3((unsigned)tiles, (unsigned)slices), WM * WN * 64, smem, s>>>(p);
+    LAUNCH_CHECK(ctx);
+    if (slices > 1) {
+        gemm_i8_finish_kernel<GLU><<<dim3((unsigned)((p.N + 1023) / 1024), (unsigned)p.M), 256, 0, s>>>(p, slices);
+        LAUNCH_CHECK(ctx);
+    }
+    return COMPACT_OK;
+}
+
+// ---------------------------------------------------------------------------
+// 256 x 256 outputs per workgroup, 8 wavefronts of 128 x 64.  The k-tiles pass through LDS as half tiles of 128 rows (16 KB), a ring of
+// eight; a k-tile is four phases, one per quarter of the wavefront's output: read the half tile that the quarter needs newly (X0, W1,
+// X1, then W0 of the next k-tile; the other operand is still in registers), request one half tile seven phases ahead, join a
+// barrier, run 16 MFMAs, join a barrier.  The two wavefronts of a SIMD belong to groups that run half a phase apart, so that
+// one's MFMAs cover the other's reads and requests; barriers wait for LDS reads and for all but the newest 12 loads.
+// ---------------------------------------------------------------------------
+typedef std::integral_constant<int, 0> I0;
+typedef std::integral_constant<int, 1> I1;
+typedef std::integral_constant<int, 2> I2;
+typedef std::integral_constant<int, 3> I3;
+
+// 16 MFMAs of 64 x 32 outputs over 128 codes
+template <int I, int J, int TM, int TN>
+__device__ __forceinline__ void i8_mfmas(intx4 (&acc)[TM][TN], const intx4 (&xf)[4][2], const intx4 (&wf)[2][2]) {
+    wave_priority_high();
+#pragma unroll
+    for (int n = 0; n < 16; ++n) {
+        const int kk = n >> 3, mt = (n >> 1) & 3, nt = (n & 1) ^ (mt & 1);
+        acc[4 * I + mt][2 * J + nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[nt][kk], xf[mt][kk], acc[4 * I + mt][2 * J + nt], 0, 0, 0);
+    }
+    wave_priority_normal();
+    plain_barrier();
+}
+
+// TAIL: K is no multiple of 128; chunks beyond it are zeros on the activations' side, the row's first chunk on the weights'
+template <bool TAIL, bool X>
+__device__ __forceinline__ void i8_load_piece(const int8_t* src, int chunk, int kt, int nk, int K, char* dst) {
+    const int k0 = kt * I8_BK;
+    if (!TAIL || kt + 1 < nk)
+        load16_to_lds(src + k0, dst);
+    else
+        load16_to_lds(k0 + chunk < K ? src + k0 : X ? zero_codes : src - chunk, dst);
+}
+
+template <bool GLU, bool GROUPED, bool TAIL>
+__device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile& tp, char* smem) {
+    constexpr int WN = 4, BK = I8_BK, WTM = 128, WTN = 64, TM = WTM / 16, TN = WTN / 16, HT = 128 * BK;
+    constexpr int WOUT = GLU ? WTN / 2 : WTN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int r = lane & 15, c4 = lane >> 4;
+
+    // Half tiles q = 0: W0, 1: X0, 2: W1, 3: X1 (the order they are read in).  Half i of X holds tile rows wm * 128 + i * 64 + .., half j of W
+    // the columns wn * 64 + j * 32 + .. of every wavefront (SwiGLU: half 0 the gate rows, half 1 the up rows of the same columns).  One
+    // instruction of a wavefront fills 1 KB = 8 rows of 8 chunks, lane l at (row l / 8, position l % 8).
+    const int8_t* src[4][2];
+    int chunk[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int row = (wave * 2 + u) * 8 + (lane >> 3);   // row of the half tile
+        chunk[u] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            int64_t sr = tp.m0 + min((row >> 6) * 128 + i * 64 + (row & 63), tp.rows_valid - 1);
+            if (GROUPED && p.g.a_gather) sr = p.g.a_gather[sr];
+            src[1 + 2 * i][u] = p.X + sr * p.K + chunk[u];
+            const int n = GLU ? min(tp.n0 + row, p.N - 1) + i * p.N : min(tp.n0 + (row >> 5) * 64 + i * 32 + (row & 31), p.N - 1);
+            src[2 * i][u] = tp.W + (int64_t)n * p.K + chunk[u];
+        }
+    }
+    intx4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = intx4{0, 0, 0, 0};
+    const int nk = (p.K + BK - 1) / BK;
+    int foff[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) foff[kk] = r * BK + (((4 * kk + c4) ^ ((r >> 1) & 7)) << 4);
+    const char* xs = smem + wm * 64 * BK;
+    const char* ws = smem + wn * 32 * BK;
+
+    auto gload = [&](auto qtag, int kt, int buf) __attribute__((always_inline)) {
+        constexpr int q = decltype(qtag)::value;
+        char* dst = smem + (buf * 4 + q) * HT + wave * 2 * 8 * BK;
+        i8_load_piece<TAIL, q % 2 == 1>(src[q][0], chunk[0], kt, nk, p.K, dst);
+        i8_load_piece<TAIL, q % 2 == 1>(src[q][1], chunk[1], kt, nk, p.K, dst + 8 * BK);
+    };
+    intx4 xf[4][2];
+    auto read_w = [&](auto jtag, int buf, intx4 (&f)[2][2]) __attribute__((always_inline)) {
+        constexpr int q = 2 * decltype(jtag)::value;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) f[nt][kk] = *reinterpret_cast<const intx4*>(ws + (buf * 4 + q) * HT + nt * 16 * BK + foff[kk]);
+    };
+    auto read_x = [&](auto itag, int buf) __attribute__((always_inline)) {
+        constexpr int q = 1 + 2 * decltype(itag)::value;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) xf[mt][kk] = *reinterpret_cast<const intx4*>(xs + (buf * 4 + q) * HT + mt * 16 * BK + foff[kk]);
+    };
+    // One k-tile = four phases (X0 W0, X0 W1, X1 W1, X1 W0); wa holds W0 of this tile, wb receives W1 and then W0 of the next.  Past the end of
+    // K the last k-tile is loaded again, into slots nobody reads.
+    auto k_tile = [&](int kt, int buf, intx4 (&wa)[2][2], intx4 (&wb)[2][2]) __attribute__((always_inline)) {
+        const int kn = min(kt + 2, nk - 1);
+        read_x(I0{}, buf);
+        gload(I0{}, kn, buf);
+        ring_barrier<12>();
+        i8_mfmas<0, 0>(acc, xf, wa);
+        read_w(I1{}, buf, wb);
+        gload(I1{}, kn, buf);
+        ring_barrier<12>();
+        i8_mfmas<0, 1>(acc, xf, wb);
+        read_x(I1{}, buf);
+        gload(I2{}, kn, buf);
+        ring_barrier<12>();
+        i8_mfmas<1, 1>(acc, xf, wb);
+        read_w(I0{}, buf ^ 1, wb);
+        gload(I3{}, kn, buf);
+        ring_barrier<12>();
+        i8_mfmas<1, 0>(acc, xf, wa);
+    };
+    {   // all half tiles of k-tiles 0 and 1; W0 and X0 of k-tile 0 have landed when all but 12 loads have
+        const int k1 = min(1, nk - 1);
+        gload(I0{}, 0, 0);
+        gload(I1{}, 0, 0);
+        gload(I2{}, 0, 0);
+        gload(I3{}, 0, 0);
+        gload(I0{}, k1, 1);
+        gload(I1{}, k1, 1);
+        gload(I2{}, k1, 1);
+        gload(I3{}, k1, 1);
+    }
+    intx4 wA[2][2], wB[2][2];
+    ring_barrier<12>();
+    read_w(I0{}, 0, wA);
+    ring_barrier<12>();
+    if (wm) plain_barrier();   // the second group of wavefronts runs half a phase behind the first
+    int kt = 0;
+    for (; kt + 1 < nk; kt += 2) {
+        k_tile(kt, 0, wA, wB);
+        k_tile(kt + 1, 1, wB, wA);
+    }
+    if (kt < nk) k_tile(kt, 0, wA, wB);
+    if (!wm) plain_barrier();
+    ring_barrier<0>();   // the repeated loads of the last k-tile must not land in the slabs
+    i8_store<GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), lane, wm * WTM, tp.n0 + wn * WOUT);
+}
+
+// The same schedule over 128 x 256 tiles (wavefronts of 64 x 64, two phases per k-tile: X0 W0, X0 W1).  A k-tile is three half tiles (W0,
+// X0, W1); the ring holds three k-tiles (nine slots, 144 KB).  A phase requests three of the six 8-row pieces that a wavefront owns of
+// a k-tile; 11 or 12 of them may still fly when the next phase's operands must be there.
+template <bool GLU, bool GROUPED, bool TAIL>
+__device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile& tp, char* smem) {
+    constexpr int WN = 4, BK = I8_BK, WTM = 64, WTN = 64, TM = WTM / 16, TN = WTN / 16, HT = 128 * BK;
+    constexpr int WOUT = GLU ? WTN / 2 : WTN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int r = lane & 15, c4 = lane >> 4;
+    const int8_t* src[3][2];   // half tiles q = 0: W0, 1: X0, 2: W1
+    int chunk[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int row = (wave * 2 + u) * 8 + (lane >> 3);
+        chunk[u] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+        int64_t sr = tp.m0 + min(row, tp.rows_valid - 1);
+        if (GROUPED && p.g.a_gather) sr = p.g.a_gather[sr];
+        src[1][u] = p.X + sr * p.K + chunk[u];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int n = GLU ? min(tp.n0 + row, p.N - 1) + j * p.N : min(tp.n0 + (row >> 5) * 64 + j * 32 + (row & 31), p.N - 1);
+            src[2 * j][u] = tp.W + (int64_t)n * p.K + chunk[u];
+        }
+    }
+    intx4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = intx4{0, 0, 0, 0};
+    const int nk = (p.K + BK - 1) / BK;
+    int foff[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) foff[kk] = r * BK + (((4 * kk + c4) ^ ((r >> 1) & 7)) << 4);
+    const char* xs = smem + wm * 64 * BK;
+    const char* ws = smem + wn * 32 * BK;
+    // piece u of half tile q of k-tile kt (past the end: the last one again), into k-tile buffer buf
+    auto gload = [&](auto qtag, int u, int kt, int buf) __attribute__((always_inline)) {
+        constexpr int q = decltype(qtag)::value;
+        i8_load_piece<TAIL, q == 1>(src[q][u], chunk[u], min(kt, nk - 1), nk, p.K, smem + (buf * 3 + q) * HT + (wave * 2 + u) * 8 * BK);
+    };
+    auto read_w = [&](int j, int buf, intx4 (&f)[2][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) f[nt][kk] = *reinterpret_cast<const intx4*>(ws + (buf * 3 + 2 * j) * HT + nt * 16 * BK + foff[kk]);
+    };
+    intx4 xf[4][2], w0[2][2], w1[2][2];
+    // k-tile kt in buffer b0, kt + 1 in b1, kt + 2 in b2
+    auto k_tile = [&](int kt, int b0, int b1, int b2) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) xf[mt][kk] = *reinterpret_cast<const intx4*>(xs + (b0 * 3 + 1) * HT + mt * 16 * BK + foff[kk]);
+        gload(I2{}, 0, kt + 2, b2);
+        gload(I2{}, 1, kt + 2, b2);
+        gload(I0{}, 0, kt + 3, b0);
+        ring_barrier<11>();
+        i8_mfmas<0, 0>(acc, xf, w0);
+        read_w(1, b0, w1);
+        read_w(0, b1, w0);
+        gload(I0{}, 1, kt + 3, b0);
+        gload(I1{}, 0, kt + 3, b0);
+        gload(I1{}, 1, kt + 3, b0);
+        ring_barrier<12>();
+        i8_mfmas<0, 1>(acc, xf, w1);
+    };
+    // k-tiles 0 and 1, and W0, X0 of k-tile 2; the first two half tiles have landed when all but 12 pieces have
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        gload(I0{}, 0, i, i);
+        gload(I0{}, 1, i, i);
+        gload(I1{}, 0, i, i);
+        gload(I1{}, 1, i, i);
+        if (i < 2) {
+            gload(I2{}, 0, i, i);
+            gload(I2{}, 1, i, i);
+        }
+    }
+    ring_barrier<12>();
+    read_w(0, 0, w0);
+    ring_barrier<12>();
+    if (wm) plain_barrier();   // the second group of wavefronts runs half a phase behind the first
+    int kt = 0;
+    for (; kt + 2 < nk; kt += 3) {
+        k_tile(kt, 0, 1, 2);
+        k_tile(kt + 1, 1, 2, 0);
+        k_tile(kt + 2, 2, 0, 1);
+    }
+    if (kt < nk) k_tile(kt, 0, 1, 2);
+    if (kt + 1 < nk) k_tile(kt + 1, 1, 2, 0);
+    if (!wm) plain_barrier();
+    ring_barrier<0>();   // the repeated loads must not land in the slabs
+    i8_store<GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), lane, wm * WTM, tp.n0 + wn * WOUT);
+}
+
+// Plain products: the output is cut into slots of 256 x 256, in groups of 4 row tiles per column tile; the first n_full of them are a
+// workgroup each, the others two workgroups of 128 x 256, and last come the halves of a bottom row tile of at most 128 rows.  Routed
+// products: a workgroup per tile of the map, in the form that its rows need.
+template <bool GLU, bool GROUPED, bool TAIL>
+__global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
+    constexpr int OUTN = GLU ? 128 : 256;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    if constexpr (GROUPED) {
+        const I8Tile tp = p.g.mtile == 256 ? i8_tile<true, GLU, 256, OUTN, 4>(p) : i8_tile<true, GLU, 128, OUTN, 8>(p);
+        if (tp.rows_valid <= 0) return;
+        if (tp.rows_valid > 128)
+            i8_tile_256<GLU, true, TAIL>(p, tp, smem);
+        else
+            i8_tile_128<GLU, true, TAIL>(p, tp, smem);
+    } else {
+        const int i = blockIdx.x;
+        int tm, tn;
+        I8Tile tp;
+        tp.W = p.W;
+        tp.ws = p.ws;
+        if (i < p.n_full) {
+            tile_at<4>(xcd_order(i, p.n_full), p.n_mtiles, p.n_ntiles, tm, tn);
+            tp.m0 = (int64_t)tm * 256;
+            tp.n0 = tn * OUTN;
+            tp.rows_valid = (int)min((int64_t)256, p.M - tp.m0);
+            i8_tile_256<GLU, false, TAIL>(p, tp, smem);
+        } else {
+            const int h = xcd_order(i - p.n_full, gridDim.x - p.n_full);
+            const int slot = p.n_full + h / 2, slots = p.n_mtiles * p.n_ntiles;
+            if (slot < slots) {
+                tile_at<4>(slot, p.n_mtiles, p.n_ntiles, tm, tn);
+                tp.m0 = (int64_t)tm * 256 + (h & 1) * 128;
+            } else {
+                tn = h - 2 * (slots - p.n_full);
+                tp.m0 = (int64_t)p.n_mtiles * 256;
+            }
+            tp.n0 = tn * OUTN;
+            tp.rows_valid = (int)min((int64_t)128, p.M - tp.m0);
+            i8_tile_128<GLU, false, TAIL>(p, tp, smem);
+        }
+    }
+}
+
+template <bool GLU, bool GROUPED, bool TAIL>
+static int launch_large_form(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
+    constexpr int OUTN = GLU ? 128 : 256;
+    constexpr size_t smem = (size_t)9 * 128 * I8_BK;   // the larger ring; the epilogue's slabs fit in
+    static_assert((size_t)8 * 16 * (OUTN / 4 + 4) * sizeof(float) <= smem, "the epilogue's slabs fit the ring");
+    static std::atomic<uint64_t> lds_set{0};
+    TRY(allow_lds(ctx, (const void*)gemm_i8_kernel<GLU, GROUPED, TAIL>, smem, lds_set));
+    p.n_ntiles = (p.N + OUTN - 1) / OUTN;
+    int64_t wgs;
+    if (GROUPED) {
+        wgs = (int64_t)p.n_mtiles * p.n_ntiles;
+    } else {
+        const LargeTiles lt = large_tiles(p.M, p.n_ntiles);
+        if (lt.slots > 0x3fffffff) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
+        p.n_mtiles = (int)(lt.slots / p.n_ntiles);
+        p.n_full = (int)std::min(n_full, lt.slots);
+        wgs = p.n_full + 2 * (lt.slots - p.n_full) + lt.bottom;
+    }
+    if (wgs == 0) return COMPACT_OK;
+    gemm_i8_kernel<GLU, GROUPED, TAIL><<<dim3((unsigned)wgs), 512, smem, s>>>(p);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
+}
+template <bool GLU, bool GROUPED>
+static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
+    return p.K % I8_BK ? launch_large_form<GLU, GROUPED, true>(ctx, p, n_full, s) : launch_large_form<GLU, GROUPED, false>(ctx, p, n_full, s);
+}
+
+template <bool GLU, bool GROUPED>
+static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params& p, hipStream_t s) {
+    switch (form) {
+        case TILE_256: return launch_large<GLU, GROUPED>(ctx, p, n_full, s);
+        case TILE_128: return launch_large<GLU, GROUPED>(ctx, p, 0, s);
+        case TILE_64_128: return launch_tile<64, 128, 2, 4, 6, GLU, GROUPED>(ctx, p, s);
+        default: break;
+    }
+    if constexpr (!GROUPED) {
+        switch (form) {
+            case TILE_128_128: return launch_tile<128, 128, 2, 4, 5, GLU, false>(ctx, p, s);
+            case TILE_128_64: return launch_tile<128, 64, 4, 2, 6, GLU, false>(ctx, p, s);
+            case TILE_64_64: return launch_tile<64, 64, 2, 2, 5, GLU, false>(ctx, p, s);
+            default: break;
+        }
+    }
+    return set_err(ctx, COMPACT_EINVAL, "unknown GEMM tile");
 }
 
 size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {
     (void)M, (void)N, (void)K, (void)epilogue;
     return 0;
 }
-int gemm_i8_group_mtile(int64_t rows, int n_experts) {
-    (void)rows, (void)n_experts;
-    return 64;
-}
+int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) { return gemm_bf16_group_mtile(rows, n_experts, F, d / 2, n_cus); }
 
-int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_bytes, hipStream_t s) {
-    (void)ws, (void)ws_bytes;
-    if (a.M == 0) return COMPACT_OK;
+static GemmI8Params i8_params(compact_ctx* ctx, const GemmI8Args& a) {
     GemmI8Params p{};
     p.X = a.a;
     p.xs = a.a_scale;
@@ -285,10 +687,40 @@ int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_by
     p.N = a.N;
     p.K = a.K;
     p.f32 = ctx->cfg.dtype == COMPACT_FP32;
+    return p;
+}
+
+int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_bytes, hipStream_t s) {
+    (void)ws, (void)ws_bytes;
+    if (a.M == 0) return COMPACT_OK;
+    GemmI8Params p = i8_params(ctx, a);
+    int n_cus = 0;
+    TRY(device_cu_count(ctx, &n_cus));
     if (a.grouped) {
         p.g = *a.grouped;
         p.n_mtiles = a.grouped->n_mtiles;
-        return a.epilogue ? launch_tile<64, 64, 2, 2, 4, true, true>(ctx, p, s) : launch_tile<64, 64, 2, 2, 4, false, true>(ctx, p, s);
+        const int form = p.g.mtile == 256 ? TILE_256 : p.g.mtile == 128 ? TILE_128 : TILE_64_128;
+        return a.epilogue ? launch_form<true, true>(ctx, form, 0, p, s) : launch_form<false, true>(ctx, form, 0, p, s);
     }
-    return a.epilogue ? launch_tile<64, 64, 2, 2, 4, true, false>(ctx, p, s) : launch_tile<64, 64, 2, 2, 4, false, false>(ctx, p, s);
+    int64_t n_full = 0;
+    const int form = pick_tile(a.M, a.N, (a.K + 127) / 128 * 64, a.epilogue, n_cus, &n_full);
+    return a.epilogue ? launch_form<true, false>(ctx, form, n_full, p, s) : launch_form<false, false>(ctx, form, n_full, p, s);
+}
+
+// For the tests, not part of compact.h: the product in tile form `form` (TILE_FORMS: whole tiles and halves mixed, as many slots
+// in either).
+extern "C" int compact_test_gemm_i8_form(compact_ctx* ctx, int32_t form, const void* a, const float* a_scale, const void* b,
+                                         const float* b_scale, const void* r, void* c, int64_t M, int32_t N, int32_t K, int32_t epilogue,
+                                         void* hip_stream) {
+    if (!ctx || !a || !a_scale || !b || !b_scale || !c || M < 1 || N < 1 || K < 16 || K % 16 || form < 0 || form > TILE_FORMS || (epilogue != 0 && epilogue != 1))
+        return COMPACT_EINVAL;
+    const GemmI8Args g{(const int8_t*)a, a_scale, (const int8_t*)b, b_scale, r, c, M, N, K, epilogue, nullptr};
+    GemmI8Params p = i8_params(ctx, g);
+    int64_t n_full = large_tiles(M, (N + (epilogue ? 127 : 255)) / (epilogue ? 128 : 256)).slots;
+    if (form == TILE_FORMS) {
+        form = TILE_256;
+        n_full /= 2;
+    }
+    hipStream_t s = (hipStream_t)hip_stream;
+    return epilogue ? launch_form<true, false>(ctx, form, n_full, p, s) : launch_form<false, false>(ctx, form, n_full, p, s);
 }

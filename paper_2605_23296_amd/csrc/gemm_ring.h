@@ -1,5 +1,7 @@
 // What the GEMM kernels with a ring of LDS stages share: barriers that do not drain the loads in flight, and the order of tiles.
 #pragma once
+#include <algorithm>
+
 #include "common.h"
 
 // Waits until at most N_IN_FLIGHT of this wave's global loads are outstanding (the older ones have landed in
@@ -48,3 +50,18 @@ __device__ __forceinline__ void tile_at(int pid, int n_mtiles, int n_ntiles, int
     tm = first_m + (pid % per_group) % gsize;
     tn = (pid % per_group) / gsize;
 }
+
+// How the 256 x 256 kernel cuts M rows: slots of 256 x 256 (a last row tile of more than 128 rows is one), and 128 x 256
+// tiles of a bottom row tile of at most 128 rows.
+struct LargeTiles {
+    int64_t slots;
+    int64_t bottom;
+};
+static inline LargeTiles large_tiles(int64_t M, int n_ntiles) {
+    const int64_t rest = M % 256;
+    return {(M / 256 + (rest > 128 ? 1 : 0)) * n_ntiles, rest > 0 && rest <= 128 ? n_ntiles : 0};
+}
+
+// The tile forms, by time: which one for C[M, N] over K elements of 2 bytes (gemm_bf16.hip); n_full: slots that TILE_256 takes as whole tiles.
+enum { TILE_256 = 0, TILE_128, TILE_128_128, TILE_128_64, TILE_64_128, TILE_64_64, TILE_FORMS };
+int pick_tile(int64_t M, int N, int K, int epilogue, int n_cus, int64_t* n_full);

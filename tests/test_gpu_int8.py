@@ -1,6 +1,7 @@
 """8-bit integer weights: codes, products, norms around a block, routing and the experts' products, against the definition in 64 bits.
 
 Tolerances count roundings: u = 2^-24 is half a step of fp32, 2^-8 that of bf16.  Codes are whole numbers and have to be equal."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -132,6 +133,31 @@ def test_products(dtype, epilogue, res, M, N, K):
     c = product(lay, a, sa, b, sb, r, epilogue)
     check_product(c, a, sa, b, sb, r, epilogue, dtype)
     assert torch.equal(product(lay, a, sa, b, sb, r, epilogue, ws=False), c)     # a workspace changes no bit
+
+
+def in_form(lay, form, a, sa, b, sb, r, epilogue):
+    """The product in one of the tile forms (6: 256 x 256 tiles and their halves, mixed)."""
+    M, K, N = a.shape[0], a.shape[1], b.shape[0] // (2 if epilogue else 1)
+    c = torch.full((M + 1, N), 7.0, dtype=lay.torch_dtype, device="cuda")
+    ptr = lambda t: None if t is None else C.c_void_p(t.data_ptr())   # noqa: E731
+    lay.check(lay.L.compact_test_gemm_i8_form(lay.ctx, C.c_int32(form), ptr(a), ptr(sa), ptr(b), ptr(sb), ptr(r), ptr(c), C.c_int64(M), C.c_int32(N), C.c_int32(K),
+                                              C.c_int32(epilogue), C.c_void_p(torch.cuda.current_stream().cuda_stream)))
+    assert bool((c[M] == 7.0).all())
+    return c[:M]
+
+
+# one to seven k-tiles of 128, whole and cut; rows and columns just under, at and over the tile edges
+@pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 368, 512, 640, 784, 896])
+@pytest.mark.parametrize("epilogue,res", [(0, True), (0, False), (1, False)])
+def test_every_tile_form_at_its_edges(K, epilogue, res):
+    lay = layer()
+    for M, N in [(1, 8), (63, 136), (65, 57), (128, 64), (129, 264), (257, 520), (300, 128), (511, 1000), (700, 259)]:
+        a, b, sa, sb = codes(M, K, 1), codes((1 + epilogue) * N, K, 2), scales(M, 3), scales((1 + epilogue) * N, 4) / math.sqrt(K) / 5000
+        r = rows_of(M, N, "bf16", 5) if res else None
+        want = in_form(lay, 5, a, sa, b, sb, r, epilogue)
+        check_product(want, a, sa, b, sb, r, epilogue, "bf16")
+        for form in (0, 1, 2, 3, 4, 6):
+            assert torch.equal(in_form(lay, form, a, sa, b, sb, r, epilogue), want), (M, N, form)
 
 
 @pytest.mark.parametrize("M", [1, 16, 40, 200, 700])
