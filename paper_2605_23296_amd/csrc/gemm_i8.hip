@@ -1,36 +1,12 @@
 // Products of 8-bit codes:  C[m, n] = a_scale[m] b_scale[n] sum_k A[m, k] B[n, k], the sum in 32-bit integers.  Integer sums are the
 // same in any order, so every tile form and every split of K gives the same bits.
 #include <algorithm>
-#include <atomic>
 #include <type_traits>
 
 #include "common.h"
+#include "gemm_i8.h"
 #include "gemm_ring.h"
 #include "vecio.h"
-
-typedef int intx4 __attribute__((ext_vector_type(4)));
-
-#define I8_BK 128   // k-tile: a row of it is one 128-byte line
-
-struct GemmI8Params {
-    const int8_t* X;
-    const float* xs;
-    const int8_t* W;
-    const float* ws;
-    const void* R;
-    void* C;
-    int64_t M;
-    int N;    // output columns (F for SwiGLU, whose W has 2N rows)
-    int K;
-    int n_mtiles, n_ntiles;
-    int n_full;  // 256 x 256 kernel, plain product: workgroups that take a whole tile (the others take halves)
-    int* sums;   // of k-slices
-    int f32;  // C and R are fp32 rather than bf16
-    GroupedArgs g;
-};
-
-// what chunks of 16 codes beyond K are read from, on the activations' side
-static __device__ const int8_t zero_codes[16] __attribute__((aligned(16))) = {};
 
 struct I8Tile {
     int64_t m0;
@@ -58,32 +34,6 @@ __device__ __forceinline__ I8Tile i8_tile(const GemmI8Params& p) {
         t.rows_valid = (int)min((int64_t)BM, p.M - t.m0);
     }
     return t;
-}
-
-// the kernel may use that much LDS, on every device that it runs on (a set bit is a device that knows)
-static int allow_lds(compact_ctx* ctx, const void* kernel, size_t bytes, std::atomic<uint64_t>& known) {
-    int dev = 0;
-    HIP_TRY(ctx, hipGetDevice(&dev));
-    const uint64_t bit = 1ull << (dev & 63);
-    if (known.load(std::memory_order_relaxed) & bit) return COMPACT_OK;
-    HIP_TRY(ctx, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    known.fetch_or(bit, std::memory_order_relaxed);
-    return COMPACT_OK;
-}
-
-// One output from its sums; the same roundings wherever it is computed.
-#pragma clang fp contract(off)
-__device__ __forceinline__ float i8_value(int sum, float xs, float ws) { return (float)sum * xs * ws; }
-__device__ __forceinline__ float i8_glu(float g, float u, bool f32) {
-    const float e = f32 ? expf(-g) : __expf(-g);   // (__expf: off by up to 3.4e-6 of the value at g = -80)
-    return g / (1.0f + e) * u;
-}
-
-__device__ __forceinline__ void i8_put(const GemmI8Params& p, int64_t o, float v) {
-    if (p.f32)
-        ((float*)p.C)[o] = v + (p.R ? ((const float*)p.R)[o] : 0.f);
-    else
-        ((bf16*)p.C)[o] = (bf16)(v + (p.R ? (float)((const bf16*)p.R)[o] : 0.f));
 }
 
 // Epilogue of one wavefront: TM x TN MFMA tiles, 16 output rows per pass through a slab of its own [16][WOUT + 4].  acc[i][j][e]: output
@@ -673,7 +623,10 @@ size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {
     (void)M, (void)N, (void)K, (void)epilogue;
     return 0;
 }
-int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) { return gemm_bf16_group_mtile(rows, n_experts, F, d / 2, n_cus); }
+int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) {
+    if (rows <= 2 * n_experts) return I8_STREAM_ROWS;
+    return gemm_bf16_group_mtile(rows, n_experts, F, d / 2, n_cus);
+}
 
 static GemmI8Params i8_params(compact_ctx* ctx, const GemmI8Args& a) {
     GemmI8Params p{};
@@ -700,8 +653,10 @@ int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_by
         p.g = *a.grouped;
         p.n_mtiles = a.grouped->n_mtiles;
         const int form = p.g.mtile == 256 ? TILE_256 : p.g.mtile == 128 ? TILE_128 : TILE_64_128;
+        if (p.g.mtile == I8_STREAM_ROWS) return launch_stream_i8(ctx, p, a.epilogue != 0, s);
         return a.epilogue ? launch_form<true, true>(ctx, form, 0, p, s) : launch_form<false, true>(ctx, form, 0, p, s);
     }
+    if (a.M <= I8_STREAM_ROWS) return launch_stream_i8(ctx, p, a.epilogue != 0, s);
     int64_t n_full = 0;
     const int form = pick_tile(a.M, a.N, (a.K + 127) / 128 * 64, a.epilogue, n_cus, &n_full);
     return a.epilogue ? launch_form<true, false>(ctx, form, n_full, p, s) : launch_form<false, false>(ctx, form, n_full, p, s);
