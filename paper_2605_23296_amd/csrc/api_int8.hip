@@ -148,9 +148,10 @@ extern "C" int compact_moe_ffn_i8_workspace_bytes(const compact_ctx* ctx, int64_
     return COMPACT_OK;
 }
 
-extern "C" int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const void* d_m, const float* d_m_scale,
-                                  const void* d_h, const int32_t* d_expert_idx, const float* d_weight, int64_t rows, void* d_y,
-                                  void* d_workspace, size_t ws_bytes, void* hip_stream) {
+// mtile: rows per tile of the experts' map (0: by the rule)
+static int moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const void* d_m, const float* d_m_scale, const void* d_h,
+                      const int32_t* d_expert_idx, const float* d_weight, int64_t rows, void* d_y, void* d_workspace, size_t ws_bytes,
+                      void* hip_stream, int mtile) {
     if (!ctx) return COMPACT_EINVAL;
     TRY(check_moe_i8(ctx, rows));
     if (!experts || !experts->d_gate_up || !experts->d_gate_up_scale || !experts->d_down || !experts->d_down_scale)
@@ -169,7 +170,7 @@ extern "C" int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* ex
     const int64_t rk = rows * c.top_k;
     int n_cus = 0;
     TRY(device_cu_count(ctx, &n_cus));
-    const int mtile = gemm_i8_group_mtile(rk, c.n_experts, c.ffn_dim, c.d_model, n_cus);
+    if (mtile == 0) mtile = gemm_i8_group_mtile(rk, c.n_experts, c.ffn_dim, c.d_model, n_cus);
     TRY(launch_moe_plan(ctx, d_expert_idx, d_weight, rows, mtile, b.plan, s));
     GroupedArgs g{};
     g.mtile = mtile;
@@ -188,4 +189,18 @@ extern "C" int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* ex
     a = GemmI8Args{b.act_q, b.act_scale, (const int8_t*)experts->d_down, experts->d_down_scale, nullptr, b.out, rk, c.d_model, c.ffn_dim, 0, &g};
     TRY(launch_gemm_i8(ctx, a, nullptr, 0, s));
     return launch_moe_combine(ctx, b.out, d_h, false, b.plan.slot_of, rows, d_y, s);
+}
+
+extern "C" int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const void* d_m, const float* d_m_scale,
+                                  const void* d_h, const int32_t* d_expert_idx, const float* d_weight, int64_t rows, void* d_y,
+                                  void* d_workspace, size_t ws_bytes, void* hip_stream) {
+    return moe_ffn_i8(ctx, experts, d_m, d_m_scale, d_h, d_expert_idx, d_weight, rows, d_y, d_workspace, ws_bytes, hip_stream, 0);
+}
+
+// For the tests, not part of compact.h: the same with row tiles of a given height.
+extern "C" int compact_test_moe_ffn_i8(compact_ctx* ctx, int32_t mtile, const compact_experts_i8* experts, const void* d_m,
+                                       const float* d_m_scale, const void* d_h, const int32_t* d_expert_idx, const float* d_weight,
+                                       int64_t rows, void* d_y, void* d_workspace, size_t ws_bytes, void* hip_stream) {
+    if (mtile != 16 && mtile != 64 && mtile != 128 && mtile != 256) return COMPACT_EINVAL;
+    return moe_ffn_i8(ctx, experts, d_m, d_m_scale, d_h, d_expert_idx, d_weight, rows, d_y, d_workspace, ws_bytes, hip_stream, mtile);
 }

@@ -624,7 +624,7 @@ size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {
     return 0;
 }
 int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) {
-    if (rows <= 2 * n_experts) return I8_STREAM_ROWS;
+    if (rows <= 12 * n_experts) return I8_STREAM_ROWS;
     return gemm_bf16_group_mtile(rows, n_experts, F, d / 2, n_cus);
 }
 

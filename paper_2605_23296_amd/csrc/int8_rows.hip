@@ -22,26 +22,139 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// A workgroup per row: the largest value, then the codes.
+// 8 elements as they lie in memory
 template <typename T>
-__global__ __launch_bounds__(NT) void quant_i8_kernel(const T* __restrict__ x, int64_t x_stride, int cols, int8_t* __restrict__ q,
-                                                      float* __restrict__ scale) {
-    __shared__ uint32_t red[NT / 64];
+struct Piece;
+template <>
+struct Piece<bf16> {
+    bf16x8 v;
+    __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const bf16x8*>(p); }
+    __device__ __forceinline__ void zero() { v = bf16x8{}; }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (float)v[j];
+    }
+};
+template <>
+struct Piece<float> {
+    floatx4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = *reinterpret_cast<const floatx4*>(p);
+        b = *reinterpret_cast<const floatx4*>(p + 4);
+    }
+    __device__ __forceinline__ void zero() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[j] = a[j];
+            f[4 + j] = b[j];
+        }
+    }
+};
+
+// TPR threads per row (64: a wavefront, four rows a workgroup; else a workgroup), a thread holds the pieces thread + TPR i: the row is read once.
+template <typename T, int TPR, int P>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_i8_kernel(const T* __restrict__ x, int64_t x_stride, int64_t rows, int cols,
+                                                                         int8_t* __restrict__ q, float* __restrict__ scale) {
+    constexpr int RPW = TPR < 256 ? 256 / TPR : 1;
+    __shared__ uint32_t red[TPR / 64];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR;
+    if (row >= rows) return;   // (a whole wavefront; only where rows need no barrier)
+    const T* xr = x + row * x_stride;
+    Piece<T> v[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int c = (t + i * TPR) * 8;
+        if (c < cols)
+            v[i].load(xr + c);
+        else
+            v[i].zero();
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float f[8];
+        v[i].get(f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(f[j]));
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if (TPR > 64) {
+        if ((t & 63) == 0) red[t / 64] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < TPR / 64; ++w) m = max(m, red[w]);
+    }
+    const RowCodes rc = row_codes(m);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int c = (t + i * TPR) * 8;
+        float f[8];
+        v[i].get(f);
+        if (c < cols) *reinterpret_cast<uint2*>(q + row * cols + c) = codes8<T>(f, rc);
+    }
+    if (t == 0) scale[row] = rc.scale;
+}
+
+// Rows that are too long for that, or whose pieces of 8 are not aligned: the largest value, then the codes, an element at a time.
+template <typename T>
+__global__ __launch_bounds__(1024) void quant_i8_any_kernel(const T* __restrict__ x, int64_t x_stride, int cols, int8_t* __restrict__ q,
+                                                            float* __restrict__ scale) {
+    __shared__ uint32_t red[16];
     const int64_t row = blockIdx.x;
     const T* xr = x + row * x_stride;
     uint32_t m = 0;
-    for (int c = threadIdx.x; c < cols; c += NT) m = max(m, abs_bits(to_f32(xr[c])));
-    const RowCodes rc = row_codes(block_max(m, red));
-    for (int c = threadIdx.x; c < cols; c += NT) q[row * cols + c] = (int8_t)code_of<T>(to_f32(xr[c]), rc);
+    for (int c = threadIdx.x; c < cols; c += 1024) m = max(m, abs_bits(to_f32(xr[c])));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) m = max(m, red[w]);
+    const RowCodes rc = row_codes(m);
+    for (int c = threadIdx.x; c < cols; c += 1024) q[row * cols + c] = (int8_t)code_of<T>(to_f32(xr[c]), rc);
     if (threadIdx.x == 0) scale[row] = rc.scale;
+}
+
+template <typename T, int TPR, int P>
+static void run_quant(const T* x, int64_t x_stride, int64_t rows, int cols, int8_t* q, float* scale, hipStream_t s) {
+    constexpr int RPW = TPR < 256 ? 256 / TPR : 1;
+    quant_i8_kernel<T, TPR, P><<<(unsigned)((rows + RPW - 1) / RPW), TPR < 256 ? 256 : TPR, 0, s>>>(x, x_stride, rows, cols, q, scale);
+}
+template <typename T>
+static void quant_rows(const T* x, int64_t x_stride, int64_t rows, int cols, int8_t* q, float* scale, hipStream_t s) {
+    const bool wide = cols % 8 == 0 && x_stride % 8 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)q & 7) == 0;
+    const int pieces = cols / 8;
+    if (!wide || pieces > 8192)
+        quant_i8_any_kernel<T><<<(unsigned)rows, 1024, 0, s>>>(x, x_stride, cols, q, scale);
+    else if (pieces <= 64)
+        run_quant<T, 64, 1>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 128)
+        run_quant<T, 64, 2>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 256)
+        run_quant<T, 64, 4>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 384 && rows >= 1024)
+        run_quant<T, 64, 6>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 512)
+        run_quant<T, 256, 2>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 1024)
+        run_quant<T, 256, 4>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 2048)
+        run_quant<T, 512, 4>(x, x_stride, rows, cols, q, scale, s);
+    else if (pieces <= 4096)
+        run_quant<T, 1024, 4>(x, x_stride, rows, cols, q, scale, s);
+    else
+        run_quant<T, 1024, 8>(x, x_stride, rows, cols, q, scale, s);
 }
 
 int launch_quant_i8(compact_ctx* ctx, const void* x, int64_t x_stride, int64_t rows, int cols, int8_t* q, float* scale, hipStream_t s) {
     if (rows == 0) return COMPACT_OK;
     if (ctx->cfg.dtype == COMPACT_BF16)
-        quant_i8_kernel<bf16><<<(unsigned)rows, NT, 0, s>>>((const bf16*)x, x_stride, cols, q, scale);
+        quant_rows((const bf16*)x, x_stride, rows, cols, q, scale, s);
     else
-        quant_i8_kernel<float><<<(unsigned)rows, NT, 0, s>>>((const float*)x, x_stride, cols, q, scale);
+        quant_rows((const float*)x, x_stride, rows, cols, q, scale, s);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }

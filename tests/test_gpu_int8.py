@@ -54,7 +54,9 @@ def quantised(lay, x, room=0):
 
 
 @pytest.mark.parametrize("dtype", DT)
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (3, 8), (2, 64), (5, 200), (4, 1000), (33, 4096), (3, 4104), (2, 14336), (2, 28672), (1, 70001), (700, 72), (0, 64)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (3, 8), (2, 64), (5, 200), (4, 1000), (33, 4096), (3, 4104), (2, 14336), (2, 28672), (1, 70001), (700, 72), (0, 64), (4, 512), (3, 520),
+                                       (5, 1024), (2, 1032), (3, 2048), (1030, 2056), (2, 2880), (1025, 2880), (2, 3080), (3, 8192), (2, 8200), (2, 16392), (1, 32776), (1, 65536),
+                                       (1, 65544)])
 def test_codes_of_rows(dtype, rows, cols):
     x = rows_of(rows, cols, dtype, 3)
     if rows:
@@ -413,6 +415,26 @@ def test_experts(E, k, d, F, rows):
         # 1 / 127 of the largest
         err = np.linalg.norm(f64(y) - ref, axis=-1) / np.linalg.norm(ref, axis=-1)
         assert err.max() < 2 * 2.0 ** -8 + 2.0 ** -9, err.max()
+
+
+def ffn_in_tiles(lay, mtile, ex, m, ms, h, idx, w):
+    lay.ws = torch.empty(lay.moe_ffn_i8_workspace_bytes(m.shape[0]), dtype=torch.uint8, device="cuda")
+    y, p = torch.empty_like(h), lambda t: C.c_void_p(t.data_ptr())
+    e = B.ExpertsI8Struct(*(t.data_ptr() for t in (ex.gate_up, ex.gate_up_scale, ex.down, ex.down_scale)))
+    lay.check(lay.L.compact_test_moe_ffn_i8(lay.ctx, C.c_int32(mtile), C.byref(e), p(m), p(ms), p(h), p(idx), p(w), C.c_int64(m.shape[0]), p(y), p(lay.ws),
+                                            C.c_size_t(lay.ws.numel()), C.c_void_p(torch.cuda.current_stream().cuda_stream)))
+    return y
+
+
+@pytest.mark.parametrize("E,k,d,F", [(8, 2, 64, 64), (16, 4, 320, 192), (8, 3, 448, 640)])
+@pytest.mark.parametrize("rows", [5, 40, 257, 900])
+def test_experts_have_the_same_bits_at_every_row_tile_height(E, k, d, F, rows):
+    lay, ex = layer(d=d, F=F, E=E, k=k), experts(E, d, F, 11)
+    m, ms, h = codes(rows, d, 1), scales(rows, 2) / 70, rows_of(rows, d, "bf16", 3)
+    idx, w = routed(rows, E, k, 5, 1.0)
+    want = ffn(lay, ex, m, ms, h, idx, w)
+    for mtile in (16, 64, 128, 256):
+        assert torch.equal(ffn_in_tiles(lay, mtile, ex, m, ms, h, idx, w), want), mtile
 
 
 @pytest.mark.parametrize("rows", [3, 16, 200])
