@@ -47,8 +47,10 @@ static inline int allow_lds(compact_ctx* ctx, const void* kernel, size_t bytes, 
 #pragma clang fp contract(off)
 __device__ __forceinline__ float i8_value(int sum, float xs, float ws) { return (float)sum * xs * ws; }
 __device__ __forceinline__ float i8_glu(float g, float u, bool f32) {
-    const float e = f32 ? expf(-g) : __expf(-g);   // (__expf: off by up to 3.4e-6 of the value at g = -80)
-    return g / (1.0f + e) * u;
+    if (f32) return g / (1.0f + expf(-g)) * u;
+    // what a bf16 result does not see: exp2(-g log2 e), off by up to 3.4e-6 of the value at g = -80, and the reciprocal to one unit in the last
+    // place (a division to half a unit is ten instructions, 64 times a lane, while the matrix pipe waits)
+    return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
 }
 
 __device__ __forceinline__ void i8_put(const GemmI8Params& p, int64_t o, float v) {

@@ -36,29 +36,49 @@ __device__ __forceinline__ I8Tile i8_tile(const GemmI8Params& p) {
     return t;
 }
 
+// The scales of a workgroup's rows and columns (and the factors of the rows) on their way to LDS, at the start: [BM] rows, [BN] weight rows of
+// the tile, [BM] factors.  They are older than the ring's loads and so have landed by its first barrier; read at the end, each
+// would be two trips to memory, one after the other, for every 16 rows.
+template <int BM, int BN, bool GLU, bool GROUPED>
+__device__ __forceinline__ void i8_load_scales(const GemmI8Params& p, const I8Tile& tp, char* sc, int wave, int lane) {
+    constexpr int UX = BM / 64, UW = BN / 64;
+    auto unit = [&](int u) __attribute__((always_inline)) {
+        char* dst = sc + u * 256;
+        if (u < UX || u >= UX + UW) {
+            const int64_t row = tp.m0 + min((u < UX ? u : u - UX - UW) * 64 + lane, tp.rows_valid - 1);
+            if (u < UX)
+                load4_to_lds(p.xs + (GROUPED && p.g.a_gather ? (int64_t)p.g.a_gather[row] : row), dst);
+            else
+                load4_to_lds(p.g.row_scale + row, dst);
+        } else {
+            const int c = (u - UX) * 64 + lane;
+            const int n = !GLU ? min(tp.n0 + c, p.N - 1) : c < BN / 2 ? min(tp.n0 + c, p.N - 1) : p.N + min(tp.n0 + c - BN / 2, p.N - 1);
+            load4_to_lds(tp.ws + n, dst);
+        }
+    };
+    const int units = UX + UW + (GROUPED && p.g.row_scale ? UX : 0);
+    for (int u = wave; u < units; u += blockDim.x / 64) unit(u);
+}
+
 // Epilogue of one wavefront: TM x TN MFMA tiles, 16 output rows per pass through a slab of its own [16][WOUT + 4].  acc[i][j][e]: output
-// row wrow + i*16 + r of the tile, column n_first + j*16 + c4*4 + e (SwiGLU: the first TN / 2 tiles are the gate, the others
-// the up values of the same columns).
-template <bool GLU, bool GROUPED, int TM, int TN>
-__device__ __forceinline__ void i8_store(const GemmI8Params& p, const I8Tile& tp, const intx4 (&acc)[TM][TN], float* slab, int lane,
-                                         int wrow, int n_first) {
+// row wrow + i*16 + r of the tile, column wcol + j*16 + c4*4 + e of it (SwiGLU: the first TN / 2 tiles are the gate, the others
+// the up values of the same columns).  sc: the scales in LDS.
+template <int BM, int BN, bool GLU, bool GROUPED, int TM, int TN>
+__device__ __forceinline__ void i8_store(const GemmI8Params& p, const I8Tile& tp, const intx4 (&acc)[TM][TN], float* slab, const float* sc,
+                                         int lane, int wrow, int wcol) {
     constexpr int TJ = GLU ? TN / 2 : TN, WOUT = TJ * 16, SLD = WOUT + 4;
     constexpr int NCH = WOUT / 8, NU = 16 * NCH / 64 > 0 ? 16 * NCH / 64 : 1;
-    const int r = lane & 15, c4 = lane >> 4;
-    float ws[TN][4];
+    const int r = lane & 15, c4 = lane >> 4, n_first = tp.n0 + wcol;
+    const float* gates = sc + BM + BN;
+    floatx4 ws[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int n = min(n_first + (j % TJ) * 16 + c4 * 4 + e, p.N - 1);
-            ws[j][e] = tp.ws[j < TJ ? n : p.N + n];
-        }
+        ws[j] = *reinterpret_cast<const floatx4*>(sc + BM + (j < TJ ? 0 : BN / 2) + wcol + (j % TJ) * 16 + c4 * 4);
     const bool wide = p.N % 8 == 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         if (wrow + i * 16 >= tp.rows_valid) break;   // (uniform in the wavefront)
-        const int64_t xr = tp.m0 + min(wrow + i * 16 + r, tp.rows_valid - 1);
-        const float xs = p.xs[GROUPED && p.g.a_gather ? (int64_t)p.g.a_gather[xr] : xr];
+        const float xs = sc[wrow + i * 16 + r];
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
             floatx4 v;
@@ -85,28 +105,24 @@ __device__ __forceinline__ void i8_store(const GemmI8Params& p, const I8Tile& tp
                 v[4 + e] = b[e];
             }
             if (GROUPED && p.g.row_scale) {
-                const float sc = p.g.row_scale[tp.m0 + lm];
+                const float f = gates[lm];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= sc;
+                for (int e = 0; e < 8; ++e) v[e] *= f;
             }
             if (wide) {
-                if (p.f32) {
-                    if (p.R) {
-                        float rv[8];
+                float rv[8];
+                if (p.R) {
+                    if (p.f32)
                         load8((const float*)p.R + o, rv);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += rv[e];
-                    }
-                    store8((float*)p.C + o, v);
-                } else {
-                    if (p.R) {
-                        float rv[8];
+                    else
                         load8((const bf16*)p.R + o, rv);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += rv[e];
-                    }
-                    store8((bf16*)p.C + o, v);
+                    for (int e = 0; e < 8; ++e) v[e] += rv[e];
                 }
+                if (p.f32)
+                    store8((float*)p.C + o, v);
+                else
+                    store8((bf16*)p.C + o, v);
             } else {
                 for (int e = 0; e < 8 && n + e < p.N; ++e) i8_put(p, o + e, v[e]);
             }
@@ -157,6 +173,8 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_tile_kernel(const GemmI8P
     const I8Tile tp = i8_tile<GROUPED, GLU, BM, OUTN, 8>(p);
     if (tp.rows_valid <= 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* const sc = smem + S * STAGE;
+    i8_load_scales<BM, BN, GLU, GROUPED>(p, tp, sc, wave, lane);
     const int wm = wave / WN, wn = wave % WN;
     const int r = lane & 15, c4 = lane >> 4;
 
@@ -241,7 +259,8 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_tile_kernel(const GemmI8P
         return;
     }
     ring_barrier<0>();   // the repeated loads must not land in the slabs
-    i8_store<GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), lane, wm * WTM, tp.n0 + wn * WOUT);
+    i8_store<BM, BN, GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), reinterpret_cast<const float*>(sc), lane,
+                                           wm * WTM, wn * WOUT);
 }
 
 // Sums of k-slices -> outputs, 4 columns a thread.
@@ -276,7 +295,7 @@ static int launch_tile(compact_ctx* ctx, GemmI8Params& p, hipStream_t s, int sli
     constexpr int OUTN = GLU ? BN / 2 : BN;
     if (!GROUPED) p.n_mtiles = (int)((p.M + BM - 1) / BM);
     p.n_ntiles = (p.N + OUTN - 1) / OUTN;
-    constexpr size_t smem = (size_t)S * (BM + BN) * I8_BK;
+    constexpr size_t smem = (size_t)S * (BM + BN) * I8_BK + (2 * BM + BN) * 4;
     static std::atomic<uint64_t> lds_set{0};
     TRY(allow_lds(ctx, (const void*)gemm_i8_tile_kernel<BM, BN, WM, WN, S, GLU, GROUPED>, smem, lds_set));
     const int64_t tiles = (int64_t)p.n_mtiles * p.n_ntiles;
@@ -298,6 +317,7 @@ static int launch_tile(compact_ctx* ctx, GemmI8Params& p, hipStream_t s, int sli
 // barrier, run 16 MFMAs, join a barrier.  The two wavefronts of a SIMD belong to groups that run half a phase apart, so that
 // one's MFMAs cover the other's reads and requests; barriers wait for LDS reads and for all but the newest 12 loads.
 // ---------------------------------------------------------------------------
+#define LARGE_RING (9 * 128 * I8_BK)   // bytes: the ring of either kind of tile, the scales behind it
 typedef std::integral_constant<int, 0> I0;
 typedef std::integral_constant<int, 1> I1;
 typedef std::integral_constant<int, 2> I2;
@@ -333,6 +353,8 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int r = lane & 15, c4 = lane >> 4;
+    char* const sc = smem + LARGE_RING;
+    i8_load_scales<256, 256, GLU, GROUPED>(p, tp, sc, wave, lane);
 
     // Half tiles q = 0: W0, 1: X0, 2: W1, 3: X1 (the order they are read in).  Half i of X holds tile rows wm * 128 + i * 64 + .., half j of W
     // the columns wn * 64 + j * 32 + .. of every wavefront (SwiGLU: half 0 the gate rows, half 1 the up rows of the same columns).  One
@@ -430,7 +452,8 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
     if (kt < nk) k_tile(kt, 0, wA, wB);
     if (!wm) plain_barrier();
     ring_barrier<0>();   // the repeated loads of the last k-tile must not land in the slabs
-    i8_store<GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), lane, wm * WTM, tp.n0 + wn * WOUT);
+    i8_store<256, 256, GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), reinterpret_cast<const float*>(sc), lane,
+                                             wm * WTM, wn * WOUT);
 }
 
 // The same schedule over 128 x 256 tiles (wavefronts of 64 x 64, two phases per k-tile: X0 W0, X0 W1).  A k-tile is three half tiles (W0,
@@ -443,6 +466,8 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int r = lane & 15, c4 = lane >> 4;
+    char* const sc = smem + LARGE_RING;
+    i8_load_scales<128, 256, GLU, GROUPED>(p, tp, sc, wave, lane);
     const int8_t* src[3][2];   // half tiles q = 0: W0, 1: X0, 2: W1
     int chunk[2];
 #pragma unroll
@@ -526,7 +551,8 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
     if (kt + 1 < nk) k_tile(kt + 1, 1, 2, 0);
     if (!wm) plain_barrier();
     ring_barrier<0>();   // the repeated loads must not land in the slabs
-    i8_store<GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), lane, wm * WTM, tp.n0 + wn * WOUT);
+    i8_store<128, 256, GLU, GROUPED, TM, TN>(p, tp, acc, reinterpret_cast<float*>(smem) + wave * 16 * (WOUT + 4), reinterpret_cast<const float*>(sc), lane,
+                                             wm * WTM, wn * WOUT);
 }
 
 // Plain products: the output is cut into slots of 256 x 256, in groups of 4 row tiles per column tile; the first n_full of them are a
@@ -575,7 +601,7 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
 template <bool GLU, bool GROUPED, bool TAIL>
 static int launch_large_form(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
     constexpr int OUTN = GLU ? 128 : 256;
-    constexpr size_t smem = (size_t)9 * 128 * I8_BK;   // the larger ring; the epilogue's slabs fit in
+    constexpr size_t smem = LARGE_RING + 3 * 256 * 4;   // the epilogue's slabs fit in
     static_assert((size_t)8 * 16 * (OUTN / 4 + 4) * sizeof(float) <= smem, "the epilogue's slabs fit the ring");
     static std::atomic<uint64_t> lds_set{0};
     TRY(allow_lds(ctx, (const void*)gemm_i8_kernel<GLU, GROUPED, TAIL>, smem, lds_set));
@@ -610,9 +636,9 @@ static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params&
     }
     if constexpr (!GROUPED) {
         switch (form) {
-            case TILE_128_128: return launch_tile<128, 128, 2, 4, 5, GLU, false>(ctx, p, s);
+            case TILE_128_128: return launch_tile<128, 128, 2, 4, 4, GLU, false>(ctx, p, s);
             case TILE_128_64: return launch_tile<128, 64, 4, 2, 6, GLU, false>(ctx, p, s);
-            case TILE_64_64: return launch_tile<64, 64, 2, 2, 5, GLU, false>(ctx, p, s);
+            case TILE_64_64: return launch_tile<64, 64, 2, 2, 4, GLU, false>(ctx, p, s);
             default: break;
         }
     }

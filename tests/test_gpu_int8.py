@@ -108,12 +108,15 @@ def product(lay, a, sa, b, sb, r=None, epilogue=0, ws=True):
 def check_product(c, a, sa, b, sb, r, epilogue, dtype):
     """Half a step for the sum's conversion, two for the scales, one for the residual, one for the storage type.  SwiGLU: silu' g / silu is at most
     1 + |g|; exp as exp2(g log2 e) is off by |g| 2^-23 and 2^-22, quotient and product by 3 u, all again as large in fp32 at most.  Below g = -88.72 exp(-g) is beyond
-    fp32, and the quotient 0 instead of g exp(g), which is less than 88.72 exp(-88.72) < 2^-121 in size."""
+    fp32, and the quotient 0 instead of g exp(g), which is less than 88.72 exp(-88.72) < 2^-121 in size.  With bf16 storage the reciprocal instruction stands
+    for the quotient: one unit (2 u) more, and 0 where it would be below 2^-126, the least normal number: g < -126 ln 2 = -87.33, and the
+    value less than 87.34 * 2^-126 < 2^-119.5."""
     p = torch.tensor(I8.product(a.cpu().numpy(), f64(sa), b.cpu().numpy(), f64(sb)))
     if epilogue:
         g, u = p.chunk(2, -1)
         ref = torch.tensor(I8.silu(g.numpy())) * u
-        tol = ref.abs() * ((1 + g.abs()) * 3 * U + 3 * U + g.abs() * 2.0 ** -23 + 2.0 ** -22 + 3 * U) + torch.where(g < -88.7, u.abs() * 2.0 ** -121, 0.0)
+        tol = ref.abs() * ((1 + g.abs()) * 3 * U + 3 * U + g.abs() * 2.0 ** -23 + 2.0 ** -22 + 3 * U) + torch.where(g < -87.3, u.abs() * (2.0 ** -119.5 if dtype == "bf16" else 2.0 ** -121), 0.0)
+        tol += ref.abs() * (2 * U if dtype == "bf16" else 0)
     else:
         ref = p + (0 if r is None else r.double().cpu())
         tol = p.abs() * 3 * U + ref.abs() * U
