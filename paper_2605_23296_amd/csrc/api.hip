@@ -185,7 +185,7 @@ void carve_moe_plan(Carver& cv, const compact_layer_cfg& c, int64_t rows, MoePla
     const int64_t rk = rows * c.top_k;
     plan.max_mtiles = (int32_t)(rk / mt + c.n_experts + 1);
     plan.counts = (int32_t*)cv.take(sizeof(int32_t) * c.n_experts);
-    plan.offsets = (int32_t*)cv.take(sizeof(int32_t) * (c.n_experts + 1));
+    plan.offsets = (int32_t*)cv.take(sizeof(int32_t) * (c.n_experts + 2));
     plan.sorted_token = (int32_t*)cv.take(sizeof(int32_t) * rk);
     plan.sorted_gate = (float*)cv.take(sizeof(float) * rk);
     plan.slot_of = (int32_t*)cv.take(sizeof(int32_t) * rk);

@@ -178,6 +178,7 @@ static int moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const
     g.tile_row0 = b.plan.tile_row0;
     g.tile_rows = b.plan.tile_rows;
     g.n_mtiles = (int32_t)std::min<int64_t>(rk / mtile + c.n_experts, b.plan.max_mtiles);   // the map's upper bound
+    g.n_live = b.plan.offsets + c.n_experts + 1;
     g.a_gather = b.plan.sorted_token;
     g.b_expert_stride = (int64_t)2 * c.ffn_dim * c.d_model;
     GemmI8Args a{(const int8_t*)d_m, d_m_scale, (const int8_t*)experts->d_gate_up, experts->d_gate_up_scale, nullptr, b.act, rk, c.ffn_dim, c.d_model, 1, &g};

@@ -212,6 +212,7 @@ struct GroupedArgs {          // all device pointers; null tile_expert => plain 
     int64_t b_expert_stride;      // elements between consecutive experts' B
     int32_t n_mtiles;
     int32_t mtile;                // rows per tile of the map (bf16: 256, 128 or 64)
+    const int32_t* n_live;        // [1] tiles of the map that have work, the first ones (products of codes)
 };
 // gemm_f32.hip : C = A B^T (+R) ; epilogue 1 = SwiGLU on stacked gate/up.  norm_g (nullable): A holds un-normalised
 // rows, RMSNorm(.; norm_g) is applied to them on the way (K = d_model)
@@ -324,7 +325,7 @@ int launch_attn_decode_prefix_bf16(compact_ctx* ctx, const BlockMeta* d_tail_met
 // moe.hip
 struct MoePlan {              // device buffers carved from the workspace
     int32_t* counts;          // [E]
-    int32_t* offsets;         // [E+1]
+    int32_t* offsets;         // [E+2]: first sorted row of every expert, rows, row tiles of the map
     int32_t* sorted_token;    // [rows*k] source token of every sorted row
     float* sorted_gate;       // [rows*k]
     int32_t* slot_of;         // [rows*k] sorted position of (token, j)

@@ -18,17 +18,21 @@ struct I8Tile {
 template <bool GROUPED, bool GLU, int BM, int OUTN, int GM>
 __device__ __forceinline__ I8Tile i8_tile(const GemmI8Params& p) {
     int tm, tn;
-    tile_at<GM>(xcd_order(blockIdx.x, gridDim.x), p.n_mtiles, p.n_ntiles, tm, tn);
     I8Tile t;
+    t.rows_valid = 0;
+    // the map's tiles with work alone are dealt out: the others are the last ones, and would be one XCD's whole share
+    const int n_mtiles = GROUPED ? *p.g.n_live : p.n_mtiles, n = GROUPED ? n_mtiles * p.n_ntiles : gridDim.x;
+    if (GROUPED && (int)blockIdx.x >= n) return t;
+    tile_at<GM>(xcd_order(blockIdx.x, n), n_mtiles, p.n_ntiles, tm, tn);
     t.n0 = tn * OUTN;
     t.W = p.W;
     t.ws = p.ws;
     if (GROUPED) {
         const int e = p.g.tile_expert[tm];
-        t.m0 = e < 0 ? 0 : p.g.tile_row0[tm];
-        t.rows_valid = e < 0 ? 0 : p.g.tile_rows[tm];
-        t.W += (int64_t)max(e, 0) * p.g.b_expert_stride;
-        t.ws += (int64_t)max(e, 0) * p.N * (GLU ? 2 : 1);
+        t.m0 = p.g.tile_row0[tm];
+        t.rows_valid = p.g.tile_rows[tm];
+        t.W += (int64_t)e * p.g.b_expert_stride;
+        t.ws += (int64_t)e * p.N * (GLU ? 2 : 1);
     } else {
         t.m0 = (int64_t)tm * BM;
         t.rows_valid = (int)min((int64_t)BM, p.M - t.m0);
@@ -336,17 +340,13 @@ __device__ __forceinline__ void i8_mfmas(intx4 (&acc)[TM][TN], const intx4 (&xf)
     plain_barrier();
 }
 
-// TAIL: K is no multiple of 128; chunks beyond it are zeros on the activations' side, the row's first chunk on the weights'
-template <bool TAIL, bool X>
-__device__ __forceinline__ void i8_load_piece(const int8_t* src, int chunk, int kt, int nk, int K, char* dst) {
-    const int k0 = kt * I8_BK;
-    if (!TAIL || kt + 1 < nk)
-        load16_to_lds(src + k0, dst);
-    else
-        load16_to_lds(k0 + chunk < K ? src + k0 : X ? zero_codes : src - chunk, dst);
+// Where a lane reads its 16 codes of the last k-tile, if that is cut: chunks beyond K are zeros on the activations' side, the row's first
+// chunk on the weights'.  Called once, before the first load of that k-tile: no load is of another one after it.
+__device__ __forceinline__ void i8_cut(const int8_t*& src, int chunk, int k_last, int K, bool is_x) {
+    if (k_last + chunk >= K) src = (is_x ? zero_codes : src - chunk) - k_last;
 }
 
-template <bool GLU, bool GROUPED, bool TAIL>
+template <bool GLU, bool GROUPED>
 __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile& tp, char* smem) {
     constexpr int WN = 4, BK = I8_BK, WTM = 128, WTN = 64, TM = WTM / 16, TN = WTN / 16, HT = 128 * BK;
     constexpr int WOUT = GLU ? WTN / 2 : WTN;
@@ -389,8 +389,14 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
     auto gload = [&](auto qtag, int kt, int buf) __attribute__((always_inline)) {
         constexpr int q = decltype(qtag)::value;
         char* dst = smem + (buf * 4 + q) * HT + wave * 2 * 8 * BK;
-        i8_load_piece<TAIL, q % 2 == 1>(src[q][0], chunk[0], kt, nk, p.K, dst);
-        i8_load_piece<TAIL, q % 2 == 1>(src[q][1], chunk[1], kt, nk, p.K, dst + 8 * BK);
+        load16_to_lds(src[q][0] + kt * BK, dst);
+        load16_to_lds(src[q][1] + kt * BK, dst + 8 * BK);
+    };
+    auto cut = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) i8_cut(src[q][u], chunk[u], (nk - 1) * BK, p.K, q % 2 == 1);
     };
     intx4 xf[4][2];
     auto read_w = [&](auto jtag, int buf, intx4 (&f)[2][2]) __attribute__((always_inline)) {
@@ -411,6 +417,7 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
     // K the last k-tile is loaded again, into slots nobody reads.
     auto k_tile = [&](int kt, int buf, intx4 (&wa)[2][2], intx4 (&wb)[2][2]) __attribute__((always_inline)) {
         const int kn = min(kt + 2, nk - 1);
+        if (kt + 2 == nk - 1) cut();
         read_x(I0{}, buf);
         gload(I0{}, kn, buf);
         ring_barrier<12>();
@@ -428,16 +435,14 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
         ring_barrier<12>();
         i8_mfmas<1, 0>(acc, xf, wa);
     };
-    {   // all half tiles of k-tiles 0 and 1; W0 and X0 of k-tile 0 have landed when all but 12 loads have
-        const int k1 = min(1, nk - 1);
-        gload(I0{}, 0, 0);
-        gload(I1{}, 0, 0);
-        gload(I2{}, 0, 0);
-        gload(I3{}, 0, 0);
-        gload(I0{}, k1, 1);
-        gload(I1{}, k1, 1);
-        gload(I2{}, k1, 1);
-        gload(I3{}, k1, 1);
+    // all half tiles of k-tiles 0 and 1; W0 and X0 of k-tile 0 have landed when all but 12 loads have
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (i == nk - 1) cut();
+        gload(I0{}, min(i, nk - 1), i);
+        gload(I1{}, min(i, nk - 1), i);
+        gload(I2{}, min(i, nk - 1), i);
+        gload(I3{}, min(i, nk - 1), i);
     }
     intx4 wA[2][2], wB[2][2];
     ring_barrier<12>();
@@ -459,7 +464,7 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
 // The same schedule over 128 x 256 tiles (wavefronts of 64 x 64, two phases per k-tile: X0 W0, X0 W1).  A k-tile is three half tiles (W0,
 // X0, W1); the ring holds three k-tiles (nine slots, 144 KB).  A phase requests three of the six 8-row pieces that a wavefront owns of
 // a k-tile; 11 or 12 of them may still fly when the next phase's operands must be there.
-template <bool GLU, bool GROUPED, bool TAIL>
+template <bool GLU, bool GROUPED>
 __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile& tp, char* smem) {
     constexpr int WN = 4, BK = I8_BK, WTM = 64, WTN = 64, TM = WTM / 16, TN = WTN / 16, HT = 128 * BK;
     constexpr int WOUT = GLU ? WTN / 2 : WTN;
@@ -495,9 +500,12 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
     const char* xs = smem + wm * 64 * BK;
     const char* ws = smem + wn * 32 * BK;
     // piece u of half tile q of k-tile kt (past the end: the last one again), into k-tile buffer buf
-    auto gload = [&](auto qtag, int u, int kt, int buf) __attribute__((always_inline)) {
-        constexpr int q = decltype(qtag)::value;
-        i8_load_piece<TAIL, q == 1>(src[q][u], chunk[u], min(kt, nk - 1), nk, p.K, smem + (buf * 3 + q) * HT + (wave * 2 + u) * 8 * BK);
+    auto gload = [&](int q, int u, int kt, int buf) __attribute__((always_inline)) {
+        load16_to_lds(src[q][u] + min(kt, nk - 1) * BK, smem + (buf * 3 + q) * HT + (wave * 2 + u) * 8 * BK);
+    };
+    auto cut = [&](int q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) i8_cut(src[q][u], chunk[u], (nk - 1) * BK, p.K, q == 1);
     };
     auto read_w = [&](int j, int buf, intx4 (&f)[2][2]) __attribute__((always_inline)) {
 #pragma unroll
@@ -508,35 +516,37 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
     intx4 xf[4][2], w0[2][2], w1[2][2];
     // k-tile kt in buffer b0, kt + 1 in b1, kt + 2 in b2
     auto k_tile = [&](int kt, int b0, int b1, int b2) __attribute__((always_inline)) {
+        if (kt + 2 == nk - 1) cut(2);
+        if (kt + 3 == nk - 1) {
+            cut(0);
+            cut(1);
+        }
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int mt = 0; mt < 4; ++mt) xf[mt][kk] = *reinterpret_cast<const intx4*>(xs + (b0 * 3 + 1) * HT + mt * 16 * BK + foff[kk]);
-        gload(I2{}, 0, kt + 2, b2);
-        gload(I2{}, 1, kt + 2, b2);
-        gload(I0{}, 0, kt + 3, b0);
+        gload(2, 0, kt + 2, b2);
+        gload(2, 1, kt + 2, b2);
+        gload(0, 0, kt + 3, b0);
         ring_barrier<11>();
         i8_mfmas<0, 0>(acc, xf, w0);
         read_w(1, b0, w1);
         read_w(0, b1, w0);
-        gload(I0{}, 1, kt + 3, b0);
-        gload(I1{}, 0, kt + 3, b0);
-        gload(I1{}, 1, kt + 3, b0);
+        gload(0, 1, kt + 3, b0);
+        gload(1, 0, kt + 3, b0);
+        gload(1, 1, kt + 3, b0);
         ring_barrier<12>();
         i8_mfmas<0, 1>(acc, xf, w1);
     };
     // k-tiles 0 and 1, and W0, X0 of k-tile 2; the first two half tiles have landed when all but 12 pieces have
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        gload(I0{}, 0, i, i);
-        gload(I0{}, 1, i, i);
-        gload(I1{}, 0, i, i);
-        gload(I1{}, 1, i, i);
-        if (i < 2) {
-            gload(I2{}, 0, i, i);
-            gload(I2{}, 1, i, i);
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int q = 0; q < (i == 2 ? 2 : 3); ++q) {
+            if (i == nk - 1) cut(q);
+            gload(q, 0, i, i);
+            gload(q, 1, i, i);
         }
-    }
     ring_barrier<12>();
     read_w(0, 0, w0);
     ring_barrier<12>();
@@ -558,7 +568,7 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
 // Plain products: the output is cut into slots of 256 x 256, in groups of 4 row tiles per column tile; the first n_full of them are a
 // workgroup each, the others two workgroups of 128 x 256, and last come the halves of a bottom row tile of at most 128 rows.  Routed
 // products: a workgroup per tile of the map, in the form that its rows need.
-template <bool GLU, bool GROUPED, bool TAIL>
+template <bool GLU, bool GROUPED>
 __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
     constexpr int OUTN = GLU ? 128 : 256;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -566,9 +576,9 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
         const I8Tile tp = p.g.mtile == 256 ? i8_tile<true, GLU, 256, OUTN, 4>(p) : i8_tile<true, GLU, 128, OUTN, 8>(p);
         if (tp.rows_valid <= 0) return;
         if (tp.rows_valid > 128)
-            i8_tile_256<GLU, true, TAIL>(p, tp, smem);
+            i8_tile_256<GLU, true>(p, tp, smem);
         else
-            i8_tile_128<GLU, true, TAIL>(p, tp, smem);
+            i8_tile_128<GLU, true>(p, tp, smem);
     } else {
         const int i = blockIdx.x;
         int tm, tn;
@@ -580,7 +590,7 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
             tp.m0 = (int64_t)tm * 256;
             tp.n0 = tn * OUTN;
             tp.rows_valid = (int)min((int64_t)256, p.M - tp.m0);
-            i8_tile_256<GLU, false, TAIL>(p, tp, smem);
+            i8_tile_256<GLU, false>(p, tp, smem);
         } else {
             const int h = xcd_order(i - p.n_full, gridDim.x - p.n_full);
             const int slot = p.n_full + h / 2, slots = p.n_mtiles * p.n_ntiles;
@@ -593,18 +603,18 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
             }
             tp.n0 = tn * OUTN;
             tp.rows_valid = (int)min((int64_t)128, p.M - tp.m0);
-            i8_tile_128<GLU, false, TAIL>(p, tp, smem);
+            i8_tile_128<GLU, false>(p, tp, smem);
         }
     }
 }
 
-template <bool GLU, bool GROUPED, bool TAIL>
-static int launch_large_form(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
+template <bool GLU, bool GROUPED>
+static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
     constexpr int OUTN = GLU ? 128 : 256;
     constexpr size_t smem = LARGE_RING + 3 * 256 * 4;   // the epilogue's slabs fit in
     static_assert((size_t)8 * 16 * (OUTN / 4 + 4) * sizeof(float) <= smem, "the epilogue's slabs fit the ring");
     static std::atomic<uint64_t> lds_set{0};
-    TRY(allow_lds(ctx, (const void*)gemm_i8_kernel<GLU, GROUPED, TAIL>, smem, lds_set));
+    TRY(allow_lds(ctx, (const void*)gemm_i8_kernel<GLU, GROUPED>, smem, lds_set));
     p.n_ntiles = (p.N + OUTN - 1) / OUTN;
     int64_t wgs;
     if (GROUPED) {
@@ -617,15 +627,10 @@ static int launch_large_form(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, 
         wgs = p.n_full + 2 * (lt.slots - p.n_full) + lt.bottom;
     }
     if (wgs == 0) return COMPACT_OK;
-    gemm_i8_kernel<GLU, GROUPED, TAIL><<<dim3((unsigned)wgs), 512, smem, s>>>(p);
+    gemm_i8_kernel<GLU, GROUPED><<<dim3((unsigned)wgs), 512, smem, s>>>(p);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }
-template <bool GLU, bool GROUPED>
-static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
-    return p.K % I8_BK ? launch_large_form<GLU, GROUPED, true>(ctx, p, n_full, s) : launch_large_form<GLU, GROUPED, false>(ctx, p, n_full, s);
-}
-
 template <bool GLU, bool GROUPED>
 static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params& p, hipStream_t s) {
     switch (form) {

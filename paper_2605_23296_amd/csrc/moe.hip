@@ -183,6 +183,7 @@ __global__ __launch_bounds__(256) void expert_scan_kernel(const int32_t* __restr
     }
     __syncthreads();
     for (int e = threadIdx.x; e <= E; e += 256) offsets[e] = off[e];
+    if (threadIdx.x == 0) offsets[E + 1] = toff[E];
     for (int e = threadIdx.x; e < E; e += 256) {
         const int cnt = off[e + 1] - off[e];
         for (int i = 0; toff[e] + i < toff[e + 1]; ++i) {
@@ -279,6 +280,7 @@ __device__ __forceinline__ void plan_small(int t, int my, float gate, int n, int
     __syncthreads();
     if (!on) return;
     for (int e = t; e <= E; e += 256) o.offsets[e] = off[e];
+    if (t == 0) o.offsets[E + 1] = toff[E];
     if (t < E) {
         for (int i = 0; toff[t] + i < toff[t + 1]; ++i) {
             const int ti = toff[t] + i;
