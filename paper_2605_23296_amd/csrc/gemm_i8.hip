@@ -340,13 +340,13 @@ __device__ __forceinline__ void i8_mfmas(intx4 (&acc)[TM][TN], const intx4 (&xf)
     plain_barrier();
 }
 
-// Where a lane reads its 16 codes of the last k-tile, if that is cut: chunks beyond K are zeros on the activations' side, the row's first
+// CUT: K is no multiple of 128.  Where a lane reads its 16 codes of the last k-tile then: chunks beyond K are zeros on the activations' side, the row's first
 // chunk on the weights'.  Called once, before the first load of that k-tile: no load is of another one after it.
 __device__ __forceinline__ void i8_cut(const int8_t*& src, int chunk, int k_last, int K, bool is_x) {
     if (k_last + chunk >= K) src = (is_x ? zero_codes : src - chunk) - k_last;
 }
 
-template <bool GLU, bool GROUPED>
+template <bool GLU, bool GROUPED, bool CUT>
 __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile& tp, char* smem) {
     constexpr int WN = 4, BK = I8_BK, WTM = 128, WTN = 64, TM = WTM / 16, TN = WTN / 16, HT = 128 * BK;
     constexpr int WOUT = GLU ? WTN / 2 : WTN;
@@ -417,7 +417,7 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
     // K the last k-tile is loaded again, into slots nobody reads.
     auto k_tile = [&](int kt, int buf, intx4 (&wa)[2][2], intx4 (&wb)[2][2]) __attribute__((always_inline)) {
         const int kn = min(kt + 2, nk - 1);
-        if (kt + 2 == nk - 1) cut();
+        if (CUT && kt + 2 == nk - 1) cut();
         read_x(I0{}, buf);
         gload(I0{}, kn, buf);
         ring_barrier<12>();
@@ -438,7 +438,7 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
     // all half tiles of k-tiles 0 and 1; W0 and X0 of k-tile 0 have landed when all but 12 loads have
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        if (i == nk - 1) cut();
+        if (CUT && i == nk - 1) cut();
         gload(I0{}, min(i, nk - 1), i);
         gload(I1{}, min(i, nk - 1), i);
         gload(I2{}, min(i, nk - 1), i);
@@ -464,7 +464,7 @@ __device__ __forceinline__ void i8_tile_256(const GemmI8Params& p, const I8Tile&
 // The same schedule over 128 x 256 tiles (wavefronts of 64 x 64, two phases per k-tile: X0 W0, X0 W1).  A k-tile is three half tiles (W0,
 // X0, W1); the ring holds three k-tiles (nine slots, 144 KB).  A phase requests three of the six 8-row pieces that a wavefront owns of
 // a k-tile; 11 or 12 of them may still fly when the next phase's operands must be there.
-template <bool GLU, bool GROUPED>
+template <bool GLU, bool GROUPED, bool CUT>
 __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile& tp, char* smem) {
     constexpr int WN = 4, BK = I8_BK, WTM = 64, WTN = 64, TM = WTM / 16, TN = WTN / 16, HT = 128 * BK;
     constexpr int WOUT = GLU ? WTN / 2 : WTN;
@@ -516,8 +516,8 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
     intx4 xf[4][2], w0[2][2], w1[2][2];
     // k-tile kt in buffer b0, kt + 1 in b1, kt + 2 in b2
     auto k_tile = [&](int kt, int b0, int b1, int b2) __attribute__((always_inline)) {
-        if (kt + 2 == nk - 1) cut(2);
-        if (kt + 3 == nk - 1) {
+        if (CUT && kt + 2 == nk - 1) cut(2);
+        if (CUT && kt + 3 == nk - 1) {
             cut(0);
             cut(1);
         }
@@ -543,7 +543,7 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
     for (int i = 0; i < 3; ++i)
 #pragma unroll
         for (int q = 0; q < (i == 2 ? 2 : 3); ++q) {
-            if (i == nk - 1) cut(q);
+            if (CUT && i == nk - 1) cut(q);
             gload(q, 0, i, i);
             gload(q, 1, i, i);
         }
@@ -568,7 +568,7 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
 // Plain products: the output is cut into slots of 256 x 256, in groups of 4 row tiles per column tile; the first n_full of them are a
 // workgroup each, the others two workgroups of 128 x 256, and last come the halves of a bottom row tile of at most 128 rows.  Routed
 // products: a workgroup per tile of the map, in the form that its rows need.
-template <bool GLU, bool GROUPED>
+template <bool GLU, bool GROUPED, bool CUT>
 __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
     constexpr int OUTN = GLU ? 128 : 256;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -576,9 +576,9 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
         const I8Tile tp = p.g.mtile == 256 ? i8_tile<true, GLU, 256, OUTN, 4>(p) : i8_tile<true, GLU, 128, OUTN, 8>(p);
         if (tp.rows_valid <= 0) return;
         if (tp.rows_valid > 128)
-            i8_tile_256<GLU, true>(p, tp, smem);
+            i8_tile_256<GLU, true, CUT>(p, tp, smem);
         else
-            i8_tile_128<GLU, true>(p, tp, smem);
+            i8_tile_128<GLU, true, CUT>(p, tp, smem);
     } else {
         const int i = blockIdx.x;
         int tm, tn;
@@ -590,7 +590,7 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
             tp.m0 = (int64_t)tm * 256;
             tp.n0 = tn * OUTN;
             tp.rows_valid = (int)min((int64_t)256, p.M - tp.m0);
-            i8_tile_256<GLU, false>(p, tp, smem);
+            i8_tile_256<GLU, false, CUT>(p, tp, smem);
         } else {
             const int h = xcd_order(i - p.n_full, gridDim.x - p.n_full);
             const int slot = p.n_full + h / 2, slots = p.n_mtiles * p.n_ntiles;
@@ -603,18 +603,18 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
             }
             tp.n0 = tn * OUTN;
             tp.rows_valid = (int)min((int64_t)128, p.M - tp.m0);
-            i8_tile_128<GLU, false>(p, tp, smem);
+            i8_tile_128<GLU, false, CUT>(p, tp, smem);
         }
     }
 }
 
-template <bool GLU, bool GROUPED>
-static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
+template <bool GLU, bool GROUPED, bool CUT>
+static int launch_large_k(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
     constexpr int OUTN = GLU ? 128 : 256;
     constexpr size_t smem = LARGE_RING + 3 * 256 * 4;   // the epilogue's slabs fit in
     static_assert((size_t)8 * 16 * (OUTN / 4 + 4) * sizeof(float) <= smem, "the epilogue's slabs fit the ring");
     static std::atomic<uint64_t> lds_set{0};
-    TRY(allow_lds(ctx, (const void*)gemm_i8_kernel<GLU, GROUPED>, smem, lds_set));
+    TRY(allow_lds(ctx, (const void*)gemm_i8_kernel<GLU, GROUPED, CUT>, smem, lds_set));
     p.n_ntiles = (p.N + OUTN - 1) / OUTN;
     int64_t wgs;
     if (GROUPED) {
@@ -627,10 +627,16 @@ static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipSt
         wgs = p.n_full + 2 * (lt.slots - p.n_full) + lt.bottom;
     }
     if (wgs == 0) return COMPACT_OK;
-    gemm_i8_kernel<GLU, GROUPED><<<dim3((unsigned)wgs), 512, smem, s>>>(p);
+    gemm_i8_kernel<GLU, GROUPED, CUT><<<dim3((unsigned)wgs), 512, smem, s>>>(p);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }
+// (a branch for the cut k-tile costs products without one 3 %)
+template <bool GLU, bool GROUPED>
+static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipStream_t s) {
+    return p.K % I8_BK ? launch_large_k<GLU, GROUPED, true>(ctx, p, n_full, s) : launch_large_k<GLU, GROUPED, false>(ctx, p, n_full, s);
+}
+
 template <bool GLU, bool GROUPED>
 static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params& p, hipStream_t s) {
     switch (form) {
