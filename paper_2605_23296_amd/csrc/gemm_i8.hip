@@ -638,27 +638,35 @@ static int launch_large(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hipSt
 }
 
 template <bool GLU, bool GROUPED>
-static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params& p, hipStream_t s) {
+static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params& p, hipStream_t s, int slices = 1) {
     switch (form) {
         case TILE_256: return launch_large<GLU, GROUPED>(ctx, p, n_full, s);
         case TILE_128: return launch_large<GLU, GROUPED>(ctx, p, 0, s);
-        case TILE_64_128: return launch_tile<64, 128, 2, 4, 6, GLU, GROUPED>(ctx, p, s);
+        case TILE_64_128: return launch_tile<64, 128, 2, 4, 6, GLU, GROUPED>(ctx, p, s, slices);
         default: break;
     }
     if constexpr (!GROUPED) {
         switch (form) {
-            case TILE_128_128: return launch_tile<128, 128, 2, 4, 4, GLU, false>(ctx, p, s);
-            case TILE_128_64: return launch_tile<128, 64, 4, 2, 6, GLU, false>(ctx, p, s);
-            case TILE_64_64: return launch_tile<64, 64, 2, 2, 4, GLU, false>(ctx, p, s);
+            case TILE_128_128: return launch_tile<128, 128, 2, 4, 4, GLU, false>(ctx, p, s, slices);
+            case TILE_128_64: return launch_tile<128, 64, 4, 2, 6, GLU, false>(ctx, p, s, slices);
+            case TILE_64_64: return launch_tile<64, 64, 2, 2, 4, GLU, false>(ctx, p, s, slices);
             default: break;
         }
     }
     return set_err(ctx, COMPACT_EINVAL, "unknown GEMM tile");
 }
 
+// Slices of K for products whose 64 x 64 tiles leave half of the chip idle and more: as many as fill its 256 compute units, of 16 k-tiles
+// at least (the second launch, which adds the slices up, costs 3 us).  N 4096 K 14336 at 17 / 64 / 128 rows 31 / 36 / 36 us whole, 17.7 /
+// 19.2 / 25.6 in 4 / 4 / 2 slices, 20 / 24 / 31 in 6; K 6144 at 64 rows 16.8 whole, 13.5 in 3; N 1024 K 14336 at 64 rows 32.6, in 4 16.0, in 8 14.6.
+static int gemm_i8_slices(int64_t M, int N, int K, int epilogue) {
+    const int64_t tiles = (M + 63) / 64 * ((N + (epilogue ? 31 : 63)) / (epilogue ? 32 : 64));
+    if (M <= I8_STREAM_ROWS || tiles > 128) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, (K + I8_BK - 1) / I8_BK / 16, 8}));
+}
 size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {
-    (void)M, (void)N, (void)K, (void)epilogue;
-    return 0;
+    const int slices = gemm_i8_slices(M, N, K, epilogue);
+    return slices < 2 ? 0 : (size_t)slices * M * N * (epilogue ? 2 : 1) * sizeof(int);
 }
 int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) {
     if (rows <= 12 * n_experts) return I8_STREAM_ROWS;
@@ -681,7 +689,6 @@ static GemmI8Params i8_params(compact_ctx* ctx, const GemmI8Args& a) {
 }
 
 int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_bytes, hipStream_t s) {
-    (void)ws, (void)ws_bytes;
     if (a.M == 0) return COMPACT_OK;
     GemmI8Params p = i8_params(ctx, a);
     int n_cus = 0;
@@ -694,25 +701,32 @@ int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_by
         return a.epilogue ? launch_form<true, true>(ctx, form, 0, p, s) : launch_form<false, true>(ctx, form, 0, p, s);
     }
     if (a.M <= I8_STREAM_ROWS) return launch_stream_i8(ctx, p, a.epilogue != 0, s);
+    const int slices = gemm_i8_slices(a.M, a.N, a.K, a.epilogue);
+    if (slices > 1 && ws && ((uintptr_t)ws & 15) == 0 && ws_bytes >= gemm_i8_workspace(a.M, a.N, a.K, a.epilogue)) {
+        p.sums = (int*)ws;
+        return a.epilogue ? launch_form<true, false>(ctx, TILE_64_64, 0, p, s, slices) : launch_form<false, false>(ctx, TILE_64_64, 0, p, s, slices);
+    }
     int64_t n_full = 0;
     const int form = pick_tile(a.M, a.N, (a.K + 127) / 128 * 64, a.epilogue, n_cus, &n_full);
     return a.epilogue ? launch_form<true, false>(ctx, form, n_full, p, s) : launch_form<false, false>(ctx, form, n_full, p, s);
 }
 
 // For the tests, not part of compact.h: the product in tile form `form` (TILE_FORMS: whole tiles and halves mixed, as many slots
-// in either).
-extern "C" int compact_test_gemm_i8_form(compact_ctx* ctx, int32_t form, const void* a, const float* a_scale, const void* b,
+// in either), the small ones in `slices` of K with room for their sums.
+extern "C" int compact_test_gemm_i8_form(compact_ctx* ctx, int32_t form, int32_t slices, void* sums, const void* a, const float* a_scale, const void* b,
                                          const float* b_scale, const void* r, void* c, int64_t M, int32_t N, int32_t K, int32_t epilogue,
                                          void* hip_stream) {
-    if (!ctx || !a || !a_scale || !b || !b_scale || !c || M < 1 || N < 1 || K < 16 || K % 16 || form < 0 || form > TILE_FORMS || (epilogue != 0 && epilogue != 1))
+    if (!ctx || !a || !a_scale || !b || !b_scale || !c || M < 1 || N < 1 || K < 16 || K % 16 || form < 0 || form > TILE_FORMS || (epilogue != 0 && epilogue != 1) ||
+        slices < 1 || slices > (K + I8_BK - 1) / I8_BK || (slices > 1 && (!sums || form <= TILE_128 || form == TILE_FORMS)))
         return COMPACT_EINVAL;
     const GemmI8Args g{(const int8_t*)a, a_scale, (const int8_t*)b, b_scale, r, c, M, N, K, epilogue, nullptr};
     GemmI8Params p = i8_params(ctx, g);
+    p.sums = (int*)sums;
     int64_t n_full = large_tiles(M, (N + (epilogue ? 127 : 255)) / (epilogue ? 128 : 256)).slots;
     if (form == TILE_FORMS) {
         form = TILE_256;
         n_full /= 2;
     }
     hipStream_t s = (hipStream_t)hip_stream;
-    return epilogue ? launch_form<true, false>(ctx, form, n_full, p, s) : launch_form<false, false>(ctx, form, n_full, p, s);
+    return epilogue ? launch_form<true, false>(ctx, form, n_full, p, s, slices) : launch_form<false, false>(ctx, form, n_full, p, s, slices);
 }

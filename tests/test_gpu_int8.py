@@ -129,7 +129,7 @@ def check_product(c, a, sa, b, sb, r, epilogue, dtype):
 @pytest.mark.parametrize("epilogue,res", [(0, False), (0, True), (1, False)])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 8, 64), (2, 3, 48), (3, 16, 128), (5, 100, 144), (8, 96, 4096), (9, 257, 272), (15, 24, 1040), (16, 64, 2880), (17, 64, 128),
                                    (31, 130, 256), (33, 7, 112), (63, 264, 1152), (64, 128, 512), (65, 72, 384), (127, 40, 640), (129, 520, 896), (200, 1001, 208),
-                                   (257, 264, 272), (300, 136, 3968), (513, 72, 1024)])
+                                   (257, 264, 272), (300, 136, 3968), (513, 72, 1024), (17, 96, 4096), (64, 1000, 4112), (130, 77, 6160)])
 def test_products(dtype, epilogue, res, M, N, K):
     lay = layer(dtype=dtype)
     a, b = codes(M, K, 1), codes((1 + epilogue) * N, K, 2, -128)
@@ -138,14 +138,21 @@ def test_products(dtype, epilogue, res, M, N, K):
     c = product(lay, a, sa, b, sb, r, epilogue)
     check_product(c, a, sa, b, sb, r, epilogue, dtype)
     assert torch.equal(product(lay, a, sa, b, sb, r, epilogue, ws=False), c)     # a workspace changes no bit
+    if lay.gemm_i8_workspace_bytes(M, N, K, epilogue):
+        lay.ws = torch.empty(lay.gemm_i8_workspace_bytes(M, N, K, epilogue) - 1, dtype=torch.uint8, device="cuda")   # one that is too small is none
+        small = torch.empty_like(c)
+        lay.compact_gemm_i8(a, sa, b, sb, r, small, epilogue)
+        assert torch.equal(small, c)
+    assert (lay.gemm_i8_workspace_bytes(M, N, K, epilogue) > 0) == (M > 16 and K >= 4096)
 
 
-def in_form(lay, form, a, sa, b, sb, r, epilogue):
-    """The product in one of the tile forms (6: 256 x 256 tiles and their halves, mixed)."""
+def in_form(lay, form, a, sa, b, sb, r, epilogue, slices=1):
+    """The product in one of the tile forms (6: 256 x 256 tiles and their halves, mixed), or in slices of K."""
     M, K, N = a.shape[0], a.shape[1], b.shape[0] // (2 if epilogue else 1)
     c = torch.full((M + 1, N), 7.0, dtype=lay.torch_dtype, device="cuda")
     ptr = lambda t: None if t is None else C.c_void_p(t.data_ptr())   # noqa: E731
-    lay.check(lay.L.compact_test_gemm_i8_form(lay.ctx, C.c_int32(form), ptr(a), ptr(sa), ptr(b), ptr(sb), ptr(r), ptr(c), C.c_int64(M), C.c_int32(N), C.c_int32(K),
+    sums = torch.empty(slices * M * len(b), dtype=torch.int32, device="cuda")
+    lay.check(lay.L.compact_test_gemm_i8_form(lay.ctx, C.c_int32(form), C.c_int32(slices), ptr(sums), ptr(a), ptr(sa), ptr(b), ptr(sb), ptr(r), ptr(c), C.c_int64(M), C.c_int32(N), C.c_int32(K),
                                               C.c_int32(epilogue), C.c_void_p(torch.cuda.current_stream().cuda_stream)))
     assert bool((c[M] == 7.0).all())
     return c[:M]
@@ -163,6 +170,9 @@ def test_every_tile_form_at_its_edges(K, epilogue, res):
         check_product(want, a, sa, b, sb, r, epilogue, "bf16")
         for form in (0, 1, 2, 3, 4, 6):
             assert torch.equal(in_form(lay, form, a, sa, b, sb, r, epilogue), want), (M, N, form)
+        for form in (2, 3, 4, 5):
+            for slices in {min(n, -(-K // 128)) for n in (2, 3, 5, 7)} - {1}:
+                assert torch.equal(in_form(lay, form, a, sa, b, sb, r, epilogue, slices), want), (M, N, form, slices)
 
 
 @pytest.mark.parametrize("M", [1, 16, 40, 200, 700])
