@@ -420,7 +420,8 @@ int compact_block_norm(compact_ctx* ctx, const void* d_x, const void* d_b, const
  *   s = softmax or sigmoid of the row's logits;  c = s + bias;  the experts are n_groups groups of neighbours, a group counts as the
  *   sum of its group_top largest c; eligible are the experts of the topk_groups best groups; the top_k eligible ones with the largest c are chosen,
  *   in descending order; weight = s * factor, divided first by the sum of the chosen s if renorm.  Ties go to the lower index.
- * Scores are compared to 44 bits.  An expert whose logit is -inf or NaN, or whose c is -inf or NaN, is chosen only where fewer than top_k
+ * c is compared to 44 bits; without a bias, and where no sums of scores rank groups (no groups, or group_top 1), the logits themselves are compared,
+ * of which scores are increasing functions.  An expert whose logit is -inf or NaN, or whose c is -inf or NaN, is chosen only where fewer than top_k
  * others are eligible (weight 0 for the logit's sake), does not count in its group, and a group of such experts is the last choice; a row without
  * a finite logit has weights 0.  Logits of +inf share the softmax among them.  Indices are always distinct and valid. */
 enum { COMPACT_SCORE_SOFTMAX = 0, COMPACT_SCORE_SIGMOID = 1 };

@@ -40,11 +40,24 @@ def residual(x, b, g_post, gate, alpha, eps):
     return x + alpha * (b if gate is None else gate * b)
 
 
+def _gap(v, n):
+    """v descending: the least distance, relative to the larger, of neighbours that differ, among the first n and up to the next smaller one."""
+    gap = np.inf
+    for i in range(len(v) - 1):
+        if v[i] != v[i + 1] and v[i] < np.inf and v[i + 1] > -np.inf:
+            gap = min(gap, (v[i] - v[i + 1]) / max(abs(v[i]), abs(v[i + 1])))
+        if i >= n - 1 and v[i] != v[i + 1]:
+            break
+    return gap
+
+
 def route(logits, bias, top_k, score, n_groups=1, topk_groups=1, group_top=1, renorm=True, factor=1.0):
-    """One row after another; (idx, weight, gap): gap is the least distance of two numbers that the choice or its order rests on."""
+    """One row after another; (idx, weight, gap): gap is the least distance, relative to the larger, of two
+    different numbers that the choice or its order rests on."""
     E = logits.shape[1]
     S = E // n_groups
     idx, weight, gaps = [], [], []
+    by_logit = bias is None and (topk_groups == n_groups or group_top == 1)    # scores are increasing functions of them
     for l in np.asarray(logits, dtype=np.float64):
         l = np.where(np.isnan(l), -np.inf, l)
         dead, top = l == -np.inf, l.max()
@@ -54,7 +67,7 @@ def route(logits, bias, top_k, score, n_groups=1, topk_groups=1, group_top=1, re
             else:
                 s = np.where(dead, 0.0, np.where(l == top, 1.0, np.exp(l - top)))
                 s = s / s.sum() if s.sum() > 0 else s
-            c = s + (0.0 if bias is None else np.asarray(bias, dtype=np.float64))
+            c = l if by_logit else s + (0.0 if bias is None else np.asarray(bias, dtype=np.float64))
         c = np.where(np.isnan(c) | dead, -np.inf, c)
         gap = np.inf
         ok = np.ones(E, dtype=bool)
@@ -65,16 +78,12 @@ def route(logits, bias, top_k, score, n_groups=1, topk_groups=1, group_top=1, re
                 if live:
                     total[g] = sum(live)
             order = sorted(range(n_groups), key=lambda g: (-total[g], g))
-            a, b = total[order[topk_groups - 1]], total[order[topk_groups]]
-            if b > -np.inf and a != b:
-                gap = a - b
+            gap = _gap(total[order], topk_groups)
             ok[:] = False
             for g in order[:topk_groups]:
                 ok[g * S:(g + 1) * S] = True
         order = sorted((e for e in range(E) if ok[e]), key=lambda e: (-c[e], e))
-        for u, v in zip(order[:top_k], order[1:top_k + 1]):
-            if c[v] > -np.inf and c[u] != c[v]:
-                gap = min(gap, c[u] - c[v])
+        gap = min(gap, _gap(c[order], top_k))
         chosen = order[:top_k]
         w = s[chosen]
         if renorm:

@@ -5,7 +5,7 @@
 // Monotone map of a number to 64 bits whose low 8 are its place: the larger key is the larger value to 44 bits, among equal ones the
 // lower place.  No key of a number is 0.
 __device__ __forceinline__ uint64_t key_of(double v, int place) {
-    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);   // (-0 is 0)
     const uint64_t u = b >> 63 ? ~b : b | 0x8000000000000000ull;
     return (u & ~255ull) | (uint64_t)(255 - place);
 }
@@ -19,22 +19,33 @@ __device__ __forceinline__ uint64_t wave_max_key(uint64_t k) {
     return k;
 }
 
-// One wavefront per row, lane l owns experts l, l + 64, l + 128, l + 192.
-__global__ __launch_bounds__(256) void route_kernel(const compact_route_rule rule, const float* __restrict__ logits,
-                                                    const float* __restrict__ bias, int64_t rows, int E, int k,
-                                                    int32_t* __restrict__ idx, float* __restrict__ weight) {
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (row >= rows) return;
-    const int lane = threadIdx.x & 63;
+// What the experts are ordered by: their c, or without a bias, and where no sums of scores rank the groups, the logits themselves, of which the scores
+// are increasing functions.
+struct RouteArgs {
+    compact_route_rule rule;
+    const float* logits;
+    const float* bias;
+    int64_t rows;
+    int E, k;
+    int by_logit;
+    int inv_size;   // 65536 / experts of a group, rounded up: e / size = e * inv_size >> 16 for e < 256
+    int32_t* idx;
+    float* weight;
+};
+
+// Every row that the kernel below passes on: one wavefront, lane l owns experts l, l + 64, l + 128, l + 192, all in 64 bits.
+__device__ __forceinline__ void route_row(const RouteArgs& a, int64_t row) {
+    const compact_route_rule& rule = a.rule;
+    const int lane = threadIdx.x & 63, E = a.E, k = a.k;
     float l[4];
-    double s[4];
+    double s[4], c[4];
     uint64_t key[4];
     bool live[4];
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int e = lane + 64 * i;
-        l[i] = e < E ? logits[row * E + e] : -INFINITY;
+        l[i] = e < E ? a.logits[row * E + e] : -INFINITY;
         if (!(l[i] == l[i])) l[i] = -INFINITY;
         live[i] = l[i] > -INFINITY;
         top = fmaxf(top, l[i]);
@@ -58,12 +69,9 @@ __global__ __launch_bounds__(256) void route_kernel(const compact_route_rule rul
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int e = lane + 64 * i;
-        double c = s[i] + (bias && e < E ? (double)bias[e] : 0.0);
-        if (!(c == c)) c = -INFINITY;
-        live[i] = live[i] && c > -INFINITY;
-        key[i] = e < E ? key_of(live[i] ? c : -INFINITY, e) : 0;
-        // (the values of the groups come from the keys' own numbers: kept beside them)
-        l[i] = 0.f;
+        c[i] = a.by_logit ? (double)l[i] : s[i] + (a.bias && e < E ? (double)a.bias[e] : 0.0);
+        live[i] = live[i] && c[i] > -INFINITY;   // (no NaN is)
+        key[i] = e < E ? key_of(live[i] ? c[i] : -INFINITY, e) : 0;
     }
     if (rule.topk_groups < rule.n_groups) {
         const int S = E / rule.n_groups;
@@ -83,11 +91,11 @@ __global__ __launch_bounds__(256) void route_kernel(const compact_route_rule rul
                 below = best;
                 if (!best) break;
                 const int e = place_of(best);
-                double c = 0.0;
+                double v = 0.0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (e == lane + 64 * i) c = s[i] + (bias ? (double)bias[e] : 0.0);
-                total += __shfl(c, e & 63, 64);
+                    if (e == lane + 64 * i) v = c[i];
+                total += __shfl(v, e & 63, 64);
                 any = true;
             }
             if (lane == g) mine = key_of(any ? total : -INFINITY, g);
@@ -126,16 +134,238 @@ __global__ __launch_bounds__(256) void route_kernel(const compact_route_rule rul
         }
     }
     if (lane < k) {
-        idx[row * k + lane] = my_e;
+        a.idx[row * k + lane] = my_e;
         const double w = rule.renorm ? (sum > 0.0 ? my_s / sum : 0.0) : my_s;
-        weight[row * k + lane] = (float)(w * (double)rule.factor);
+        a.weight[row * k + lane] = (float)(w * (double)rule.factor);
     }
+}
+
+// ---- 16 lanes that have a row together: a DPP row -----------------------------------------------------------------------
+template <int N>
+__device__ __forceinline__ uint32_t ror16(uint32_t x) {   // from the lane N below, around
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, false);
+}
+template <int N>
+__device__ __forceinline__ float ror16(float x) {
+    return __uint_as_float(ror16<N>(__float_as_uint(x)));
+}
+template <int N>
+__device__ __forceinline__ uint32_t up16(uint32_t x) {    // from the lane N below, 0 beyond the first
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x110 + N, 0xf, 0xf, true);
+}
+__device__ __forceinline__ float max16(float x) {
+    x = fmaxf(x, ror16<8>(x));
+    x = fmaxf(x, ror16<4>(x));
+    x = fmaxf(x, ror16<2>(x));
+    return fmaxf(x, ror16<1>(x));
+}
+__device__ __forceinline__ float sum16(float x) {
+    x += ror16<8>(x);
+    x += ror16<4>(x);
+    x += ror16<2>(x);
+    return x + ror16<1>(x);
+}
+template <int N>
+__device__ __forceinline__ double ror16(double x) {
+    const uint64_t b = (uint64_t)__double_as_longlong(x);
+    return __longlong_as_double((long long)((uint64_t)ror16<N>((uint32_t)(b >> 32)) << 32 | ror16<N>((uint32_t)b)));
+}
+__device__ __forceinline__ double sum16(double x) {
+    x += ror16<8>(x);
+    x += ror16<4>(x);
+    x += ror16<2>(x);
+    return x + ror16<1>(x);
+}
+// how many of the 16 are larger
+template <int N = 1>
+__device__ __forceinline__ int larger16(float x) {
+    if constexpr (N == 16)
+        return 0;
+    else
+        return (ror16<N>(x) > x ? 1 : 0) + larger16<N + 1>(x);
+}
+template <int N = 1>
+__device__ __forceinline__ int larger16(uint32_t hi, uint32_t lo) {
+    if constexpr (N == 16) {
+        return 0;
+    } else {
+        const uint64_t other = (uint64_t)ror16<N>(hi) << 32 | ror16<N>(lo);
+        return (other > ((uint64_t)hi << 32 | lo) ? 1 : 0) + larger16<N + 1>(hi, lo);
+    }
+}
+
+// 16 lanes per row, four rows per wavefront; lane t of a row has experts t + 16 j.  In 32 bits the row's values tell which experts may be among the top_k:
+// those that reach T less twice the error of a value, T being the top_k-th largest of the lanes' two largest each.  They are
+// 8 or 9 of 256 as a rule; each goes to a lane of its own, is evaluated in 64 bits, and its place is the number of larger
+// ones.  A row goes to route_row() instead if it holds an infinity or NaN where that matters, if fewer than top_k experts are live, if more
+// than 16 pass, or if 32 bits do not tell the last chosen group from the first that is not.
+template <int V>
+__global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
+    extern __shared__ __attribute__((aligned(16))) float smem[];   // per row of the workgroup: 16 V values (with groups), 16 candidates
+    const compact_route_rule& rule = a.rule;
+    const int t = threadIdx.x & 15, at = threadIdx.x >> 4, E = a.E, k = a.k;
+    const bool grouped = rule.topk_groups < rule.n_groups;
+    uint8_t* list = reinterpret_cast<uint8_t*>(smem + (grouped ? (blockDim.x >> 4) * 16 * V : 0)) + at * 16;
+    float* vals = smem + at * 16 * V;
+    const int64_t row0 = ((int64_t)blockIdx.x * blockDim.x + (threadIdx.x & ~63)) >> 4;   // of the wavefront
+    if (row0 >= a.rows) return;
+    const int64_t mine = row0 + (at & 3), row = min(mine, a.rows - 1);
+    const float* lr = a.logits + row * E;
+    float v[V];
+    bool slow = false;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = t + 16 * j < E ? lr[t + 16 * j] : -INFINITY;
+    // (NaN and +inf, and NaN out of the bias, are route_row()'s)
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        slow |= !(v[j] < INFINITY);
+        top = fmaxf(top, v[j]);
+    }
+    double sum = 0.0;    // of the softmax, where values are scores
+    float sum32 = 0.f;   // where they are logits
+    if (rule.score == COMPACT_SCORE_SOFTMAX) {
+        top = max16(top);
+        if (!a.by_logit) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += v[j] > -INFINITY ? exp((double)v[j] - (double)top) : 0.0;
+            sum = sum16(sum);
+        } else if (!rule.renorm) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum32 += v[j] > -INFINITY ? __expf(v[j] - top) : 0.f;
+            sum32 = sum16(sum32);
+        }
+    }
+    if (!a.by_logit) {
+        const float scale = (float)(1.0 / sum);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (!(v[j] > -INFINITY)) continue;
+            const float sc = rule.score == COMPACT_SCORE_SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-v[j])) : __expf(v[j] - top) * scale;
+            v[j] = sc + (a.bias ? a.bias[t + 16 * j] : 0.f);
+            slow |= !(v[j] < INFINITY);
+        }
+    }
+    if (grouped) {
+        const int S = E / rule.n_groups;
+#pragma unroll
+        for (int j = 0; j < V; ++j) vals[t + 16 * j] = v[j];
+        __builtin_amdgcn_wave_barrier();
+        float m1 = -INFINITY, m2 = -INFINITY;   // lane g: the two largest of group g (at most 16 groups come here)
+        if (t < rule.n_groups)
+            for (int i = 0, o = t % S; i < S; ++i, o = o + 1 == S ? 0 : o + 1) {   // (each lane begins elsewhere: other banks)
+                const float x = vals[t * S + o];
+                m2 = fmaxf(m2, fminf(m1, x));
+                m1 = fmaxf(m1, x);
+            }
+        float g = m1;
+        if (rule.group_top == 2) {
+            g = m2 > -INFINITY ? m1 + m2 : -INFINITY;
+            slow |= m1 > -INFINITY && !(m2 > -INFINITY);   // (its only live expert counts alone)
+        }
+        const int above = larger16(g);   // (of all lanes: none of them may sleep)
+        const bool chosen = t < rule.n_groups && above < rule.topk_groups;
+        const uint32_t groups = (uint32_t)(__ballot(chosen) >> (at % 4 * 16)) & 0xffff;
+        const float least = -max16(chosen ? -g : -INFINITY), first_out = max16(t < rule.n_groups && !chosen ? g : -INFINITY);
+        // (equal ones at the border are all chosen, or none)
+        slow |= __popc(groups) != rule.topk_groups || !(least > -INFINITY) ||
+                (!a.by_logit && !(least - first_out > 0x1p-18f + fabsf(least) * 0x1p-20f));
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (!(groups >> ((t + 16 * j) * a.inv_size >> 16) & 1)) v[j] = -INFINITY;
+    }
+    // T
+    float m1 = -INFINITY, m2 = -INFINITY, T = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        m2 = fmaxf(m2, fminf(m1, v[j]));
+        m1 = fmaxf(m1, v[j]);
+    }
+    for (int i = 0; i < k; ++i) {
+        T = max16(m1);
+        if (m1 == T) {   // (equal ones go together: T ends lower, never too high)
+            m1 = m2;
+            m2 = -INFINITY;
+        }
+    }
+    slow |= !(T > -INFINITY);
+    // Twice the error of a value: a score has 2^-21, its sum with the bias 2^-24 of it.
+    if (!a.by_logit) T -= 0x1p-19f + fabsf(T) * 0x1p-21f;
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) n += v[j] >= T ? 1 : 0;
+    uint32_t before = n;
+    before += up16<1>(before);
+    before += up16<2>(before);
+    before += up16<4>(before);
+    before += up16<8>(before);
+    uint32_t total = n;
+    total += ror16<8>(total);
+    total += ror16<4>(total);
+    total += ror16<2>(total);
+    total += ror16<1>(total);
+    slow |= total > 16;
+    uint32_t pos = before - n;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (v[j] >= T && pos < 16) list[pos++] = (uint8_t)(t + 16 * j);
+    __builtin_amdgcn_wave_barrier();
+    // a candidate per lane
+    const bool have = (uint32_t)t < total;
+    const int e = have ? list[t] : 0;
+    const double l = lr[e];
+    double s, c = l;
+    if (rule.score == COMPACT_SCORE_SIGMOID)
+        s = 1.0 / (1.0 + exp(-l));
+    else
+        s = exp(l - (double)top) / (!a.by_logit ? sum : rule.renorm ? 1.0 : (double)sum32);
+    if (!a.by_logit) c = s + (a.bias ? (double)a.bias[e] : 0.0);
+    const uint64_t key = have ? key_of(c, e) : 0;
+    const int rank = larger16((uint32_t)(key >> 32), (uint32_t)key);
+    const bool chosen = have && rank < k;
+    const double all = sum16(chosen ? s : 0.0);
+    const uint64_t passed = __ballot(slow);
+    const bool row_slow = (passed >> (at % 4 * 16) & 0xffff) != 0;
+    if (chosen && mine < a.rows && !row_slow) {
+        a.idx[row * k + rank] = e;
+        a.weight[row * k + rank] = (float)((rule.renorm ? (all > 0.0 ? s / all : 0.0) : s) * (double)rule.factor);
+    }
+    if (passed)
+        for (int i = 0; i < 4; ++i)
+            if ((passed >> (16 * i) & 0xffff) && row0 + i < a.rows) route_row(a, row0 + i);
+}
+
+// more than 16 groups
+__global__ __launch_bounds__(256) void route_rows_kernel(const RouteArgs a) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (row < a.rows) route_row(a, row);
+}
+
+template <int V>
+static void run_route(const RouteArgs& a, hipStream_t s) {
+    // few rows: a wavefront per workgroup, over as many compute units
+    const int threads = a.rows <= 4096 ? 64 : 256, per = threads / 16;
+    const size_t smem = (size_t)per * ((a.rule.topk_groups < a.rule.n_groups ? 16 * V * 4 : 0) + 16);
+    route_kernel<V><<<(unsigned)((a.rows + per - 1) / per), threads, smem, s>>>(a);
 }
 
 int launch_route(compact_ctx* ctx, const compact_route_rule& rule, const float* logits, const float* bias, int64_t rows, int32_t* idx,
                  float* weight, hipStream_t s) {
     if (rows == 0) return COMPACT_OK;
-    route_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(rule, logits, bias, rows, ctx->cfg.n_experts, ctx->cfg.top_k, idx, weight);
+    const int E = ctx->cfg.n_experts, size = E / rule.n_groups;
+    const RouteArgs a{rule, logits, bias, rows, E, ctx->cfg.top_k, !bias && (rule.topk_groups == rule.n_groups || rule.group_top == 1), (65536 + size - 1) / size, idx, weight};
+    if (rule.n_groups > 16 && rule.topk_groups < rule.n_groups)
+        route_rows_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a);
+    else if (E <= 16)
+        run_route<1>(a, s);
+    else if (E <= 32)
+        run_route<2>(a, s);
+    else if (E <= 64)
+        run_route<4>(a, s);
+    else if (E <= 128)
+        run_route<8>(a, s);
+    else
+        run_route<16>(a, s);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;
 }
