@@ -29,6 +29,7 @@ struct RouteArgs {
     int E, k;
     int by_logit;
     int inv_size;   // 65536 / experts of a group, rounded up: e / size = e * inv_size >> 16 for e < 256
+    int lanes;      // of the 16, that share a group in the quick way to rank groups; 0: the general one
     int32_t* idx;
     float* weight;
 };
@@ -194,6 +195,15 @@ __device__ __forceinline__ int larger16(uint32_t hi, uint32_t lo) {
     }
 }
 
+// the two largest of a lane's two and those of the lane that CTRL names
+template <int CTRL>
+__device__ __forceinline__ void join_two(float& m1, float& m2) {
+    const float o1 = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m1), CTRL, 0xf, 0xf, false));
+    const float o2 = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m2), CTRL, 0xf, 0xf, false));
+    m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
+    m1 = fmaxf(m1, o1);
+}
+
 // 16 lanes per row, four rows per wavefront; lane t of a row has experts t + 16 j.  In 32 bits the row's values tell which experts may be among the top_k:
 // those that reach T less twice the error of a value, T being the top_k-th largest of the lanes' two largest each.  They are
 // 8 or 9 of 256 as a rule; each goes to a lane of its own, is evaluated in 64 bits, and its place is the number of larger
@@ -216,12 +226,13 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = t + 16 * j < E ? lr[t + 16 * j] : -INFINITY;
     // (NaN and +inf, and NaN out of the bias, are route_row()'s)
-    float top = -INFINITY;
+    float top = -INFINITY, all_v = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        slow |= !(v[j] < INFINITY);
+        all_v += v[j];
         top = fmaxf(top, v[j]);
     }
+    slow |= !(all_v < INFINITY);   // (a sum that overflows goes there too)
     double sum = 0.0;    // of the softmax, where values are scores
     float sum32 = 0.f;   // where they are logits
     if (rule.score == COMPACT_SCORE_SOFTMAX) {
@@ -238,41 +249,63 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
     }
     if (!a.by_logit) {
         const float scale = (float)(1.0 / sum);
+        all_v = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if (!(v[j] > -INFINITY)) continue;
-            const float sc = rule.score == COMPACT_SCORE_SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-v[j])) : __expf(v[j] - top) * scale;
-            v[j] = sc + (a.bias ? a.bias[t + 16 * j] : 0.f);
-            slow |= !(v[j] < INFINITY);
+            float sc = rule.score == COMPACT_SCORE_SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-v[j])) : __expf(v[j] - top) * scale;
+            if (a.bias) sc += t + 16 * j < E ? a.bias[t + 16 * j] : 0.f;
+            v[j] = v[j] > -INFINITY ? sc : -INFINITY;
+            all_v += v[j];
         }
+        slow |= !(all_v < INFINITY);
     }
     if (grouped) {
-        const int S = E / rule.n_groups;
 #pragma unroll
         for (int j = 0; j < V; ++j) vals[t + 16 * j] = v[j];
         __builtin_amdgcn_wave_barrier();
-        float m1 = -INFINITY, m2 = -INFINITY;   // lane g: the two largest of group g (at most 16 groups come here)
-        if (t < rule.n_groups)
-            for (int i = 0, o = t % S; i < S; ++i, o = o + 1 == S ? 0 : o + 1) {   // (each lane begins elsewhere: other banks)
-                const float x = vals[t * S + o];
+        float m1 = -INFINITY, m2 = -INFINITY;   // the two largest
+        const int share = a.lanes ? a.lanes : 1;
+        if (a.lanes) {   // V neighbours a lane, then the lanes of a group
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float x = vals[t * V + j];
                 m2 = fmaxf(m2, fminf(m1, x));
                 m1 = fmaxf(m1, x);
             }
+            if (a.lanes > 1) join_two<0xb1>(m1, m2);    // lane ^ 1
+            if (a.lanes > 2) join_two<0x4e>(m1, m2);    // lane ^ 2
+            if (a.lanes > 4) join_two<0x141>(m1, m2);   // 7 - lane of 8
+        } else {         // lane g: group g
+            const int S = E / rule.n_groups;
+            if (t < rule.n_groups)
+                for (int i = 0, o = t % S; i < S; ++i, o = o + 1 == S ? 0 : o + 1) {   // (each lane begins elsewhere: other banks)
+                    const float x = vals[t * S + o];
+                    m2 = fmaxf(m2, fminf(m1, x));
+                    m1 = fmaxf(m1, x);
+                }
+        }
         float g = m1;
         if (rule.group_top == 2) {
             g = m2 > -INFINITY ? m1 + m2 : -INFINITY;
             slow |= m1 > -INFINITY && !(m2 > -INFINITY);   // (its only live expert counts alone)
         }
         const int above = larger16(g);   // (of all lanes: none of them may sleep)
-        const bool chosen = t < rule.n_groups && above < rule.topk_groups;
+        const bool here_is_one = t < rule.n_groups * share, chosen = here_is_one && above < rule.topk_groups * share;
         const uint32_t groups = (uint32_t)(__ballot(chosen) >> (at % 4 * 16)) & 0xffff;
-        const float least = -max16(chosen ? -g : -INFINITY), first_out = max16(t < rule.n_groups && !chosen ? g : -INFINITY);
+        const float least = -max16(chosen ? -g : -INFINITY), first_out = max16(here_is_one && !chosen ? g : -INFINITY);
         // (equal ones at the border are all chosen, or none)
-        slow |= __popc(groups) != rule.topk_groups || !(least > -INFINITY) ||
+        slow |= __popc(groups) != rule.topk_groups * share || !(least > -INFINITY) ||
                 (!a.by_logit && !(least - first_out > 0x1p-18f + fabsf(least) * 0x1p-20f));
+        if (a.lanes) {   // expert t + 16 j was lane (t + 16 j) / V's
+            const uint32_t mine_first = groups >> (t / V);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (!(groups >> ((t + 16 * j) * a.inv_size >> 16) & 1)) v[j] = -INFINITY;
+            for (int j = 0; j < V; ++j)
+                if (!(mine_first >> (j * (16 / V)) & 1)) v[j] = -INFINITY;
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (!(groups >> ((t + 16 * j) * a.inv_size >> 16) & 1)) v[j] = -INFINITY;
+        }
     }
     // T
     float m1 = -INFINITY, m2 = -INFINITY, T = 0.f;
@@ -291,9 +324,10 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
     slow |= !(T > -INFINITY);
     // Twice the error of a value: a score has 2^-21, its sum with the bias 2^-24 of it.
     if (!a.by_logit) T -= 0x1p-19f + fabsf(T) * 0x1p-21f;
-    uint32_t n = 0;
+    uint32_t found = 0;   // bit j: expert t + 16 j is a candidate
 #pragma unroll
-    for (int j = 0; j < V; ++j) n += v[j] >= T ? 1 : 0;
+    for (int j = 0; j < V; ++j) found |= v[j] >= T ? 1u << j : 0;
+    const uint32_t n = __popc(found);
     uint32_t before = n;
     before += up16<1>(before);
     before += up16<2>(before);
@@ -305,10 +339,7 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
     total += ror16<2>(total);
     total += ror16<1>(total);
     slow |= total > 16;
-    uint32_t pos = before - n;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (v[j] >= T && pos < 16) list[pos++] = (uint8_t)(t + 16 * j);
+    for (uint32_t pos = before - n; found && pos < 16; ++pos, found &= found - 1) list[pos] = (uint8_t)(t + 16 * (__ffs(found) - 1));
     __builtin_amdgcn_wave_barrier();
     // a candidate per lane
     const bool have = (uint32_t)t < total;
@@ -353,7 +384,10 @@ int launch_route(compact_ctx* ctx, const compact_route_rule& rule, const float* 
                  float* weight, hipStream_t s) {
     if (rows == 0) return COMPACT_OK;
     const int E = ctx->cfg.n_experts, size = E / rule.n_groups;
-    const RouteArgs a{rule, logits, bias, rows, E, ctx->cfg.top_k, !bias && (rule.topk_groups == rule.n_groups || rule.group_top == 1), (65536 + size - 1) / size, idx, weight};
+    // the quick way: the experts fill the 16 lanes, and a group is 1, 2, 4 or 8 whole lanes
+    const int values = E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <= 128 ? 8 : 16;
+    const int lanes = E == 16 * values && size % values == 0 && rule.n_groups > 1 && 16 % rule.n_groups == 0 ? 16 / rule.n_groups : 0;
+    const RouteArgs a{rule, logits, bias, rows, E, ctx->cfg.top_k, !bias && (rule.topk_groups == rule.n_groups || rule.group_top == 1), (65536 + size - 1) / size, lanes, idx, weight};
     if (rule.n_groups > 16 && rule.topk_groups < rule.n_groups)
         route_rows_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a);
     else if (E <= 16)

@@ -310,7 +310,8 @@ def check_route(lay, rule, logits, bias, share=0.999):
 
 RULES = [dict(score="softmax"), dict(score="softmax", renorm=False, factor=1.5), dict(score="sigmoid"), dict(score="sigmoid", renorm=False, factor=2.5),
          dict(score="sigmoid", n_groups=8, topk_groups=4, group_top=2), dict(score="softmax", n_groups=4, topk_groups=2, group_top=1),
-         dict(score="sigmoid", n_groups=2, topk_groups=1, group_top=2, factor=0.1), dict(score="softmax", n_groups=8, topk_groups=8, group_top=2)]
+         dict(score="sigmoid", n_groups=2, topk_groups=1, group_top=2, factor=0.1), dict(score="softmax", n_groups=8, topk_groups=8, group_top=2),
+         dict(score="sigmoid", n_groups=16, topk_groups=8, group_top=2), dict(score="softmax", n_groups=16, topk_groups=5, group_top=1)]
 
 
 @pytest.mark.parametrize("E,k", [(8, 1), (16, 2), (64, 6), (128, 4), (160, 8), (232, 5), (256, 8)])
