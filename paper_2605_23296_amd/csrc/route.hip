@@ -160,6 +160,17 @@ __device__ __forceinline__ float max16(float x) {
     x = fmaxf(x, ror16<2>(x));
     return fmaxf(x, ror16<1>(x));
 }
+__device__ __forceinline__ int max16(int x) {
+    x = max(x, (int)ror16<8>((uint32_t)x));
+    x = max(x, (int)ror16<4>((uint32_t)x));
+    x = max(x, (int)ror16<2>((uint32_t)x));
+    return max(x, (int)ror16<1>((uint32_t)x));
+}
+// a whole number that is the larger the larger x is (and x again from it)
+__device__ __forceinline__ int ordered(float x) {
+    const int i = __float_as_int(x);
+    return i ^ (i >> 31 & 0x7fffffff);
+}
 __device__ __forceinline__ float sum16(float x) {
     x += ror16<8>(x);
     x += ror16<4>(x);
@@ -223,8 +234,21 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
     const float* lr = a.logits + row * E;
     float v[V];
     bool slow = false;
+    // (a lane's place in a row is one address for all of its experts)
+    const bool full = E == 16 * V;
+    auto load = [&](const float* p, float (&x)[V], float none) __attribute__((always_inline)) {
+        if (full) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = t + 16 * j < E ? lr[t + 16 * j] : -INFINITY;
+            for (int j = 0; j < V; ++j) x[j] = p[t + 16 * j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float y = p[min(t + 16 * j, E - 1)];
+                x[j] = t + 16 * j < E ? y : none;
+            }
+        }
+    };
+    load(lr, v, -INFINITY);
     // (NaN and +inf, and NaN out of the bias, are route_row()'s)
     float top = -INFINITY, all_v = 0.f;
 #pragma unroll
@@ -249,11 +273,13 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
     }
     if (!a.by_logit) {
         const float scale = (float)(1.0 / sum);
+        float b[V];
+        if (a.bias) load(a.bias, b, 0.f);
         all_v = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             float sc = rule.score == COMPACT_SCORE_SIGMOID ? __builtin_amdgcn_rcpf(1.0f + __expf(-v[j])) : __expf(v[j] - top) * scale;
-            if (a.bias) sc += t + 16 * j < E ? a.bias[t + 16 * j] : 0.f;
+            if (a.bias) sc += b[j];
             v[j] = v[j] > -INFINITY ? sc : -INFINITY;
             all_v += v[j];
         }
@@ -314,12 +340,15 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
         m2 = fmaxf(m2, fminf(m1, v[j]));
         m1 = fmaxf(m1, v[j]);
     }
-    for (int i = 0; i < k; ++i) {
-        T = max16(m1);
-        if (m1 == T) {   // (equal ones go together: T ends lower, never too high)
-            m1 = m2;
-            m2 = -INFINITY;
+    {   // (as whole numbers in the same order: their maximum takes its other operand from another lane by itself)
+        int i1 = ordered(m1), i2 = ordered(m2), top_i = 0;
+        for (int i = 0; i < k; ++i) {
+            top_i = max16(i1);
+            const bool it = i1 == top_i;   // (equal ones go together: T ends lower, never too high)
+            i1 = it ? i2 : i1;
+            i2 = it ? ordered(-INFINITY) : i2;
         }
+        T = __int_as_float(top_i ^ (top_i >> 31 & 0x7fffffff));
     }
     slow |= !(T > -INFINITY);
     // Twice the error of a value: a score has 2^-21, its sum with the bias 2^-24 of it.
