@@ -359,7 +359,7 @@ class Layer:
             setattr(self.w, name, t.data_ptr() if t is not None else None)
         self.ws = None
         self.torch_dtype = torch.bfloat16 if layer.dtype == "bf16" else torch.float32
-        self.kv_heads = (layer.n_kv_heads, layer.head_dim)
+        self.kv_heads, self.d_model, self.experts = (layer.n_kv_heads, layer.head_dim), layer.d_model, (layer.n_experts, layer.top_k)
         self.q_cols, self.qkv_cols = layer.n_q_heads * layer.head_dim, (layer.n_q_heads + 2 * layer.n_kv_heads) * layer.head_dim
 
     def close(self):
@@ -623,51 +623,57 @@ class Layer:
     def compact_block_norm(self, x, b=None, g_post=None, gate=None, alpha=1.0, h=None, g_pre=None, n=None, q=None, q_scale=None):
         """Rows [rows, d_model]; h, n, q (int8) and q_scale (fp32 [rows]) are written where given.  gate: [d_model], or [rows, d_model] whose rows
         may be apart."""
-        device, dt, shape, d = torch.cuda.current_device(), self.torch_dtype, x.shape, self.layer.d_model
-        if len(shape) != 2 or shape[1] != d:
-            _refuse("rows: %s, [rows, %d] needed" % (tuple(shape), d))
-        rows, ptr, gate_stride = shape[0], [], 0
-        for t in (x, b, h, n):
-            if t is None:
-                ptr.append(None)
-                continue
-            if t.dtype is not dt or t.shape != shape or t.get_device() != device or not t.is_contiguous():
-                _refuse("rows: %s %s on %s; contiguous %s of %s on the current GPU needed" % (t.dtype, tuple(t.shape), t.device, dt, tuple(shape)))
-            ptr.append(t.data_ptr())
-        for t in (g_post, g_pre):
-            ptr.append(None if t is None else _array(t, dt, d, device, "gain"))
-        if gate is None:
-            ptr.append(None)
-        else:
-            if gate.dtype is not dt or gate.get_device() != device or gate.shape != shape and tuple(gate.shape) != (d,) or gate.stride(-1) != 1:
-                _refuse("gate: %s %s with strides %s on %s; [%d] or %s of %s on the current GPU needed"
-                        % (gate.dtype, tuple(gate.shape), gate.stride(), gate.device, d, tuple(shape), dt))
-            gate_stride = 0 if gate.dim() == 1 or rows <= 1 else gate.stride(0)
-            ptr.append(gate.data_ptr())
-        if q is not None and q.shape != shape:
-            _refuse("codes: %s, %s needed" % (tuple(q.shape), tuple(shape)))
-        rc = self.L.compact_block_norm(self.ctx, ptr[0], ptr[1], ptr[4], ptr[6], gate_stride, alpha, ptr[2], ptr[5], ptr[3],
-                                       None if q is None else _array(q, torch.int8, rows * d, device, "codes"),
-                                       None if q_scale is None else _array(q_scale, torch.float32, rows, device, "scale"), rows, _raw_stream(device))
+        device, dt, shape, d = torch.cuda.current_device(), self.torch_dtype, x.shape, self.d_model
+        rows = shape[0] if len(shape) == 2 else -1
+        gate_stride = 0 if gate is None or rows <= 1 or gate.dim() == 1 else gate.stride(0)
+        if (rows < 0 or shape[1] != d or x.dtype is not dt or x.get_device() != device or not x.is_contiguous()
+                or b is not None and (b.dtype is not dt or b.shape != shape or b.get_device() != device or not b.is_contiguous())
+                or h is not None and (h.dtype is not dt or h.shape != shape or h.get_device() != device or not h.is_contiguous())
+                or n is not None and (n.dtype is not dt or n.shape != shape or n.get_device() != device or not n.is_contiguous())
+                or g_post is not None and (g_post.dtype is not dt or g_post.numel() < d or g_post.get_device() != device or not g_post.is_contiguous())
+                or g_pre is not None and (g_pre.dtype is not dt or g_pre.numel() < d or g_pre.get_device() != device or not g_pre.is_contiguous())
+                or gate is not None and (gate.dtype is not dt or gate.get_device() != device or gate.shape != shape and tuple(gate.shape) != (d,)
+                                         or gate.stride(-1) != 1)
+                or q is not None and (q.dtype is not torch.int8 or q.shape != shape or q.get_device() != device or not q.is_contiguous())
+                or q_scale is not None and (q_scale.dtype is not torch.float32 or q_scale.numel() < rows or q_scale.get_device() != device
+                                            or not q_scale.is_contiguous())):
+            if rows < 0 or shape[1] != d:
+                _refuse("rows: %s, [rows, %d] needed" % (tuple(shape), d))
+            for name, t, dtype, size in (("x", x, dt, rows * d), ("b", b, dt, rows * d), ("h", h, dt, rows * d), ("n", n, dt, rows * d), ("g_post", g_post, dt, d),
+                                         ("g_pre", g_pre, dt, d), ("codes", q, torch.int8, rows * d), ("scale", q_scale, torch.float32, rows)):
+                if t is not None:
+                    _array(t, dtype, size, device, name)
+            _refuse("rows %s: gate %s, b, h, n and codes %s; gate of %s [%d] or rows of it, the others of the rows' shape needed"
+                    % (tuple(shape), None if gate is None else (gate.dtype, tuple(gate.shape), gate.stride()),
+                       [None if t is None else tuple(t.shape) for t in (b, h, n, q)], dt, d))
+        rc = self.L.compact_block_norm(self.ctx, x.data_ptr(), None if b is None else b.data_ptr(), None if g_post is None else g_post.data_ptr(),
+                                       None if gate is None else gate.data_ptr(), gate_stride, alpha, None if h is None else h.data_ptr(),
+                                       None if g_pre is None else g_pre.data_ptr(), None if n is None else n.data_ptr(),
+                                       None if q is None else q.data_ptr(), None if q_scale is None else q_scale.data_ptr(), rows, _raw_stream(device))
         if rc:
             self.check(rc)
 
     def compact_route(self, rule, logits, bias, idx, weight, m=None, w_router=None):
         """logits fp32 [rows, n_experts], given, or written as m w_router^T where these are; bias fp32 [n_experts] or None; idx int32 and weight fp32
         [rows, top_k]."""
-        device, E, k, shape = torch.cuda.current_device(), self.layer.n_experts, self.layer.top_k, logits.shape
-        if len(shape) != 2 or shape[1] != E:
-            _refuse("logits: %s, [rows, %d] needed" % (tuple(shape), E))
-        rows = shape[0]
-        if m is not None and m.shape != (rows, self.layer.d_model) or w_router is not None and w_router.shape != (E, self.layer.d_model):
-            _refuse("router: rows %s, weights %s; %s and %s needed" % (None if m is None else tuple(m.shape), None if w_router is None else tuple(w_router.shape),
-                                                                      (rows, self.layer.d_model), (E, self.layer.d_model)))
+        device, (E, k), shape, f32 = torch.cuda.current_device(), self.experts, logits.shape, torch.float32
+        rows = shape[0] if len(shape) == 2 else -1
+        if (rows < 0 or shape[1] != E or logits.dtype is not f32 or logits.get_device() != device or not logits.is_contiguous()
+                or bias is not None and (bias.dtype is not f32 or bias.numel() < E or bias.get_device() != device or not bias.is_contiguous())
+                or idx.dtype is not torch.int32 or idx.numel() < rows * k or idx.get_device() != device or not idx.is_contiguous()
+                or weight.dtype is not f32 or weight.numel() < rows * k or weight.get_device() != device or not weight.is_contiguous()
+                or m is not None and m.shape != (rows, self.d_model) or w_router is not None and w_router.shape != (E, self.d_model)):
+            if rows >= 0 and shape[1] == E:
+                _array(logits, f32, 0, device, "logits")
+                _array(idx, torch.int32, rows * k, device, "idx")
+                _array(weight, f32, rows * k, device, "weight")
+                if bias is not None:
+                    _array(bias, f32, E, device, "bias")
+            _refuse("router: logits %s, rows %s, weights %s; [rows, %d], [rows, %d] and [%d, %d] needed"
+                    % (tuple(shape), None if m is None else tuple(m.shape), None if w_router is None else tuple(w_router.shape), E, self.d_model, E, self.d_model))
         rc = self.L.compact_route(self.ctx, rule.ref, None if m is None else _array(m, self.torch_dtype, 0, device, "rows"),
-                                  None if w_router is None else _array(w_router, self.torch_dtype, 0, device, "router weights"),
-                                  _array(logits, torch.float32, 0, device, "logits"),
-                                  None if bias is None else _array(bias, torch.float32, E, device, "bias"), rows,
-                                  _array(idx, torch.int32, rows * k, device, "idx"), _array(weight, torch.float32, rows * k, device, "weight"),
-                                  _raw_stream(device))
+                                  None if w_router is None else _array(w_router, self.torch_dtype, 0, device, "router weights"), logits.data_ptr(),
+                                  None if bias is None else bias.data_ptr(), rows, idx.data_ptr(), weight.data_ptr(), _raw_stream(device))
         if rc:
             self.check(rc)
 
