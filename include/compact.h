@@ -398,7 +398,7 @@ int compact_quant_i8(compact_ctx* ctx, const void* d_x, int64_t x_stride, int64_
 
 /* C[m, n] = a_scale[m] b_scale[n] sum_k A[m, k] B[n, k] (+ R[m, n] if d_r != NULL): codes A int8 [M, K], B int8 [N, K] (any int8 value,
  * -128 among them), the sum in 32-bit integers, C and R in the storage type.  Epilogue 1 treats B as [2N, K] (b_scale [2N]) stacked gate/up and stores
- * silu(gate) * up.  d_r may be d_c.  K a multiple of 16, at most 131056; d_a and d_b 16-byte aligned, any M and N.  With a
+ * silu(gate) * up.  The sum is scaled in fp32, by a_scale first.  d_r may be d_c.  K a multiple of 16, at most 131056; d_a and d_b 16-byte aligned, any M and N.  With a
  * workspace of compact_gemm_i8_workspace_bytes few rows are faster; a smaller one, or none, changes no bit. */
 int compact_gemm_i8_workspace_bytes(const compact_ctx* ctx, int64_t M, int32_t N, int32_t K, int32_t epilogue, size_t* bytes);
 int compact_gemm_i8(compact_ctx* ctx, const void* d_a, const float* d_a_scale, const void* d_b, const float* d_b_scale, const void* d_r,
@@ -409,7 +409,7 @@ int compact_gemm_i8(compact_ctx* ctx, const void* d_a, const float* d_a_scale, c
  *   h = T(x + alpha * gate * p),  p = RMSNorm(b; g_post), or b itself if d_g_post is NULL;   h = x if d_b is NULL
  *   n = T(RMSNorm(h; g_pre)), and the codes of n.
  * d_b: the block's output rows; d_gate (nullable = 1): one row for all (gate_stride 0) or a row each (gate_stride >= d_model,
- * a multiple of 8); d_h, d_n, and the pair d_q (int8) / d_q_scale: each NULL where it is not wanted, one at least is.  d_g_pre is needed for d_n
+ * a multiple of 8); d_h, d_n (not one array), and the pair d_q (int8) / d_q_scale: each NULL where it is not wanted, one at least is.  d_g_pre is needed for d_n
  * and d_q, d_b for d_h.  d_h and d_n may be d_x or d_b themselves (in place).  Arithmetic is fp32; n comes from the rounded h, as if
  * the two norms were calls of their own.  Row arrays and gains 16-byte aligned (d_q 8). */
 int compact_block_norm(compact_ctx* ctx, const void* d_x, const void* d_b, const void* d_g_post, const void* d_gate, int64_t gate_stride,
@@ -435,7 +435,7 @@ typedef struct compact_route_rule {
 } compact_route_rule;
 /* d_logits [rows, n_experts] fp32: given, or, where d_m [rows, d_model] and d_w_router [n_experts, d_model] (storage type) are,
  * written as their product in fp32 (by the kernel that compact_moe_route uses, with its bits).  d_bias [n_experts] fp32 or NULL.
- * d_expert_idx, d_weight [rows, top_k]. */
+ * d_expert_idx, d_weight [rows, top_k].  d_m, d_w_router and the d_logits that they give are 16-byte aligned. */
 int compact_route(compact_ctx* ctx, const compact_route_rule* rule, const void* d_m, const void* d_w_router, float* d_logits,
                   const float* d_bias, int64_t rows, int32_t* d_expert_idx, float* d_weight, void* hip_stream);
 

@@ -4,7 +4,7 @@
 #include "common.h"
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-#define MAX_ROWS 0x7fffffffll   // a workgroup per row
+#define MAX_ROWS 0x7fffffffll
 
 extern "C" int compact_quant_i8(compact_ctx* ctx, const void* d_x, int64_t x_stride, int64_t rows, int32_t cols, void* d_q,
                                 float* d_scale, void* hip_stream) {
@@ -72,6 +72,7 @@ extern "C" int compact_block_norm(compact_ctx* ctx, const void* d_x, const void*
     if ((d_q == nullptr) != (d_q_scale == nullptr)) return set_err(ctx, COMPACT_EINVAL, "codes and their scales belong together");
     if ((d_n || d_q) && !d_g_pre) return set_err(ctx, COMPACT_EINVAL, "normalised rows need the gain g_pre");
     if (!d_b && (d_h || d_g_post || d_gate)) return set_err(ctx, COMPACT_EINVAL, "h, g_post and gate need the block's output b");
+    if (d_h && d_h == d_n) return set_err(ctx, COMPACT_EINVAL, "h and n are one array");
     if (rows > 0 && !d_x) return set_err(ctx, COMPACT_EINVAL, "null rows");
     if (d_gate && gate_stride != 0 && (gate_stride < ctx->cfg.d_model || gate_stride % 8 != 0))
         return set_err(ctx, COMPACT_EINVAL, "gate_stride must be 0, or a multiple of 8 that is d_model at least");
@@ -102,6 +103,8 @@ extern "C" int compact_route(compact_ctx* ctx, const compact_route_rule* rule, c
     if (!d_logits || !d_expert_idx || !d_weight) return set_err(ctx, COMPACT_EINVAL, "null pointer");
     hipStream_t s = (hipStream_t)hip_stream;
     if (d_m) {
+        for (const void* p : {d_m, d_w_router, (const void*)d_logits})
+            if (!aligned(p, 16)) return set_err(ctx, COMPACT_EINVAL, "rows, router weights and the logits that they give must be 16-byte aligned");
         if (c.dtype == COMPACT_BF16)
             TRY(launch_gemm_bf16(ctx, (const bf16*)d_m, (const bf16*)d_w_router, nullptr, false, (bf16*)d_logits, rows, c.n_experts,
                                  c.d_model, 2, nullptr, s));

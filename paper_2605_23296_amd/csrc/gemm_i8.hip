@@ -304,7 +304,7 @@ static int launch_tile(compact_ctx* ctx, GemmI8Params& p, hipStream_t s, int sli
     TRY(allow_lds(ctx, (const void*)gemm_i8_tile_kernel<BM, BN, WM, WN, S, GLU, GROUPED>, smem, lds_set));
     const int64_t tiles = (int64_t)p.n_mtiles * p.n_ntiles;
     if (tiles == 0) return COMPACT_OK;
-    if (tiles > 0x7fffffff) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
+    if (tiles * WM * WN * 64 > MAX_GRID_THREADS) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
     gemm_i8_tile_kernel<BM, BN, WM, WN, S, GLU, GROUPED><<<dim3((unsigned)tiles, (unsigned)slices), WM * WN * 64, smem, s>>>(p);
     LAUNCH_CHECK(ctx);
     if (slices > 1) {
@@ -621,12 +621,12 @@ static int launch_large_k(compact_ctx* ctx, GemmI8Params& p, int64_t n_full, hip
         wgs = (int64_t)p.n_mtiles * p.n_ntiles;
     } else {
         const LargeTiles lt = large_tiles(p.M, p.n_ntiles);
-        if (lt.slots > 0x3fffffff) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
         p.n_mtiles = (int)(lt.slots / p.n_ntiles);
         p.n_full = (int)std::min(n_full, lt.slots);
         wgs = p.n_full + 2 * (lt.slots - p.n_full) + lt.bottom;
     }
     if (wgs == 0) return COMPACT_OK;
+    if (wgs * 512 > MAX_GRID_THREADS) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
     gemm_i8_kernel<GLU, GROUPED, CUT><<<dim3((unsigned)wgs), 512, smem, s>>>(p);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;

@@ -175,7 +175,7 @@ static int launch_stream_form(compact_ctx* ctx, const GemmI8Params& p, hipStream
     TRY(allow_lds(ctx, (const void*)stream_i8_kernel<W, T, XI, GLU, GROUPED>, smem, lds_set));
     const int64_t wgs = (int64_t)((n_tiles + T - 1) / T) * (GROUPED ? p.n_mtiles : 1);
     if (wgs == 0) return COMPACT_OK;
-    if (wgs > 0x7fffffff) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
+    if (wgs * W * 64 > MAX_GRID_THREADS) return set_err(ctx, COMPACT_ESHAPE, "too many output tiles");
     stream_i8_kernel<W, T, XI, GLU, GROUPED><<<(unsigned)wgs, W * 64, smem, s>>>(p);
     LAUNCH_CHECK(ctx);
     return COMPACT_OK;

@@ -1,4 +1,7 @@
 // Rows as 8-bit codes, and the norms around a block whose rows leave as codes.
+#include <algorithm>
+#include <type_traits>
+
 #include "common.h"
 #include "int8_codes.h"
 #include "vecio.h"
@@ -149,13 +152,19 @@ static void quant_rows(const T* x, int64_t x_stride, int64_t rows, int cols, int
         run_quant<T, 1024, 8>(x, x_stride, rows, cols, q, scale, s);
 }
 
+// rows of a launch at most (of up to 1024 threads each)
+#define ROWS_PER_LAUNCH (1ll << 21)
+static_assert(ROWS_PER_LAUNCH * 1024 <= MAX_GRID_THREADS, "one launch");
+
 int launch_quant_i8(compact_ctx* ctx, const void* x, int64_t x_stride, int64_t rows, int cols, int8_t* q, float* scale, hipStream_t s) {
-    if (rows == 0) return COMPACT_OK;
-    if (ctx->cfg.dtype == COMPACT_BF16)
-        quant_rows((const bf16*)x, x_stride, rows, cols, q, scale, s);
-    else
-        quant_rows((const float*)x, x_stride, rows, cols, q, scale, s);
-    LAUNCH_CHECK(ctx);
+    for (int64_t r = 0; r < rows; r += ROWS_PER_LAUNCH) {
+        const int64_t n = std::min<int64_t>(rows - r, ROWS_PER_LAUNCH);
+        if (ctx->cfg.dtype == COMPACT_BF16)
+            quant_rows((const bf16*)x + r * x_stride, x_stride, n, cols, q + r * cols, scale + r, s);
+        else
+            quant_rows((const float*)x + r * x_stride, x_stride, n, cols, q + r * cols, scale + r, s);
+        LAUNCH_CHECK(ctx);
+    }
     return COMPACT_OK;
 }
 
@@ -253,12 +262,21 @@ static void run_block_norm(const BlockNormArgs& a, int d, float eps, hipStream_t
         default: block_norm_kernel<T, 4><<<rows, NT, 0, s>>>(a, d, eps); break;
     }
 }
-int launch_block_norm(compact_ctx* ctx, const BlockNormArgs& a, hipStream_t s) {
-    if (a.rows == 0) return COMPACT_OK;
-    if (ctx->cfg.dtype == COMPACT_BF16)
-        run_block_norm<bf16>(a, ctx->cfg.d_model, ctx->cfg.rms_eps, s);
-    else
-        run_block_norm<float>(a, ctx->cfg.d_model, ctx->cfg.rms_eps, s);
-    LAUNCH_CHECK(ctx);
+int launch_block_norm(compact_ctx* ctx, const BlockNormArgs& all, hipStream_t s) {
+    const int d = ctx->cfg.d_model;
+    const size_t es = dtype_size(ctx->cfg.dtype);
+    for (int64_t r = 0; r < all.rows; r += ROWS_PER_LAUNCH) {
+        BlockNormArgs a = all;
+        a.rows = std::min<int64_t>(all.rows - r, ROWS_PER_LAUNCH);
+        auto from = [&](auto*& p, int64_t stride, size_t size) {
+            if (p) p = reinterpret_cast<std::decay_t<decltype(p)>>((char*)p + r * stride * size);
+        };
+        from(a.x, d, es), from(a.b, d, es), from(a.gate, a.gate_stride, es), from(a.h, d, es), from(a.n, d, es), from(a.q, d, 1), from(a.q_scale, 1, 4);
+        if (ctx->cfg.dtype == COMPACT_BF16)
+            run_block_norm<bf16>(a, d, ctx->cfg.rms_eps, s);
+        else
+            run_block_norm<float>(a, d, ctx->cfg.rms_eps, s);
+        LAUNCH_CHECK(ctx);
+    }
     return COMPACT_OK;
 }

@@ -411,6 +411,14 @@ static void run_route(const RouteArgs& a, hipStream_t s) {
 
 int launch_route(compact_ctx* ctx, const compact_route_rule& rule, const float* logits, const float* bias, int64_t rows, int32_t* idx,
                  float* weight, hipStream_t s) {
+    constexpr int64_t most = 1ll << 25;   // rows of a launch, of up to 64 threads each
+    static_assert(most * 64 <= MAX_GRID_THREADS, "one launch");
+    if (rows > most) {
+        for (int64_t r = 0; r < rows; r += most)
+            TRY(launch_route(ctx, rule, logits + r * ctx->cfg.n_experts, bias, rows - r < most ? rows - r : most, idx + r * ctx->cfg.top_k,
+                             weight + r * ctx->cfg.top_k, s));
+        return COMPACT_OK;
+    }
     if (rows == 0) return COMPACT_OK;
     const int E = ctx->cfg.n_experts, size = E / rule.n_groups;
     // the quick way: the experts fill the 16 lanes, and a group is 1, 2, 4 or 8 whole lanes

@@ -566,3 +566,56 @@ def test_calls_on_side_streams_have_the_same_bits():
                 c.run()
         torch.cuda.synchronize()
         assert torch.equal(a.y, want) and torch.equal(b.y, want)
+
+
+# ---- offsets beyond 32 bits ------------------------------------------------------------------------------------------------------
+
+def test_rows_of_more_than_4_gi_elements():
+    n, d, k = 600_000, 8192, 5
+    lay = layer(d=d)
+    x = torch.zeros((n, d), dtype=torch.bfloat16, device="cuda")
+    some = rows_of(k, d, "bf16", 1)
+    x[:k], x[-k:] = some, some
+    q, s = torch.full((n, d), 3, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+    lay.compact_quant_i8(x, q, s)
+    want, ws = quantised(lay, some)
+    for at in (slice(0, k), slice(n - k, n)):
+        assert torch.equal(q[at], want) and torch.equal(s[at], ws)
+    assert int(q[k:-k:9973].abs().max()) == 0 and not s[k:-k].any()
+    g, h = torch.ones(d, dtype=torch.bfloat16, device="cuda"), torch.empty_like(x)
+    lay.compact_block_norm(x, b=x, h=h, g_pre=g, q=q, q_scale=s)
+    h2, q2, s2 = torch.empty_like(some), torch.empty_like(want), torch.empty_like(ws)
+    lay.compact_block_norm(some, b=some, h=h2, g_pre=g, q=q2, q_scale=s2)
+    for at in (slice(0, k), slice(n - k, n)):
+        assert torch.equal(q[at], q2) and torch.equal(s[at], s2) and torch.equal(h[at], h2)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40_000, 131_056), (300, 40_000, 131_056), (40_000, 24, 131_056), (70_000, 40_000, 32)])
+def test_products_of_more_than_4_gi_elements(M, N, K):
+    lay = layer()
+    a, b = codes(M, K, 1), codes(N, K, 2)
+    sa, sb = scales(M, 3), scales(N, 4) * 1e-6
+    c = product(lay, a, sa, b, sb)
+    rows, cols = sorted({0, M // 2, M - 2, M - 1}), sorted({0, 7, N // 2 + 1, N - 1})
+    check_product(c[rows][:, cols], a[rows], sa[rows], b[cols], sb[cols], None, 0, "bf16")
+
+
+def test_experts_of_more_than_4_gi_hidden_elements():
+    E, k, d, F, rows = 8, 8, 64, 2944, 200_000
+    lay, ex = layer(d=d, F=F, E=E, k=k), experts(E, d, F, 11)
+    m, ms, h = codes(rows, d, 1), scales(rows, 2) / 70, rows_of(rows, d, "bf16", 3)
+    idx, w = routed(rows, E, k, 5)
+    y = ffn(lay, ex, m, ms, h, idx, w)
+    for at in (slice(0, 40), slice(rows - 40, rows)):
+        assert torch.equal(y[at], by_products(E, d, F, ex, m[at].contiguous(), ms[at].contiguous(), h[at].contiguous(), idx[at].contiguous(), w[at].contiguous()))
+
+
+def test_routing_of_many_rows():
+    lay, rows = layer(E=256, k=8), 9_000_000      # 2.3 gi logits
+    x = torch.randn((1000, 256), generator=gen(1), device="cuda").repeat(rows // 1000, 1)
+    idx, w = torch.empty((rows, 8), dtype=torch.int32, device="cuda"), torch.empty((rows, 8), device="cuda")
+    for rule in (dict(score="sigmoid", n_groups=8, topk_groups=4, group_top=2), dict(score="softmax")):
+        lay.compact_route(B.RouteRule(**rule), x, None, idx, w)
+        i2, w2 = torch.empty((1000, 8), dtype=torch.int32, device="cuda"), torch.empty((1000, 8), device="cuda")
+        lay.compact_route(B.RouteRule(**rule), x[:1000].contiguous(), None, i2, w2)
+        assert torch.equal(idx.view(-1, 1000, 8), i2.expand(rows // 1000, -1, -1)) and torch.equal(w.view(-1, 1000, 8), w2.expand(rows // 1000, -1, -1))

@@ -88,9 +88,9 @@ def test_calls_refuse_what_the_kernels_cannot_take():
     assert code(lay, "compact_gemm_i8", P, P, P, P, P, P, 4, 64, 64, 1, None, 0, None) == 1      # a residual behind SwiGLU
     assert code(lay, "compact_gemm_i8_workspace_bytes", 4, 64, 72, 0, C.byref(n)) == 2
     assert code(lay, "compact_gemm_i8_workspace_bytes", 4, 64, 64, 0, None) == 1
-    good = [P, P, P, P, 0, 1.0, P, P, P, P, P, 4]
+    good = [P, P, P, P, 0, 1.0, P, P, 2 * P, P, P, 4]
     for change in ({6: None, 8: None, 9: None, 10: None}, {9: None}, {10: None}, {7: None}, {1: None}, {1: None, 2: None, 3: None}, {0: None}, {4: 4}, {4: 4092}, {4: -4096},
-                   {11: -1}, {0: P + 8}, {2: P + 8}, {9: P + 4}):
+                   {11: -1}, {0: P + 8}, {2: P + 8}, {9: P + 4}, {8: P}):
         args = [change.get(i, v) for i, v in enumerate(good)]
         assert code(lay, "compact_block_norm", *args, None) == 1, change
     assert code(lay, "compact_block_norm", *good[:-1], 1 << 31, None) == 2
@@ -109,6 +109,7 @@ def test_routing_refuses_rules_that_do_not_fit():
     assert route(n_groups=0) == 2 and route(n_groups=3) == 2 and route(topk_groups=0) == 2 and route(topk_groups=5) == 2
     assert route(n_groups=16, topk_groups=3) == 2      # fewer experts than top_k
     assert route(m=P) == 1 and route(w=P) == 1 and route(logits=None) == 1 and route(rows=-1) == 1 and route(rows=1 << 31) == 2
+    assert route(m=P, w=P + 8) == 1 and route(m=P + 2, w=P) == 1 and route(m=P, w=P, logits=P + 4) == 1
     assert route(rows=0, logits=None) == 0
     assert code(lay, "compact_route", None, None, None, P, None, 4, P, P, None) == 1
     assert route(lay=B.Layer(WORKLOADS["dense_8x4096"].layer, None)) == 1
