@@ -267,7 +267,7 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_tile_kernel(const GemmI8P
                                            wm * WTM, wn * WOUT);
 }
 
-// Sums of k-slices -> outputs, 4 columns a thread.
+// Sums of k-slices -> outputs, 4 columns a thread; the slices' sums (8 at most) are all requested before the first is used.
 template <bool GLU>
 __global__ __launch_bounds__(256) void gemm_i8_finish_kernel(const GemmI8Params p, int slices) {
     const int cols = GLU ? 2 * p.N : p.N;
@@ -275,15 +275,32 @@ __global__ __launch_bounds__(256) void gemm_i8_finish_kernel(const GemmI8Params 
     const int64_t m = blockIdx.y;
     if (n >= p.N) return;
     const float xs = p.xs[m];
-    int g[4] = {0, 0, 0, 0}, u[4] = {0, 0, 0, 0};
-    for (int s = 0; s < slices; ++s) {
-        const int* row = p.sums + ((int64_t)s * p.M + m) * cols + n;
+    intx4 g = intx4{0, 0, 0, 0}, u = g;
+    const int* first = p.sums + m * cols + n;
+    if (p.N % 4 == 0) {
+        intx4 gv[8], uv[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < p.N) {
-                g[e] += row[e];
-                if (GLU) u[e] += row[p.N + e];
+        for (int s = 0; s < 8; ++s) {
+            const int* row = first + (int64_t)min(s, slices - 1) * p.M * cols;
+            gv[s] = *reinterpret_cast<const intx4*>(row);
+            if (GLU) uv[s] = *reinterpret_cast<const intx4*>(row + p.N);
+        }
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            if (s < slices) {
+                g += gv[s];
+                if (GLU) u += uv[s];
             }
+    } else {
+        for (int s = 0; s < slices; ++s) {
+            const int* row = first + (int64_t)s * p.M * cols;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < p.N) {
+                    g[e] += row[e];
+                    if (GLU) u[e] += row[p.N + e];
+                }
+        }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)

@@ -176,15 +176,25 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, i
     __shared__ uint32_t redm[NT / 64];
     const int64_t row = blockIdx.x;
     float v[P][8], b[P][8];
+    // everything that the row needs is requested before anything is used: few rows would wait for each of it
+    Piece<T> xv[P], bv[P], g_post[P], gate[P], g_pre[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
         const int c = (threadIdx.x + i * NT) * 8;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = b[i][j] = 0.f;
+        xv[i].zero();
+        bv[i].zero();
         if (c < d) {
-            load8((const T*)a.x + row * d + c, v[i]);
-            if (a.b) load8((const T*)a.b + row * d + c, b[i]);
+            xv[i].load((const T*)a.x + row * d + c);
+            if (a.b) bv[i].load((const T*)a.b + row * d + c);
+            if (a.g_post) g_post[i].load((const T*)a.g_post + c);
+            if (a.gate) gate[i].load((const T*)a.gate + row * a.gate_stride + c);
+            if (a.g_pre) g_pre[i].load((const T*)a.g_pre + c);
         }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        xv[i].get(v[i]);
+        bv[i].get(b[i]);
     }
     if (a.b) {
         float inv = 1.f;
@@ -202,12 +212,12 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, i
             if (c >= d) continue;
             float g[8];
             if (a.g_post) {
-                load8((const T*)a.g_post + c, g);
+                g_post[i].get(g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) b[i][j] = b[i][j] * inv * g[j];
             }
             if (a.gate) {
-                load8((const T*)a.gate + row * a.gate_stride + c, g);
+                gate[i].get(g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) b[i][j] *= g[j];
             }
@@ -233,7 +243,7 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, i
         if (a.h) store8((T*)a.h + row * d + c, v[i]);
         if (a.g_pre) {
             float g[8];
-            load8((const T*)a.g_pre + c, g);
+            g_pre[i].get(g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 v[i][j] = to_f32(from_f32<T>(v[i][j] * inv * g[j]));
