@@ -1,5 +1,18 @@
 // Products of 8-bit codes:  C[m, n] = a_scale[m] b_scale[n] sum_k A[m, k] B[n, k], the sum in 32-bit integers.  Integer sums are the
-// same in any order, so every tile form and every split of K gives the same bits.
+// same in any order, so every tile form and every split of K gives the same bits, and the choice may look at the number of rows.
+//
+//  * v_mfma_i32_16x16x64_i8 takes the 16 clocks and the 16 bytes a lane of its bf16 sibling of half the depth: a k-tile is 128 codes, a
+//    128-byte line of either operand, and the tiles, rings and phases are those of the bf16 products, k-tile for k-tile.  So is the rule that
+//    picks a form: it is asked for K / 2 elements of 2 bytes (it was within 3 % of the best of the seven forms at 22 of 23 sizes looked at, N 4096 .. 14336, K 2880 ..
+//    14336, 17 .. 32768 rows, and 8 % off at 2 * 14336 x 4096 with 17 rows: 29.8 us, 27.5 in 64 x 64 tiles);
+//  * at most 16 rows: gemv_i8.hip; 64 x 64 tiles that leave half of the chip idle, and a long K: slices of K, added up by a second launch;
+//  * chunks beyond K (K % 128 != 0) are zeros on the activations' side; N and the rows are clamped in the loads and checked at the stores;
+//  * per-row and per-column scales reach LDS with the first loads of a tile.  Read where they are used they cost two trips to memory, one
+//    after the other, for every 16 rows: 2 * 14336 x 4096 at 32768 rows 3079 -> 2820 us, experts of 16384 rows 2755 -> 2508.
+// Bound: large products run at the chip's power limit (1.85 GHz of 2.4; codes that are all zero: 2393 us instead of 2850), matrix pipes 70 % busy; 2.7 POP/s for
+// 2 * 14336 x 4096 at 32768 rows (64 x 64 tiles alone 5881 us), 2.9 for N 4096 K 14336 at 16384 rows, 22 us for N 5120 K 2880 at 1001 rows.  A tile has
+// 8 to 10 us beside its k-tiles (1.3 us each): starting the next tile's loads before this one's outputs are written hides 4 of them, but
+// takes the registers and the free order of workgroups: 1.006 of the time for the first, 0.987 for experts of 16384 rows, 1.03 .. 1.06 for fewer, so it is not done.
 #include <algorithm>
 #include <type_traits>
 
@@ -582,7 +595,8 @@ __device__ __forceinline__ void i8_tile_128(const GemmI8Params& p, const I8Tile&
                                              wm * WTM, wn * WOUT);
 }
 
-// Plain products: the output is cut into slots of 256 x 256, in groups of 4 row tiles per column tile; the first n_full of them are a
+// Plain products: the output is cut into slots of 256 x 256, in groups of 4 row tiles per column tile (6 and 8: 0.98 .. 1.03 of the time, the most for
+// K 14336); the first n_full of them are a
 // workgroup each, the others two workgroups of 128 x 256, and last come the halves of a bottom row tile of at most 128 rows.  Routed
 // products: a workgroup per tile of the map, in the form that its rows need.
 template <bool GLU, bool GROUPED, bool CUT>
@@ -590,7 +604,9 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
     constexpr int OUTN = GLU ? 128 : 256;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     if constexpr (GROUPED) {
-        const I8Tile tp = p.g.mtile == 256 ? i8_tile<true, GLU, 256, OUTN, 4>(p) : i8_tile<true, GLU, 128, OUTN, 8>(p);
+        // groups of 2 row tiles per column tile: a third one is another expert's as often as not (groups of 4 / 6 / 8: experts of 16384
+        // rows 2265 / 2238 / 2233 us, 2207 so)
+        const I8Tile tp = p.g.mtile == 256 ? i8_tile<true, GLU, 256, OUTN, 2>(p) : i8_tile<true, GLU, 128, OUTN, 8>(p);
         if (tp.rows_valid <= 0) return;
         if (tp.rows_valid > 128)
             i8_tile_256<GLU, true, CUT>(p, tp, smem);

@@ -21,9 +21,9 @@ __device__ __forceinline__ RowCodes row_codes(uint32_t amax_bits) {
     rc.up = amax < 1e-30f ? 0x1p100f : 1.0f;
     rc.amax = amax * rc.up;
     rc.inv = 127.0f / rc.amax;
-    // The only tie among bf16 values is x = amax / 2 (127 divides the other candidates' denominators): 63.5, which 127 / amax rounded
-    // down would put below.  Rounded up, the product is 63.5 or more, hence 64; every other quotient of two 8-bit numbers is
-    // 2^-16 of itself or more away from a tie, the error here is 2^-22.
+    // bf16 values x = X 2^s, amax = A 2^t with 8-bit X and A are a tie where 254 X = (2 j + 1) A 2^n, so where the prime 127 divides 2 j + 1 (j = 63: x = amax / 2) or
+    // A (then 127 / amax is a power of two and the product exact).  The first is 63.5, which 127 / amax rounded down would put below; rounded up, the
+    // product is 63.5 or more, hence 64.  Every other quotient is 2^-16 of itself or more away from a tie, the error here is 2^-22.
     if (fmaf(rc.inv, rc.amax, -127.0f) < 0.0f) rc.inv = __uint_as_float(__float_as_uint(rc.inv) + 1);
     if (amax_bits == 0) rc.inv = 0.0f;
     if (amax_bits >= 0x7f800000u) {

@@ -1,4 +1,6 @@
-// Rows as 8-bit codes, and the norms around a block whose rows leave as codes.
+// Rows as 8-bit codes, and the norms around a block whose rows leave as codes.  Both are bound by HBM and read a row once: it waits in
+// registers for its largest value or its sum of squares.  Codes of 1652 x 14336 13.2 us (5.4 TB/s; an element at a time and twice 99), of 65536 x 2880 89 (6.4);
+// norm with a block's output of 32768 x 4096 rows 181 us (5.9 TB/s, what a copy of that size reaches), of 8 rows 5.0.
 #include <algorithm>
 #include <type_traits>
 
@@ -128,6 +130,8 @@ static void run_quant(const T* x, int64_t x_stride, int64_t rows, int cols, int8
 }
 template <typename T>
 static void quant_rows(const T* x, int64_t x_stride, int64_t rows, int cols, int8_t* q, float* scale, hipStream_t s) {
+    // A wavefront per row up to 4 pieces a lane, and up to 6 where rows fill the chip anyway (no barrier, all lanes at work: 65536 x 2880 in workgroups of
+    // 256 leaves 30 % of the lanes idle); beyond, as many threads as hold the row in 4 or 8 pieces each.
     const bool wide = cols % 8 == 0 && x_stride % 8 == 0 && ((uintptr_t)x & 15) == 0 && ((uintptr_t)q & 7) == 0;
     const int pieces = cols / 8;
     if (!wide || pieces > 8192)
