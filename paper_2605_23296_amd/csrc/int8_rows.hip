@@ -10,10 +10,14 @@
 
 #define NT 256
 
-// largest |x| of the workgroup, as bits: they are ordered as the values are, infinities and NaN above all of them
-__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
+// largest |x| of the wavefront, of the workgroup, as bits: they are ordered as the values are, infinities and NaN above all of them
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+    return v;
+}
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
+    v = wave_max_bits(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = v;
     __syncthreads();
@@ -84,8 +88,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_i8_kernel(const T
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max(m, abs_bits(f[j]));
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    m = wave_max_bits(m);
     if (TPR > 64) {
         if ((t & 63) == 0) red[t / 64] = m;
         __syncthreads();
@@ -112,8 +115,7 @@ __global__ __launch_bounds__(1024) void quant_i8_any_kernel(const T* __restrict_
     const T* xr = x + row * x_stride;
     uint32_t m = 0;
     for (int c = threadIdx.x; c < cols; c += 1024) m = max(m, abs_bits(to_f32(xr[c])));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    m = wave_max_bits(m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = m;
     __syncthreads();
 #pragma unroll
@@ -172,19 +174,22 @@ int launch_quant_i8(compact_ctx* ctx, const void* x, int64_t x_stride, int64_t r
     return COMPACT_OK;
 }
 
-// A workgroup per row, the row in registers: a thread holds the 8-element pieces threadIdx + 256 i.  (h, n may be x or b: nothing is
+// TPR threads per row (64: a wavefront, four rows a workgroup, no barrier; 256: a workgroup), the row in registers: a thread holds the 8-element pieces t + TPR i.  (h, n may be x or b: nothing is
 // written before the whole row has been read, and no pointer promises to be alone.)
-template <typename T, int P>
+template <typename T, int TPR, int P>
 __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, int d, float eps) {
     __shared__ float red[NT / 64];
     __shared__ uint32_t redm[NT / 64];
-    const int64_t row = blockIdx.x;
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
+    if (TPR < NT && row >= a.rows) return;
+    auto sum = [&](float x) __attribute__((always_inline)) { return TPR == 64 ? wave_sum(x) : block_sum(x, red); };
     float v[P][8], b[P][8];
     // everything that the row needs is requested before anything is used: few rows would wait for each of it
     Piece<T> xv[P], bv[P], g_post[P], gate[P], g_pre[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        const int c = (threadIdx.x + i * NT) * 8;
+        const int c = (t + i * TPR) * 8;
         xv[i].zero();
         bv[i].zero();
         if (c < d) {
@@ -208,11 +213,11 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, i
             for (int i = 0; i < P; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) ss += b[i][j] * b[i][j];
-            inv = 1.0f / sqrtf(block_sum(ss, red) / (float)d + eps);
+            inv = 1.0f / sqrtf(sum(ss) / (float)d + eps);
         }
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int c = (threadIdx.x + i * NT) * 8;
+            const int c = (t + i * TPR) * 8;
             if (c >= d) continue;
             float g[8];
             if (a.g_post) {
@@ -236,13 +241,13 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, i
         for (int i = 0; i < P; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) ss += v[i][j] * v[i][j];
-        inv = 1.0f / sqrtf(block_sum(ss, red) / (float)d + eps);
+        inv = 1.0f / sqrtf(sum(ss) / (float)d + eps);
     }
-    __syncthreads();
+    if (TPR > 64) __syncthreads();
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        const int c = (threadIdx.x + i * NT) * 8;
+        const int c = (t + i * TPR) * 8;
         if (c >= d) continue;
         if (a.h) store8((T*)a.h + row * d + c, v[i]);
         if (a.g_pre) {
@@ -257,24 +262,31 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(const BlockNormArgs a, i
         }
     }
     if (!a.q) return;
-    const RowCodes rc = row_codes(block_max(m, redm));
+    const RowCodes rc = row_codes(TPR == 64 ? wave_max_bits(m) : block_max(m, redm));
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        const int c = (threadIdx.x + i * NT) * 8;
+        const int c = (t + i * TPR) * 8;
         if (c < d) *reinterpret_cast<uint2*>(a.q + row * d + c) = codes8<T>(v[i], rc);
     }
-    if (threadIdx.x == 0) a.q_scale[row] = rc.scale;
+    if (t == 0) a.q_scale[row] = rc.scale;
 }
 
 template <typename T>
 static void run_block_norm(const BlockNormArgs& a, int d, float eps, hipStream_t s) {
-    const unsigned rows = (unsigned)a.rows;
-    switch ((d + NT * 8 - 1) / (NT * 8)) {   // (d_model is at most 8192)
-        case 1: block_norm_kernel<T, 1><<<rows, NT, 0, s>>>(a, d, eps); break;
-        case 2: block_norm_kernel<T, 2><<<rows, NT, 0, s>>>(a, d, eps); break;
-        case 3: block_norm_kernel<T, 3><<<rows, NT, 0, s>>>(a, d, eps); break;
-        default: block_norm_kernel<T, 4><<<rows, NT, 0, s>>>(a, d, eps); break;
-    }
+    const unsigned rows = (unsigned)a.rows, fours = (rows + 3) / 4;
+    const int pieces = d / 8;   // (d_model is at most 8192; the choice goes by it alone: a row's bits do not depend on the others)
+    if (pieces <= 64)
+        block_norm_kernel<T, 64, 1><<<fours, NT, 0, s>>>(a, d, eps);
+    else if (pieces <= 128)
+        block_norm_kernel<T, 64, 2><<<fours, NT, 0, s>>>(a, d, eps);
+    else if (pieces <= 256)
+        block_norm_kernel<T, 256, 1><<<rows, NT, 0, s>>>(a, d, eps);
+    else if (pieces <= 512)
+        block_norm_kernel<T, 256, 2><<<rows, NT, 0, s>>>(a, d, eps);
+    else if (pieces <= 768)
+        block_norm_kernel<T, 256, 3><<<rows, NT, 0, s>>>(a, d, eps);
+    else
+        block_norm_kernel<T, 256, 4><<<rows, NT, 0, s>>>(a, d, eps);
 }
 int launch_block_norm(compact_ctx* ctx, const BlockNormArgs& all, hipStream_t s) {
     const int d = ctx->cfg.d_model;

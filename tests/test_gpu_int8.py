@@ -78,6 +78,7 @@ def test_codes_of_values_at_every_size(dtype):
     x[13], x[13, 40] = 0, -2.5
     x[14, 0], x[15, 135], x[16, 9], x[17, 3], x[17, 4] = math.inf, -math.inf, math.nan, math.nan, math.inf
     x[18] = -1.0
+    x[20], x[21] = x[20] * tiny * 2.0 ** -4, x[21] * tiny * 2.0 ** -7      # below the normal numbers
     x[19] = torch.arange(136, device="cuda").to(DT[dtype]) - 60.5 if dtype == "fp32" else x[19]    # ties and neighbours of them
     q, s = quantised(layer(dtype=dtype), x)
     rq, rs = I8.row_codes(f64(x))
@@ -252,7 +253,8 @@ def check_norm(lay, x, b, g_post, gate, alpha, g_pre, dtype):
 
 
 @pytest.mark.parametrize("dtype", DT)
-@pytest.mark.parametrize("rows,d", [(1, 64), (3, 128), (5, 448), (70, 512), (4, 1088), (33, 2048), (2, 2112), (9, 2880), (8, 4096), (3, 6080), (5, 8192), (1100, 256)])
+@pytest.mark.parametrize("rows,d", [(1, 64), (3, 128), (5, 448), (70, 512), (4, 1088), (33, 2048), (2, 2112), (9, 2880), (8, 4096), (3, 6080), (5, 8192), (1100, 256), (7, 576), (6, 1024), (3, 2048),
+                                    (2, 4160)])
 @pytest.mark.parametrize("post,gate", [(False, None), (True, "vector"), (False, "rows"), (True, "apart")])
 def test_norms_around_a_block(dtype, rows, d, post, gate):
     lay = layer(d=d, dtype=dtype)
