@@ -253,7 +253,7 @@ def check_norm(lay, x, b, g_post, gate, alpha, g_pre, dtype):
 
 
 @pytest.mark.parametrize("dtype", DT)
-@pytest.mark.parametrize("rows,d", [(1, 64), (3, 128), (5, 448), (70, 512), (4, 1088), (33, 2048), (2, 2112), (9, 2880), (8, 4096), (3, 6080), (5, 8192), (1100, 256), (7, 576), (6, 1024), (3, 2048),
+@pytest.mark.parametrize("rows,d", [(1, 64), (3, 128), (5, 448), (70, 512), (4, 1088), (33, 2048), (2, 2112), (9, 2880), (8, 4096), (3, 6080), (5, 8192), (1100, 256), (7, 576), (6, 1024), (5, 1536), (2, 1600), (3, 2048),
                                     (2, 4160)])
 @pytest.mark.parametrize("post,gate", [(False, None), (True, "vector"), (False, "rows"), (True, "apart")])
 def test_norms_around_a_block(dtype, rows, d, post, gate):
