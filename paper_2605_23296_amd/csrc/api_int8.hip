@@ -68,12 +68,13 @@ extern "C" int compact_block_norm(compact_ctx* ctx, const void* d_x, const void*
                                   int64_t rows, void* hip_stream) {
     if (!ctx) return COMPACT_EINVAL;
     if (rows < 0) return set_err(ctx, COMPACT_EINVAL, "negative rows");
+    if (rows == 0) return COMPACT_OK;   // (arrays without rows may be null)
     if (!d_h && !d_n && !d_q) return set_err(ctx, COMPACT_EINVAL, "no output is wanted");
     if ((d_q == nullptr) != (d_q_scale == nullptr)) return set_err(ctx, COMPACT_EINVAL, "codes and their scales belong together");
     if ((d_n || d_q) && !d_g_pre) return set_err(ctx, COMPACT_EINVAL, "normalised rows need the gain g_pre");
     if (!d_b && (d_h || d_g_post || d_gate)) return set_err(ctx, COMPACT_EINVAL, "h, g_post and gate need the block's output b");
     if (d_h && d_h == d_n) return set_err(ctx, COMPACT_EINVAL, "h and n are one array");
-    if (rows > 0 && !d_x) return set_err(ctx, COMPACT_EINVAL, "null rows");
+    if (!d_x) return set_err(ctx, COMPACT_EINVAL, "null rows");
     if (d_gate && gate_stride != 0 && (gate_stride < ctx->cfg.d_model || gate_stride % 8 != 0))
         return set_err(ctx, COMPACT_EINVAL, "gate_stride must be 0, or a multiple of 8 that is d_model at least");
     if (rows > MAX_ROWS) return set_err(ctx, COMPACT_ESHAPE, "at most 2^31 - 1 rows");
@@ -97,9 +98,9 @@ extern "C" int compact_route(compact_ctx* ctx, const compact_route_rule* rule, c
     if (rule->topk_groups < 1 || rule->topk_groups > rule->n_groups || c.n_experts / rule->n_groups * rule->topk_groups < c.top_k)
         return set_err(ctx, COMPACT_ESHAPE, "topk_groups must be in 1 .. n_groups, with top_k experts at least in them");
     if (rule->group_top != 1 && rule->group_top != 2) return set_err(ctx, COMPACT_EINVAL, "group_top must be 1 or 2");
+    if (rows == 0) return COMPACT_OK;   // (arrays without rows may be null)
     if ((d_m == nullptr) != (d_w_router == nullptr)) return set_err(ctx, COMPACT_EINVAL, "rows and router weights belong together");
     if (rows > MAX_ROWS) return set_err(ctx, COMPACT_ESHAPE, "at most 2^31 - 1 rows");
-    if (rows == 0) return COMPACT_OK;
     if (!d_logits || !d_expert_idx || !d_weight) return set_err(ctx, COMPACT_EINVAL, "null pointer");
     hipStream_t s = (hipStream_t)hip_stream;
     if (d_m) {

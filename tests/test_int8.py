@@ -97,6 +97,9 @@ def test_calls_refuse_what_the_kernels_cannot_take():
     # nothing to do: nothing is looked at
     assert code(lay, "compact_quant_i8", None, 64, 0, 64, None, None, None) == 0
     assert code(lay, "compact_gemm_i8", None, None, None, None, None, None, 0, 64, 64, 0, None, 0, None) == 0
+    assert code(lay, "compact_block_norm", None, None, P, P, 0, 1.0, None, P, None, None, None, 0, None) == 0
+    assert code(lay, "compact_block_norm", None, None, P, P, 0, 1.0, None, P, None, None, P, 0, None) == 0   # arrays without rows have no address
+    assert code(lay, "compact_block_norm", None, None, P, P, 0, 1.0, None, P, None, None, None, -1, None) == 1
 
 
 def test_routing_refuses_rules_that_do_not_fit():
@@ -110,7 +113,7 @@ def test_routing_refuses_rules_that_do_not_fit():
     assert route(n_groups=16, topk_groups=3) == 2      # fewer experts than top_k
     assert route(m=P) == 1 and route(w=P) == 1 and route(logits=None) == 1 and route(rows=-1) == 1 and route(rows=1 << 31) == 2
     assert route(m=P, w=P + 8) == 1 and route(m=P + 2, w=P) == 1 and route(m=P, w=P, logits=P + 4) == 1
-    assert route(rows=0, logits=None) == 0
+    assert route(rows=0, logits=None) == 0 and route(rows=0, logits=None, w=P) == 0 and route(rows=0, n_groups=3) == 2
     assert code(lay, "compact_route", None, None, None, P, None, 4, P, P, None) == 1
     assert route(lay=B.Layer(WORKLOADS["dense_8x4096"].layer, None)) == 1
     assert refused(lambda: B.RouteRule(score="tanh"))
