@@ -316,18 +316,21 @@ __global__ __launch_bounds__(256) void route_kernel(const RouteArgs a) {
                     m1 = fmaxf(m1, x);
                 }
         }
-        float g = m1;
+        float g = m1, size = fabsf(m1);
         if (rule.group_top == 2) {
             g = m2 > -INFINITY ? m1 + m2 : -INFINITY;
+            size += fabsf(m2);
             slow |= m1 > -INFINITY && !(m2 > -INFINITY);   // (its only live expert counts alone)
         }
+        // Error of g, twice: a value has 2^-21 (a score) and 2^-24 of itself, the sum 2^-24 of what is added, which may be much more than g.
+        const float off = !a.by_logit && g > -INFINITY ? 0x1p-19f + size * 0x1p-22f : 0.f;
         const int above = larger16(g);   // (of all lanes: none of them may sleep)
         const bool here_is_one = t < rule.n_groups * share, chosen = here_is_one && above < rule.topk_groups * share;
         const uint32_t groups = (uint32_t)(__ballot(chosen) >> (at % 4 * 16)) & 0xffff;
-        const float least = -max16(chosen ? -g : -INFINITY), first_out = max16(here_is_one && !chosen ? g : -INFINITY);
+        const float least = -max16(chosen ? off - g : -INFINITY), first_out = max16(here_is_one && !chosen ? g + off : -INFINITY);
         // (equal ones at the border are all chosen, or none)
         slow |= __popc(groups) != rule.topk_groups * share || !(least > -INFINITY) ||
-                (!a.by_logit && !(least - first_out > 0x1p-18f + fabsf(least) * 0x1p-20f));
+                (!a.by_logit && !(least > first_out));
         if (a.lanes) {   // expert t + 16 j was lane (t + 16 j) / V's
             const uint32_t mine_first = groups >> (t / V);
 #pragma unroll

@@ -381,6 +381,18 @@ def test_routing_ties_masks_and_broken_logits(rule, bias):
         assert not np.isin(got[rest], [20, 21]).any()
 
 
+@pytest.mark.parametrize("E,k,groups,of", [(16, 4, 8, 4), (24, 5, 12, 4), (64, 6, 8, 3), (256, 8, 8, 4), (160, 8, 16, 5)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20])
+def test_routing_where_the_biases_of_a_group_cancel(E, k, groups, of, score, size):
+    """The two best of every group are size + s and -size + s': their sum is decided by digits that neither has in 32 bits."""
+    S, bias = E // groups, torch.full((E,), -size, device="cuda")
+    for g in range(groups):
+        bias[g * S + g % S] = size
+    x = torch.randn((2000, E), generator=gen(E), device="cuda")
+    check_route(layer(E=E, k=k), dict(score=score, n_groups=groups, topk_groups=of, group_top=2), x, bias, share=0.99)
+
+
 @pytest.mark.parametrize("dtype,E", [("bf16", 128), ("fp32", 24)])
 @pytest.mark.parametrize("rows", [1, 16, 300])
 def test_routing_from_the_rows(dtype, E, rows):
