@@ -107,11 +107,47 @@ __device__ __forceinline__ void i8_store(const GemmI8Params& p, const I8Tile& tp
             *reinterpret_cast<floatx4*>(slab + r * SLD + j * 16 + c4 * 4) = v;
         }
         __builtin_amdgcn_wave_barrier();
+        // (rows that are not aligned: an element a lane, neighbours side by side, B of them at a time; with 8 neighbours a lane 8192 x 4100 K 4096 took
+        // 175 us for 150, 221 for 178 with a residual, fp32 201 for 150, 255 for 181)
+        constexpr int B = WOUT / 4 < 8 ? WOUT / 4 : 8;
+        const int64_t own = (tp.m0 + wrow + i * 16) * p.N + n_first;
+        for (int u0 = 0; u0 < (wide || n_first >= p.N ? 0 : WOUT / 4); u0 += B) {
+            float v[B];
+            int64_t o[B];
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                const int row = (lane + 64 * (u0 + u)) / WOUT, c = (lane + 64 * (u0 + u)) % WOUT;
+                const int lm = wrow + i * 16 + row, n = n_first + c;
+                o[u] = lm < tp.rows_valid && n < p.N ? (tp.m0 + lm) * p.N + n : -1;
+                v[u] = slab[row * SLD + c];
+                if (GROUPED && p.g.row_scale) v[u] *= gates[lm];
+            }
+            if (p.R) {   // (all requested before the first is used; where there is nothing to add, the slab's first element)
+                float rv[B];
+                if (p.f32) {
+#pragma unroll
+                    for (int u = 0; u < B; ++u) rv[u] = ((const float*)p.R)[o[u] < 0 ? own : o[u]];
+                } else {
+#pragma unroll
+                    for (int u = 0; u < B; ++u) rv[u] = (float)((const bf16*)p.R)[o[u] < 0 ? own : o[u]];
+                }
+#pragma unroll
+                for (int u = 0; u < B; ++u) v[u] += rv[u];
+            }
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                if (o[u] < 0) continue;
+                if (p.f32)
+                    ((float*)p.C)[o[u]] = v[u];
+                else
+                    ((bf16*)p.C)[o[u]] = (bf16)v[u];
+            }
+        }
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             const int row = (lane + 64 * u) / NCH, c = (lane + 64 * u) % NCH;
             const int lm = wrow + i * 16 + row, n = n_first + c * 8;
-            if (row >= 16 || lm >= tp.rows_valid || n >= p.N) continue;
+            if (!wide || row >= 16 || lm >= tp.rows_valid || n >= p.N) continue;
             const int64_t o = (tp.m0 + lm) * p.N + n;
             float v[8];
             const floatx4 a = *reinterpret_cast<const floatx4*>(slab + row * SLD + c * 8);
@@ -126,23 +162,19 @@ __device__ __forceinline__ void i8_store(const GemmI8Params& p, const I8Tile& tp
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= f;
             }
-            if (wide) {
-                float rv[8];
-                if (p.R) {
-                    if (p.f32)
-                        load8((const float*)p.R + o, rv);
-                    else
-                        load8((const bf16*)p.R + o, rv);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += rv[e];
-                }
+            float rv[8];
+            if (p.R) {
                 if (p.f32)
-                    store8((float*)p.C + o, v);
+                    load8((const float*)p.R + o, rv);
                 else
-                    store8((bf16*)p.C + o, v);
-            } else {
-                for (int e = 0; e < 8 && n + e < p.N; ++e) i8_put(p, o + e, v[e]);
+                    load8((const bf16*)p.R + o, rv);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += rv[e];
             }
+            if (p.f32)
+                store8((float*)p.C + o, v);
+            else
+                store8((bf16*)p.C + o, v);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -750,7 +782,7 @@ extern "C" int compact_test_gemm_i8_form(compact_ctx* ctx, int32_t form, int32_t
                                          const float* b_scale, const void* r, void* c, int64_t M, int32_t N, int32_t K, int32_t epilogue,
                                          void* hip_stream) {
     if (!ctx || !a || !a_scale || !b || !b_scale || !c || M < 1 || N < 1 || K < 16 || K % 16 || form < 0 || form > TILE_FORMS || (epilogue != 0 && epilogue != 1) ||
-        slices < 1 || slices > (K + I8_BK - 1) / I8_BK || (slices > 1 && (!sums || form <= TILE_128 || form == TILE_FORMS)))
+        slices < 1 || slices > 8 || slices > (K + I8_BK - 1) / I8_BK || (slices > 1 && (!sums || form <= TILE_128 || form == TILE_FORMS)))
         return COMPACT_EINVAL;
     const GemmI8Args g{(const int8_t*)a, a_scale, (const int8_t*)b, b_scale, r, c, M, N, K, epilogue, nullptr};
     GemmI8Params p = i8_params(ctx, g);
