@@ -67,6 +67,9 @@ class PagedStepStruct(C.Structure):
                                           "d_kv_len", "d_cu", "d_slot", "d_rot")] + [("max_rows", C.c_int32)]
 
 
+MAX_INT = 0x7fffffff   # (a 32-bit argument takes a larger number modulo 2^32, without a word)
+
+
 class RouteRuleStruct(C.Structure):
     _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("topk_groups", C.c_int32), ("group_top", C.c_int32), ("renorm", C.c_int32),
                 ("factor", C.c_float)]
@@ -330,6 +333,8 @@ class RouteRule:
     def __init__(self, score="softmax", n_groups=1, topk_groups=None, group_top=1, renorm=True, factor=1.0):
         if score not in ("softmax", "sigmoid"):
             _refuse("route: score %r; softmax or sigmoid needed" % (score,))
+        if max(n_groups, topk_groups or 0, group_top) > MAX_INT or min(n_groups, topk_groups or 0, group_top) < 0:
+            _refuse("route: %d groups, %s of them, %d experts of each; counts needed" % (n_groups, topk_groups, group_top))
         self.c = RouteRuleStruct(int(score == "sigmoid"), n_groups, n_groups if topk_groups is None else topk_groups, group_top, bool(renorm), factor)
         self.ref = C.byref(self.c)
 
@@ -575,7 +580,7 @@ class Layer:
         apart, step = x.stride()
         if rows <= 1:
             apart = cols
-        if (x.dtype is not self.torch_dtype or x.get_device() != device or step != 1 and cols > 1
+        if (x.dtype is not self.torch_dtype or x.get_device() != device or step != 1 and cols > 1 or cols > MAX_INT
                 or q.dtype is not torch.int8 or q.shape != shape or q.get_device() != device or not q.is_contiguous()
                 or scale.dtype is not torch.float32 or scale.numel() < rows or scale.get_device() != device or not scale.is_contiguous()):
             _array(q, torch.int8, rows * cols, device, "codes")
@@ -597,7 +602,7 @@ class Layer:
         if len(a.shape) != 2 or len(b.shape) != 2 or len(c.shape) != 2:
             _refuse("product: a %s, b %s, c %s; [M, K], [N, K] and [M, N] needed" % (tuple(a.shape), tuple(b.shape), tuple(c.shape)))
         (M, K), (M2, N), (n, K2) = a.shape, c.shape, b.shape
-        if (M2 != M or K2 != K or n != (2 * N if epilogue == 1 else N)
+        if (M2 != M or K2 != K or n != (2 * N if epilogue == 1 else N) or N > MAX_INT or K > MAX_INT
                 or a.dtype is not torch.int8 or a.get_device() != device or not a.is_contiguous()
                 or b.dtype is not torch.int8 or b.get_device() != device or not b.is_contiguous()
                 or a_scale.dtype is not torch.float32 or a_scale.numel() < M or a_scale.get_device() != device or not a_scale.is_contiguous()

@@ -117,6 +117,8 @@ def test_routing_refuses_rules_that_do_not_fit():
     assert code(lay, "compact_route", None, None, None, P, None, 4, P, P, None) == 1
     assert route(lay=B.Layer(WORKLOADS["dense_8x4096"].layer, None)) == 1
     assert refused(lambda: B.RouteRule(score="tanh"))
+    for wrong in (dict(n_groups=2 ** 32 + 4), dict(n_groups=4, topk_groups=2 ** 32 + 2), dict(group_top=2 ** 32 + 1), dict(n_groups=1 - 2 ** 32)):
+        assert refused(lambda: B.RouteRule(**wrong)), wrong
 
 
 def test_experts_refuse_what_the_kernels_cannot_take():
@@ -205,3 +207,17 @@ def test_arrays_that_may_be_refused_or_not(on_the_host, monkeypatch):
     for op in a:
         assert refused(lambda: call(lay, op, a[op])), op
     assert lay.L.n == 6
+
+
+def test_sizes_beyond_32_bits_are_refused(on_the_host):
+    lay, n, bf, i8 = on_the_host, 2 ** 32 + 64, torch.bfloat16, torch.int8
+
+    def z(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+    lay.compact_gemm_i8(z(1, 16, dtype=i8), z(1), z(8, 16, dtype=i8), z(8), None, z(1, 8, dtype=bf))
+    lay.compact_quant_i8(z(1, 64, dtype=bf), z(1, 64, dtype=i8), z(1))
+    assert lay.L.n == 2
+    assert refused(lambda: lay.compact_quant_i8(z(1, n, dtype=bf), z(1, n, dtype=i8), z(1)))
+    assert refused(lambda: lay.compact_gemm_i8(z(1, n, dtype=i8), z(1), z(1, n, dtype=i8), z(1), None, z(1, 1, dtype=bf)))
+    assert refused(lambda: lay.compact_gemm_i8(z(1, 16, dtype=i8), z(1), z(n, 16, dtype=i8), z(n), None, z(1, n, dtype=bf)))
+    assert lay.L.n == 2
