@@ -28,8 +28,9 @@ struct GemmI8Params {
 // what chunks of 16 codes beyond K are read from, on the activations' side
 static __device__ const int8_t zero_codes[16] __attribute__((aligned(16))) = {};
 
-// gemv_i8.hip : at most this many rows, of the call or of a tile of the experts' map
+// gemv_i8.hip : at most this many rows, of a tile of the experts' map or of the call; of the call up to MOST where that pays
 #define I8_STREAM_ROWS 16
+#define I8_STREAM_ROWS_MOST 48
 int launch_stream_i8(compact_ctx* ctx, GemmI8Params& p, bool glu, hipStream_t s);
 
 // the kernel may use that much LDS, on every device that it runs on (a set bit is a device that knows)

@@ -5,7 +5,7 @@
 //    128-byte line of either operand, and the tiles, rings and phases are those of the bf16 products, k-tile for k-tile.  So is the rule that
 //    picks a form: it is asked for K / 2 elements of 2 bytes (it was within 3 % of the best of the seven forms at 22 of 23 sizes looked at, N 4096 .. 14336, K 2880 ..
 //    14336, 17 .. 32768 rows, and 8 % off at 2 * 14336 x 4096 with 17 rows: 29.8 us, 27.5 in 64 x 64 tiles);
-//  * at most 16 rows: gemv_i8.hip; 64 x 64 tiles that leave half of the chip idle, and a long K: slices of K, added up by a second launch;
+//  * at most 16 rows, and up to 48 of few columns: gemv_i8.hip; 64 x 64 tiles that leave half of the chip idle, and a long K: slices of K, added up by a second launch;
 //  * chunks beyond K (K % 128 != 0) are zeros on the activations' side; N and the rows are clamped in the loads and checked at the stores;
 //  * per-row and per-column scales reach LDS with the first loads of a tile.  Read where they are used they cost two trips to memory, one
 //    after the other, for every 16 rows: 2 * 14336 x 4096 at 32768 rows 3079 -> 2820 us, experts of 16384 rows 2755 -> 2508.
@@ -724,13 +724,27 @@ static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params&
 // Slices of K for products whose 64 x 64 tiles leave half of the chip idle and more: as many as fill its 256 compute units, of 16 k-tiles
 // at least (the second launch, which adds the slices up, costs 3 us).  N 4096 K 14336 at 17 / 64 / 128 rows 31 / 36 / 36 us whole, 17.7 /
 // 19.2 / 25.6 in 4 / 4 / 2 slices, 20 / 24 / 31 in 6; K 6144 at 64 rows 16.8 whole, 13.5 in 3; N 1024 K 14336 at 64 rows 32.6, in 4 16.0, in 8 14.6.
+static int64_t gemm_i8_small_tiles(int64_t M, int N, int epilogue) { return (M + 63) / 64 * ((N + (epilogue ? 31 : 63)) / (epilogue ? 32 : 64)); }
 static int gemm_i8_slices(int64_t M, int N, int K, int epilogue) {
-    const int64_t tiles = (M + 63) / 64 * ((N + (epilogue ? 31 : 63)) / (epilogue ? 32 : 64));
-    if (M <= I8_STREAM_ROWS || tiles > 128) return 1;
+    const int64_t tiles = gemm_i8_small_tiles(M, N, epilogue);
+    if (tiles > 128) return 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, (K + I8_BK - 1) / I8_BK / 16, 8}));
 }
+// Whether 17 to 48 rows are a weight stream (gemv_i8.hip; M at most 16 always is), rather than 64 x 64 tiles, in slices of K if it is long.  Every workgroup of
+// the stream reads all activations, at its compute unit's pace; slices are a second launch.  The stream's time, the other's = 1, at 17 / 32 / 33 / 48 rows:
+//  * no slices: N 2880 K 2880 0.88 / 0.88 / 0.88 / 0.90, 5120 x 2880 0.89 / 0.88 / 0.98 / 1.03, SwiGLU 4096 x 2048 0.98 / 0.97 / 1.05 / 1.06;
+//  * slices: 512 x 4096 0.7, 6144 x 4096 0.81 / 0.83 / 0.90 / 0.90, 8192 x 4096 0.83 / 0.84 / 0.91 / 0.91, 1024 x 8192 0.70 / 0.75 / 0.84 / 0.89, 4096 x 8192
+//    0.87 / 0.91 / 0.97 / 1.04, 8192 x 14336 0.92 / 0.97 / 1.01 / 1.03, 4096 x 14336 0.93 / 1.06 / 1.0 / 1.0, 2048 x 28672 1.3 and more;
+//  * 64 rows: 0.80 (512 x 4096) .. 1.18 (5120 x 2880).
+static bool gemm_i8_streams(int64_t M, int N, int K, int epilogue) {
+    if (M <= I8_STREAM_ROWS) return true;
+    const int64_t tiles = gemm_i8_small_tiles(M, N, epilogue);
+    if (M > I8_STREAM_ROWS_MOST || tiles > 128) return false;
+    if (gemm_i8_slices(M, N, K, epilogue) == 1) return M <= 32 || tiles <= 64;
+    return (int64_t)(16 + (M <= 32 ? 32 : 48)) * K <= 400000;
+}
 size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {
-    const int slices = gemm_i8_slices(M, N, K, epilogue);
+    const int slices = gemm_i8_streams(M, N, K, epilogue) ? 1 : gemm_i8_slices(M, N, K, epilogue);
     return slices < 2 ? 0 : (size_t)slices * M * N * (epilogue ? 2 : 1) * sizeof(int);
 }
 int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) {
@@ -765,9 +779,11 @@ int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_by
         if (p.g.mtile == I8_STREAM_ROWS) return launch_stream_i8(ctx, p, a.epilogue != 0, s);
         return a.epilogue ? launch_form<true, true>(ctx, form, 0, p, s) : launch_form<false, true>(ctx, form, 0, p, s);
     }
-    if (a.M <= I8_STREAM_ROWS) return launch_stream_i8(ctx, p, a.epilogue != 0, s);
     const int slices = gemm_i8_slices(a.M, a.N, a.K, a.epilogue);
-    if (slices > 1 && ws && ((uintptr_t)ws & 15) == 0 && ws_bytes >= gemm_i8_workspace(a.M, a.N, a.K, a.epilogue)) {
+    const bool room = ws && ((uintptr_t)ws & 15) == 0 && ws_bytes >= gemm_i8_workspace(a.M, a.N, a.K, a.epilogue);
+    // (without room for the slices' sums the stream is better than whole tiles)
+    if (gemm_i8_streams(a.M, a.N, a.K, a.epilogue) || (a.M <= I8_STREAM_ROWS_MOST && slices > 1 && !room)) return launch_stream_i8(ctx, p, a.epilogue != 0, s);
+    if (slices > 1 && room) {
         p.sums = (int*)ws;
         return a.epilogue ? launch_form<true, false>(ctx, TILE_64_64, 0, p, s, slices) : launch_form<false, false>(ctx, TILE_64_64, 0, p, s, slices);
     }

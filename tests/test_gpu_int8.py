@@ -130,7 +130,8 @@ def check_product(c, a, sa, b, sb, r, epilogue, dtype):
 @pytest.mark.parametrize("epilogue,res", [(0, False), (0, True), (1, False)])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 8, 64), (2, 3, 48), (3, 16, 128), (5, 100, 144), (8, 96, 4096), (9, 257, 272), (15, 24, 1040), (16, 64, 2880), (17, 64, 128),
                                    (31, 130, 256), (33, 7, 112), (63, 264, 1152), (64, 128, 512), (65, 72, 384), (127, 40, 640), (129, 520, 896), (200, 1001, 208),
-                                   (257, 264, 272), (300, 136, 3968), (513, 72, 1024), (17, 96, 4096), (64, 1000, 4112), (130, 77, 6160)])
+                                   (257, 264, 272), (300, 136, 3968), (513, 72, 1024), (17, 96, 4096), (64, 1000, 4112), (130, 77, 6160), (40, 96, 16400), (18, 520, 8208), (49, 72, 8192),
+                                   (48, 1000, 336)])
 def test_products(dtype, epilogue, res, M, N, K):
     lay = layer(dtype=dtype)
     a, b = codes(M, K, 1), codes((1 + epilogue) * N, K, 2, -128)
@@ -144,7 +145,7 @@ def test_products(dtype, epilogue, res, M, N, K):
         small = torch.empty_like(c)
         lay.compact_gemm_i8(a, sa, b, sb, r, small, epilogue)
         assert torch.equal(small, c)
-    assert (lay.gemm_i8_workspace_bytes(M, N, K, epilogue) > 0) == (M > 16 and K >= 4096)
+    assert (lay.gemm_i8_workspace_bytes(M, N, K, epilogue) > 0) == (M > 48 and K >= 4096 or M > 16 and K > 16000)
 
 
 def in_form(lay, form, a, sa, b, sb, r, epilogue, slices=1):
