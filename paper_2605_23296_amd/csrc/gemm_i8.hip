@@ -637,8 +637,8 @@ __global__ __launch_bounds__(512) void gemm_i8_kernel(const GemmI8Params p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     if constexpr (GROUPED) {
         // groups of 2 row tiles per column tile: a third one is another expert's as often as not (groups of 4 / 6 / 8: experts of 16384
-        // rows 2265 / 2238 / 2233 us, 2207 so)
-        const I8Tile tp = p.g.mtile == 256 ? i8_tile<true, GLU, 256, OUTN, 2>(p) : i8_tile<true, GLU, 128, OUTN, 8>(p);
+        // rows 2265 / 2238 / 2233 us, 2207 so; of 512 rows, in tiles of 128, 8: 695, 672 so)
+        const I8Tile tp = i8_tile<true, GLU, 256, OUTN, 2>(p);
         if (tp.rows_valid <= 0) return;
         if (tp.rows_valid > 128)
             i8_tile_256<GLU, true, CUT>(p, tp, smem);
@@ -748,8 +748,13 @@ size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {
     return slices < 2 ? 0 : (size_t)slices * M * N * (epilogue ? 2 : 1) * sizeof(int);
 }
 int gemm_i8_group_mtile(int64_t rows, int n_experts, int F, int d, int n_cus) {
-    if (rows <= 12 * n_experts) return I8_STREAM_ROWS;
-    return gemm_bf16_group_mtile(rows, n_experts, F, d / 2, n_cus);
+    // up to 9 rows an expert on average the weight stream, whose tiles of 16 rows read the weights again beyond that: 128 experts of 2880 x 2880 with 8 / 9 / 10 / 12 rows
+    // each 578 / 602 / 635 / 686 us, in tiles 600 / 605 / 617 / 633; 64 of 1024 x 1408 with 7.5 / 9 / 12 rows 77 / 79 / 88, 72 / 73 / 79
+    if (rows <= 9 * n_experts) return I8_STREAM_ROWS;
+    const int mtile = gemm_bf16_group_mtile(rows, n_experts, F, d / 2, n_cus);
+    // tiles of 256 rows that hold 128 at most are done as those; with many rounds of workgroups the others' larger steps count more than an even last round:
+    // 128 experts, 4096 rows 987 for 1090 us, 512 .. 2048 rows 0.99; 64 of 1024 x 1408 (3 rounds), 2048 rows 156 for 146; 8 of 4096 x 1408, 400 rows 81 for 59
+    return mtile == 128 && n_experts * (int64_t)((F + 127) / 128) >= 8 * n_cus ? 256 : mtile;
 }
 
 static GemmI8Params i8_params(compact_ctx* ctx, const GemmI8Args& a) {

@@ -8,8 +8,8 @@
 // 16 wavefronts for a plain product, with T as small as one workgroup per compute unit allows; 8 for experts, two workgroups per compute unit, so that one streams while
 // the other finishes (8 for plain products: 0.97 .. 1.19 of the time); 8, and rings as deep as LDS holds, with more than 16 rows, whose activations take most of it.
 // Bound: HBM.  2 * 14336 x 4096 at 8 rows 20.2 us of kernel (5.8 TB/s; in 64 x 64 tiles the call took 27.6 us, so 25.1), N 4096 K 14336 at 8 rows 13.3 a call, experts (128 of
-// 2880 x 2880, top-4) of 16 rows 119 + 64 us (5.8 TB/s; in 64 x 64 tiles the whole call took 461, so 202), of 256 rows 584
-// (660 in tiles of 256 rows), of 512 rows 786 (753): from 12 rows an expert on average the tiles take over.
+// 2880 x 2880, top-4) of 16 rows 119 + 64 us (5.8 TB/s; in 64 x 64 tiles the whole call took 461, so 202).  Tiles of 32 rows for experts, two columns of MFMAs:
+// 1.01 .. 1.09 of the time up to 8 rows an expert, at 12 0.95, where 256-row tiles take 0.92.
 #include <algorithm>
 #include <utility>
 
