@@ -721,26 +721,30 @@ static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params&
     return set_err(ctx, COMPACT_EINVAL, "unknown GEMM tile");
 }
 
-// Slices of K for products whose 64 x 64 tiles leave half of the chip idle and more: as many as fill its 256 compute units, of 16 k-tiles
-// at least (the second launch, which adds the slices up, costs 3 us).  N 4096 K 14336 at 17 / 64 / 128 rows 31 / 36 / 36 us whole, 17.7 /
-// 19.2 / 25.6 in 4 / 4 / 2 slices, 20 / 24 / 31 in 6; K 6144 at 64 rows 16.8 whole, 13.5 in 3; N 1024 K 14336 at 64 rows 32.6, in 4 16.0, in 8 14.6.
+// Slices of K for products whose 64 x 64 tiles leave half of the chip idle and more: as many as fill its 256 compute units, of 8 k-tiles at least, and
+// from K 5120 on (the second launch, which adds the slices up, costs 3 us, and the caller's thread 1 more).  Whole and in 2, 3, 4, 5 slices, us:
+//  * 64 rows: N 4096 K 4096 12.0, 11.9, 11.8, 11.1, 13.7 (N 2048 at 128 rows 10.1, 11.1, 10.6, 10.8); K 5120 15.6, 13.8, 12.6, 12.1; K 8192 20.7, 16.4, 14.4, 13.1,
+//    16.7; K 14336 36 whole, 19.2 in 4, 24 in 6;
+//  * N 2048 at 64 rows: K 4096 9.9, 10.6, 9.6, 9.2, 9.5, K 6144 16.2, 13.4, 11.3, 10.7, 10.3; N 1024 K 14336 32.6 whole, 16.0 in 4, 14.6 in 8;
+//  * 128 tiles: N 4096 at 128 rows, K 4096 12.1, 13.0, K 5120 15.4, 15.1, K 6144 16.6, 15.1.
 static int64_t gemm_i8_small_tiles(int64_t M, int N, int epilogue) { return (M + 63) / 64 * ((N + (epilogue ? 31 : 63)) / (epilogue ? 32 : 64)); }
 static int gemm_i8_slices(int64_t M, int N, int K, int epilogue) {
     const int64_t tiles = gemm_i8_small_tiles(M, N, epilogue);
-    if (tiles > 128) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, (K + I8_BK - 1) / I8_BK / 16, 8}));
+    const int k_tiles = (K + I8_BK - 1) / I8_BK;
+    if (tiles > 128 || k_tiles < 40) return 1;
+    return (int)std::min<int64_t>({256 / tiles, k_tiles / 8, 8});
 }
 // Whether 17 to 48 rows are a weight stream (gemv_i8.hip; M at most 16 always is), rather than 64 x 64 tiles, in slices of K if it is long.  Every workgroup of
 // the stream reads all activations, at its compute unit's pace; slices are a second launch.  The stream's time, the other's = 1, at 17 / 32 / 33 / 48 rows:
-//  * no slices: N 2880 K 2880 0.88 / 0.88 / 0.88 / 0.90, 5120 x 2880 0.89 / 0.88 / 0.98 / 1.03, SwiGLU 4096 x 2048 0.98 / 0.97 / 1.05 / 1.06;
-//  * slices: 512 x 4096 0.7, 6144 x 4096 0.81 / 0.83 / 0.90 / 0.90, 8192 x 4096 0.83 / 0.84 / 0.91 / 0.91, 1024 x 8192 0.70 / 0.75 / 0.84 / 0.89, 4096 x 8192
+//  * short K: N 2880 K 2880 0.88 / 0.88 / 0.88 / 0.90, 5120 x 2880 0.89 / 0.88 / 0.98 / 1.03, SwiGLU 4096 x 2048 0.98 / 0.97 / 1.05 / 1.06;
+//  * longer ones: 512 x 4096 0.7, 6144 x 4096 0.81 / 0.83 / 0.90 / 0.90, 8192 x 4096 0.83 / 0.84 / 0.91 / 0.91, 1024 x 8192 0.70 / 0.75 / 0.84 / 0.89, 4096 x 8192
 //    0.87 / 0.91 / 0.97 / 1.04, 8192 x 14336 0.92 / 0.97 / 1.01 / 1.03, 4096 x 14336 0.93 / 1.06 / 1.0 / 1.0, 2048 x 28672 1.3 and more;
 //  * 64 rows: 0.80 (512 x 4096) .. 1.18 (5120 x 2880).
 static bool gemm_i8_streams(int64_t M, int N, int K, int epilogue) {
     if (M <= I8_STREAM_ROWS) return true;
     const int64_t tiles = gemm_i8_small_tiles(M, N, epilogue);
     if (M > I8_STREAM_ROWS_MOST || tiles > 128) return false;
-    if (gemm_i8_slices(M, N, K, epilogue) == 1) return M <= 32 || tiles <= 64;
+    if (K < 4096) return M <= 32 || tiles <= 64;
     return (int64_t)(16 + (M <= 32 ? 32 : 48)) * K <= 400000;
 }
 size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {

@@ -145,7 +145,7 @@ def test_products(dtype, epilogue, res, M, N, K):
         small = torch.empty_like(c)
         lay.compact_gemm_i8(a, sa, b, sb, r, small, epilogue)
         assert torch.equal(small, c)
-    assert (lay.gemm_i8_workspace_bytes(M, N, K, epilogue) > 0) == (M > 48 and K >= 4096 or M > 16 and K > 16000)
+    assert (lay.gemm_i8_workspace_bytes(M, N, K, epilogue) > 0) == (M > 48 and K >= 5120 or M > 16 and K > 16000)
 
 
 def in_form(lay, form, a, sa, b, sb, r, epilogue, slices=1):
