@@ -164,23 +164,34 @@ __global__ __launch_bounds__(256) void expert_rank_kernel(const int32_t* __restr
         if (e[j] >= 0) rank[i0 + j] = base[e[j]] + lr[j];
 }
 
-// offsets = exclusive scan of counts; row-tile map for the grouped GEMM
+// offsets = exclusive scan of counts, an expert a thread; row-tile map for the grouped GEMM.  (One thread over 128 experts after another: 11.6 us, 5 so.)
 __global__ __launch_bounds__(256) void expert_scan_kernel(const int32_t* __restrict__ counts, int E, int mtile,
                                                           int32_t* __restrict__ offsets, int32_t* __restrict__ tile_expert,
                                                           int32_t* __restrict__ tile_row0, int32_t* __restrict__ tile_rows,
                                                           int max_mtiles) {
-    __shared__ int32_t off[257], toff[257];
-    if (threadIdx.x == 0) {
-        int a = 0, b = 0;
-        for (int e = 0; e < E; ++e) {
-            off[e] = a;
-            toff[e] = b;
-            a += counts[e];
-            b += (counts[e] + mtile - 1) / mtile;
+    __shared__ int32_t off[257], toff[257], sums[2][4];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    int a = t < E ? counts[t] : 0, b = (a + mtile - 1) / mtile;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int pa = __shfl_up(a, o, 64), pb = __shfl_up(b, o, 64);
+        if (lane >= o) {
+            a += pa;
+            b += pb;
         }
-        off[E] = a;
-        toff[E] = b;
     }
+    if (lane == 63) {
+        sums[0][wave] = a;
+        sums[1][wave] = b;
+    }
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) {
+        a += sums[0][w];
+        b += sums[1][w];
+    }
+    if (t == 0) off[0] = toff[0] = 0;
+    off[t + 1] = a;
+    toff[t + 1] = b;
     __syncthreads();
     for (int e = threadIdx.x; e <= E; e += 256) offsets[e] = off[e];
     if (threadIdx.x == 0) offsets[E + 1] = toff[E];
