@@ -212,11 +212,12 @@ def test_broken_scales_stay_in_their_rows_and_columns():
 
 def test_the_residual_may_be_the_output():
     lay = layer()
-    for M in (3, 50, 400):
-        a, b, sa, sb, r = codes(M, 320, 1), codes(136, 320, 2), scales(M, 3), scales(136, 4) * 1e-3, rows_of(M, 136, "bf16", 5)
-        want = product(lay, a, sa, b, sb, r)
-        lay.compact_gemm_i8(a, sa, b, sb, r, r)
-        assert torch.equal(r, want)
+    for M in (3, 20, 40, 50, 400):
+        for N in (136, 137):
+            a, b, sa, sb, r = codes(M, 320, 1), codes(N, 320, 2), scales(M, 3), scales(N, 4) * 1e-3, rows_of(M, N, "bf16", 5)
+            want = product(lay, a, sa, b, sb, r)
+            lay.compact_gemm_i8(a, sa, b, sb, r, r)
+            assert torch.equal(r, want), (M, N)
 
 
 # ---- norms around a block ------------------------------------------------------------------------------------------------------
