@@ -149,7 +149,7 @@ __device__ __forceinline__ void wait_all_memory() {
 #endif
 }
 
-// threads of a launch and grid dimension at most: beyond 32 bits the runtime refuses it
+// threads of a launch and grid dimension at most: beyond 32 bits too few workgroups run, and no error says so
 #define MAX_GRID_THREADS 0xffffffffll
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline size_t dtype_size(int dtype) { return dtype == COMPACT_BF16 ? 2 : 4; }

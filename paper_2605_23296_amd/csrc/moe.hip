@@ -1,6 +1,8 @@
 // Mixture-of-experts plumbing: top-k routing from fp32 logits, the
 // token -> expert permutation (histogram, scan, scatter, row-tile map for the
 // grouped GEMM) and the weighted un-permute + residual.
+#include <algorithm>
+
 #include "common.h"
 #include "vecio.h"
 
@@ -420,16 +422,21 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const T* __restrict__ 
 
 int launch_moe_combine(compact_ctx* ctx, const void* expert_out, const void* h, bool h_is_f32, const int32_t* slot_of,
                        int64_t rows, void* y, hipStream_t s) {
-    if (rows == 0) return COMPACT_OK;
     const compact_layer_cfg& c = ctx->cfg;
-    const unsigned g = (unsigned)rows;
-    if (c.dtype == COMPACT_BF16 && h_is_f32)
-        moe_combine_kernel<bf16, float><<<g, 256, 0, s>>>((const bf16*)expert_out, (const float*)h, slot_of, c.top_k, c.d_model, (bf16*)y);
-    else if (c.dtype == COMPACT_BF16)
-        moe_combine_kernel<bf16, bf16><<<g, 256, 0, s>>>((const bf16*)expert_out, (const bf16*)h, slot_of, c.top_k, c.d_model, (bf16*)y);
-    else
-        moe_combine_kernel<float, float><<<g, 256, 0, s>>>((const float*)expert_out, (const float*)h, slot_of, c.top_k, c.d_model, (float*)y);
-    LAUNCH_CHECK(ctx);
+    constexpr int64_t most = 1ll << 23;   // rows of a launch, of 256 threads each
+    static_assert(most * 256 <= MAX_GRID_THREADS, "one launch");
+    for (int64_t r = 0; r < rows; r += most) {
+        const unsigned g = (unsigned)std::min<int64_t>(rows - r, most);
+        const int32_t* slot = slot_of + r * c.top_k;
+        const int64_t o = r * c.d_model;
+        if (c.dtype == COMPACT_BF16 && h_is_f32)
+            moe_combine_kernel<bf16, float><<<g, 256, 0, s>>>((const bf16*)expert_out, (const float*)h + o, slot, c.top_k, c.d_model, (bf16*)y + o);
+        else if (c.dtype == COMPACT_BF16)
+            moe_combine_kernel<bf16, bf16><<<g, 256, 0, s>>>((const bf16*)expert_out, (const bf16*)h + o, slot, c.top_k, c.d_model, (bf16*)y + o);
+        else
+            moe_combine_kernel<float, float><<<g, 256, 0, s>>>((const float*)expert_out, (const float*)h + o, slot, c.top_k, c.d_model, (float*)y + o);
+        LAUNCH_CHECK(ctx);
+    }
     return COMPACT_OK;
 }
 
