@@ -107,6 +107,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_i8_kernel(const T
 }
 
 // Rows that are too long for that, or whose pieces of 8 are not aligned: the largest value, then the codes, an element at a time.
+// (The column is unsigned: with up to 2^31 - 1 of them, the step past the last one does not fit an int.)
 template <typename T>
 __global__ __launch_bounds__(1024) void quant_i8_any_kernel(const T* __restrict__ x, int64_t x_stride, int cols, int8_t* __restrict__ q,
                                                             float* __restrict__ scale) {
@@ -114,14 +115,14 @@ __global__ __launch_bounds__(1024) void quant_i8_any_kernel(const T* __restrict_
     const int64_t row = blockIdx.x;
     const T* xr = x + row * x_stride;
     uint32_t m = 0;
-    for (int c = threadIdx.x; c < cols; c += 1024) m = max(m, abs_bits(to_f32(xr[c])));
+    for (uint32_t c = threadIdx.x; c < (uint32_t)cols; c += 1024) m = max(m, abs_bits(to_f32(xr[c])));
     m = wave_max_bits(m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = m;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 16; ++w) m = max(m, red[w]);
     const RowCodes rc = row_codes(m);
-    for (int c = threadIdx.x; c < cols; c += 1024) q[row * cols + c] = (int8_t)code_of<T>(to_f32(xr[c]), rc);
+    for (uint32_t c = threadIdx.x; c < (uint32_t)cols; c += 1024) q[row * cols + c] = (int8_t)code_of<T>(to_f32(xr[c]), rc);
     if (threadIdx.x == 0) scale[row] = rc.scale;
 }
 

@@ -13,6 +13,20 @@ def pieces(n, *borders, k=20):
     return [slice(max(0, b - k), min(n, b + k)) for b in (0, *borders, n)]
 
 
+@pytest.mark.parametrize("cols", [2 ** 31 - 1023, 2 ** 31 - 1])
+def test_codes_of_the_longest_rows(cols):
+    """The column that is looked at next passes 2^31 for the first time, and at its most."""
+    x, room = torch.zeros((1, cols), dtype=torch.bfloat16, device="cuda"), 4096
+    buf, scale = torch.full((cols + room,), 77, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+    at, value = [0, 1023, 2 ** 30 + 5, cols - 1025, cols - 2, cols - 1], [127.0, -3.0, 12.0, -127.0, 5.0, -64.0]
+    x[0, at] = torch.tensor(value, dtype=torch.bfloat16, device="cuda")
+    layer().compact_quant_i8(x, buf[:cols].view(1, cols), scale)
+    assert bool((buf[cols:] == 77).all()) and float(scale) == 1.0
+    assert buf[at].tolist() == value
+    buf[at] = 0
+    assert not any(bool(part.any()) for part in buf[:cols].split(2 ** 28))
+
+
 def test_experts_of_more_rows_than_one_launch_of_workgroups():
     E, k, d, F, rows = 8, 1, 64, 64, 2 ** 24 + 5
     lay, ex = layer(d=d, F=F, E=E, k=k), experts(E, d, F, 11)
