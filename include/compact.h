@@ -398,7 +398,8 @@ int compact_quant_i8(compact_ctx* ctx, const void* d_x, int64_t x_stride, int64_
 
 /* C[m, n] = a_scale[m] b_scale[n] sum_k A[m, k] B[n, k] (+ R[m, n] if d_r != NULL): codes A int8 [M, K], B int8 [N, K] (any int8 value,
  * -128 among them), the sum in 32-bit integers, C and R in the storage type.  Epilogue 1 treats B as [2N, K] (b_scale [2N]) stacked gate/up and stores
- * silu(gate) * up.  The sum is scaled in fp32, by a_scale first.  d_r may be d_c.  K a multiple of 16, at most 131056; d_a and d_b 16-byte aligned, any M and N.  With a
+ * silu(gate) * up.  The sum is scaled in fp32, by a_scale first.  d_r may be d_c.  K a multiple of 16, at most 131056; d_a and d_b 16-byte aligned, and d_r and d_c too
+ * where N is a multiple of 8.  At most 2^31 - 1 rows and 2^29 - 128 columns (SwiGLU: 2^28 - 64), any M and N up to there.  With a
  * workspace of compact_gemm_i8_workspace_bytes few rows are faster; a smaller one, or none, changes no bit. */
 int compact_gemm_i8_workspace_bytes(const compact_ctx* ctx, int64_t M, int32_t N, int32_t K, int32_t epilogue, size_t* bytes);
 int compact_gemm_i8(compact_ctx* ctx, const void* d_a, const float* d_a_scale, const void* d_b, const float* d_b_scale, const void* d_r,

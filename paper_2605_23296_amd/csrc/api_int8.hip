@@ -16,23 +16,23 @@ extern "C" int compact_quant_i8(compact_ctx* ctx, const void* d_x, int64_t x_str
     return launch_quant_i8(ctx, d_x, x_stride, rows, cols, (int8_t*)d_q, d_scale, (hipStream_t)hip_stream);
 }
 
-static int check_gemm_i8(const compact_ctx* ctx, int64_t M, int32_t N, int32_t K, int32_t epilogue, const char** why) {
-    (void)ctx;
+static int check_gemm_i8(int64_t M, int32_t N, int32_t K, int32_t epilogue, const char** why) {
     *why = "bad GEMM shape";
     if (M < 0 || N < 1 || K < 1) return COMPACT_EINVAL;
     *why = "epilogue must be 0 or 1";
     if (epilogue != 0 && epilogue != 1) return COMPACT_EINVAL;
     *why = "products of codes need K % 16 == 0 and K <= 131056 (sums of 32 bits)";
     if (K % 16 != 0 || K > 131056) return COMPACT_ESHAPE;
-    *why = "at most 2^31 - 1 rows, 2^30 - 1 columns";
-    if (M > MAX_ROWS || N > 0x3fffffff) return COMPACT_ESHAPE;
+    // (what one launch of the weight stream covers, 128 or 64 columns in 1024 threads; rows go in as many launches as they need)
+    *why = "at most 2^31 - 1 rows, 2^29 - 128 columns (SwiGLU: 2^28 - 64)";
+    if (M > MAX_ROWS || N > (epilogue ? (1 << 28) - 64 : (1 << 29) - 128)) return COMPACT_ESHAPE;
     return COMPACT_OK;
 }
 
 extern "C" int compact_gemm_i8_workspace_bytes(const compact_ctx* ctx, int64_t M, int32_t N, int32_t K, int32_t epilogue, size_t* bytes) {
     if (!ctx || !bytes) return COMPACT_EINVAL;
     const char* why;
-    if (const int rc = check_gemm_i8(ctx, M, N, K, epilogue, &why)) return set_err(const_cast<compact_ctx*>(ctx), rc, why);
+    if (const int rc = check_gemm_i8(M, N, K, epilogue, &why)) return set_err(const_cast<compact_ctx*>(ctx), rc, why);
     *bytes = gemm_i8_workspace(M, N, K, epilogue);
     return COMPACT_OK;
 }
@@ -42,7 +42,7 @@ extern "C" int compact_gemm_i8(compact_ctx* ctx, const void* d_a, const float* d
                                size_t ws_bytes, void* hip_stream) {
     if (!ctx) return COMPACT_EINVAL;
     const char* why;
-    if (const int rc = check_gemm_i8(ctx, M, N, K, epilogue, &why)) return set_err(ctx, rc, why);
+    if (const int rc = check_gemm_i8(M, N, K, epilogue, &why)) return set_err(ctx, rc, why);
     if (M == 0) return COMPACT_OK;
     if (!d_a || !d_a_scale || !d_b || !d_b_scale || !d_c) return set_err(ctx, COMPACT_EINVAL, "null operand");
     if (epilogue == 1 && d_r) return set_err(ctx, COMPACT_EINVAL, "no residual with epilogue 1");

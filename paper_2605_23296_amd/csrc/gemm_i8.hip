@@ -781,6 +781,21 @@ int launch_gemm_i8(compact_ctx* ctx, const GemmI8Args& a, void* ws, size_t ws_by
     GemmI8Params p = i8_params(ctx, a);
     int n_cus = 0;
     TRY(device_cu_count(ctx, &n_cus));
+    // more rows than the smallest row tiles (128 x 64: 512 threads) have workgroups for in one launch: several
+    const int64_t most = 128 * (MAX_GRID_THREADS / (512 * (((int64_t)a.N + (a.epilogue ? 31 : 63)) / (a.epilogue ? 32 : 64))));
+    if (!a.grouped && a.M > most) {
+        const int64_t step = most < 256 ? most : most / 256 * 256, es = dtype_size(ctx->cfg.dtype);
+        for (int64_t r = 0; r < a.M; r += step) {
+            GemmI8Args part = a;
+            part.M = std::min(a.M - r, step);
+            part.a += r * a.K;
+            part.a_scale += r;
+            if (a.r) part.r = (const char*)a.r + r * a.N * es;
+            part.c = (char*)a.c + r * a.N * es;
+            TRY(launch_gemm_i8(ctx, part, ws, ws_bytes, s));
+        }
+        return COMPACT_OK;
+    }
     if (a.grouped) {
         p.g = *a.grouped;
         p.n_mtiles = a.grouped->n_mtiles;

@@ -3,7 +3,7 @@ bits do not depend on the other rows of a call, so large calls are held against 
 import pytest
 import torch
 
-from tests.test_gpu_int8 import by_products, codes, experts, layer, routed, rows_of, scales
+from tests.test_gpu_int8 import by_products, codes, experts, layer, product, routed, rows_of, scales
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,14 @@ def test_experts_of_more_rows_than_one_launch_of_workgroups():
     assert bool((y[rows] == 7.0).all())
     for at in pieces(rows, 2 ** 23, 2 ** 24 - 1):
         assert torch.equal(y[:rows][at], by_products(E, d, F, ex, *(t[at].contiguous() for t in (m, ms, h, idx, w))))
+
+
+def test_products_of_more_rows_than_one_launch_of_workgroups():
+    lay, M, K, N = layer(), 2 ** 30 + 200, 16, 1
+    a, b, sa, sb = codes(M, K, 1), codes(N, K, 2), scales(M, 3), scales(N, 4) / 5000
+    r = scales(M, 5)[:, None].bfloat16()
+    for res in (None, r):
+        c = product(lay, a, sa, b, sb, res)
+        for at in pieces(M, 2 ** 30 - 256, 2 ** 30 - 128, 2 ** 30):
+            assert torch.equal(c[at], product(lay, a[at].contiguous(), sa[at].contiguous(), b, sb, None if res is None else res[at].contiguous()))
+        del c
