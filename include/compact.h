@@ -449,7 +449,8 @@ typedef struct compact_experts_i8 {
 } compact_experts_i8;
 /* y = h + sum_k weight_k FFN_{idx_k}(m), rows m as codes (d_m int8 [rows, d], d_m_scale [rows]), routing given, as compact_moe_ffn; silu(gate) * up is
  * rounded to the storage type and then to codes, a row for each of its experts.  Indices outside 0 .. n_experts - 1 choose no
- * expert.  d_y may be d_h.  bf16 storage only; at most 2^26 / top_k rows. */
+ * expert.  d_y may be d_h.  bf16 storage only; at most 2^26 / top_k rows.  (More rows than one launch covers, some ten million routed ones at F 2880, go in pieces, for
+ * one of which the workspace is.) */
 int compact_moe_ffn_i8_workspace_bytes(const compact_ctx* ctx, int64_t rows, size_t* bytes);
 int compact_moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const void* d_m, const float* d_m_scale, const void* d_h,
                        const int32_t* d_expert_idx, const float* d_weight, int64_t rows, void* d_y, void* d_workspace,

@@ -124,7 +124,13 @@ struct MoeI8Bufs {
     float* act_scale;
 };
 #define MOE_I8_MIN_MTILE 16
+// Rows whose products one launch covers, at any row-tile height (most tiles of 512 threads: 64 x 128): more go in pieces, whose rows have the same bits.
+static int64_t moe_i8_most_rows(const compact_layer_cfg& c) {
+    const int64_t n_tiles = std::max((c.ffn_dim + 63) / 64, (c.d_model + 127) / 128);
+    return std::max<int64_t>(1, 64 * (MAX_GRID_THREADS / (512 * n_tiles) - c.n_experts) / c.top_k);
+}
 static void carve_moe_i8(Carver& cv, const compact_layer_cfg& c, int64_t rows, MoeI8Bufs& b) {
+    rows = std::min(rows, moe_i8_most_rows(c));
     const int64_t rk = rows * c.top_k;
     carve_moe_plan(cv, c, rows, b.plan, MOE_I8_MIN_MTILE);
     b.act_q = (int8_t*)cv.take((size_t)rk * c.ffn_dim);
@@ -170,6 +176,14 @@ static int moe_ffn_i8(compact_ctx* ctx, const compact_experts_i8* experts, const
     carve_moe_i8(cv, c, rows, b);
     if (!d_workspace || !aligned(d_workspace, 16) || cv.off > ws_bytes)
         return set_err(ctx, COMPACT_EWORKSPACE, "workspace too small for the expert feed-forward");
+    if (const int64_t most = moe_i8_most_rows(c); rows > most) {
+        for (int64_t r = 0; r < rows; r += most) {
+            const int64_t o = r * c.d_model, k = r * c.top_k;
+            TRY(moe_ffn_i8(ctx, experts, (const int8_t*)d_m + o, d_m_scale + r, (const bf16*)d_h + o, d_expert_idx + k, d_weight + k,
+                           std::min(rows - r, most), (bf16*)d_y + o, d_workspace, ws_bytes, hip_stream, mtile));
+        }
+        return COMPACT_OK;
+    }
     hipStream_t s = (hipStream_t)hip_stream;
     const int64_t rk = rows * c.top_k;
     int n_cus = 0;

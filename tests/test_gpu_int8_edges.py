@@ -40,6 +40,23 @@ def test_experts_of_more_rows_than_one_launch_of_workgroups():
         assert torch.equal(y[:rows][at], by_products(E, d, F, ex, *(t[at].contiguous() for t in (m, ms, h, idx, w))))
 
 
+def test_experts_whose_products_need_more_workgroups_than_one_launch_has():
+    E, k, d, F, rows = 8, 1, 64, 131008, 270_000
+    lay, ex = layer(d=d, F=F, E=E, k=k), experts(E, d, F, 11)
+    m, ms, h = codes(rows, d, 1), scales(rows, 2) / 70, rows_of(rows, d, "bf16", 3)
+    idx, w = routed(rows, E, k, 5)
+    need = lay.moe_ffn_i8_workspace_bytes(rows)
+    assert need == lay.moe_ffn_i8_workspace_bytes(2 * rows)     # of a piece
+    lay.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    y = torch.full((rows + 1, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    lay.compact_moe_ffn_i8(ex, m, ms, h, idx, w, y[:rows])
+    lay.ws = None
+    assert bool((y[rows] == 7.0).all())
+    border = next(n for n in range(rows) if lay.moe_ffn_i8_workspace_bytes(n) == need)
+    for part in pieces(rows, border):
+        assert torch.equal(y[:rows][part], by_products(E, d, F, ex, *(t[part].contiguous() for t in (m, ms, h, idx, w))))
+
+
 def test_products_of_more_rows_than_one_launch_of_workgroups():
     lay, M, K, N = layer(), 2 ** 30 + 200, 16, 1
     a, b, sa, sb = codes(M, K, 1), codes(N, K, 2), scales(M, 3), scales(N, 4) / 5000
