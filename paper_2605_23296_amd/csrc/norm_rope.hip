@@ -50,16 +50,20 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(const TI* __restrict__ x, c
 }
 
 int launch_rmsnorm(compact_ctx* ctx, const void* x, bool x_is_f32, const void* g, void* y, int64_t rows, hipStream_t s) {
-    if (rows == 0) return COMPACT_OK;
     const int d = ctx->cfg.d_model;
-    const dim3 grid((unsigned)rows);
-    if (ctx->cfg.dtype == COMPACT_BF16 && x_is_f32)
-        rmsnorm_kernel<float, bf16><<<grid, NT, 0, s>>>((const float*)x, (const bf16*)g, (bf16*)y, d, ctx->cfg.rms_eps);
-    else if (ctx->cfg.dtype == COMPACT_BF16)
-        rmsnorm_kernel<bf16, bf16><<<grid, NT, 0, s>>>((const bf16*)x, (const bf16*)g, (bf16*)y, d, ctx->cfg.rms_eps);
-    else
-        rmsnorm_kernel<float, float><<<grid, NT, 0, s>>>((const float*)x, (const float*)g, (float*)y, d, ctx->cfg.rms_eps);
-    LAUNCH_CHECK(ctx);
+    constexpr int64_t most = 1ll << 23;   // rows of a launch
+    static_assert(most * NT <= MAX_GRID_THREADS, "one launch");
+    for (int64_t r = 0; r < rows; r += most) {
+        const dim3 grid((unsigned)std::min<int64_t>(rows - r, most));
+        const int64_t o = r * d;
+        if (ctx->cfg.dtype == COMPACT_BF16 && x_is_f32)
+            rmsnorm_kernel<float, bf16><<<grid, NT, 0, s>>>((const float*)x + o, (const bf16*)g, (bf16*)y + o, d, ctx->cfg.rms_eps);
+        else if (ctx->cfg.dtype == COMPACT_BF16)
+            rmsnorm_kernel<bf16, bf16><<<grid, NT, 0, s>>>((const bf16*)x + o, (const bf16*)g, (bf16*)y + o, d, ctx->cfg.rms_eps);
+        else
+            rmsnorm_kernel<float, float><<<grid, NT, 0, s>>>((const float*)x + o, (const float*)g, (float*)y + o, d, ctx->cfg.rms_eps);
+        LAUNCH_CHECK(ctx);
+    }
     return COMPACT_OK;
 }
 
