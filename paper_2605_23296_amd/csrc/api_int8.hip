@@ -106,12 +106,7 @@ extern "C" int compact_route(compact_ctx* ctx, const compact_route_rule* rule, c
     if (d_m) {
         for (const void* p : {d_m, d_w_router, (const void*)d_logits})
             if (!aligned(p, 16)) return set_err(ctx, COMPACT_EINVAL, "rows, router weights and the logits that they give must be 16-byte aligned");
-        if (c.dtype == COMPACT_BF16)
-            TRY(launch_gemm_bf16(ctx, (const bf16*)d_m, (const bf16*)d_w_router, nullptr, false, (bf16*)d_logits, rows, c.n_experts,
-                                 c.d_model, 2, nullptr, s));
-        else
-            TRY(launch_gemm_f32(ctx, (const float*)d_m, (const float*)d_w_router, nullptr, d_logits, rows, c.n_experts, c.d_model, 0,
-                                nullptr, s));
+        TRY(launch_router_logits(ctx, d_m, d_w_router, rows, d_logits, s));
     }
     return launch_route(ctx, *rule, d_logits, d_bias, rows, d_expert_idx, d_weight, s);
 }

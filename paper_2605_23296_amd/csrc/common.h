@@ -338,6 +338,8 @@ struct MoePlan {              // device buffers carved from the workspace
 };
 // mt: rows per tile of the plan's tile map, which has room for rows * top_k routed rows
 void carve_moe_plan(Carver& cv, const compact_layer_cfg& c, int64_t rows, MoePlan& plan, int mt);
+// logits [rows, n_experts] fp32 = m w_router^T
+int launch_router_logits(compact_ctx* ctx, const void* m, const void* w_router, int64_t rows, float* logits, hipStream_t s);
 int launch_moe_route(compact_ctx* ctx, const void* m, const void* w_router, int64_t rows, int32_t* idx,
                      float* gate, float* logits, hipStream_t s,
                      float* partials_ws = nullptr);   // partials_ws: [ks][rows][E] scratch; enables the few-rows path

@@ -100,6 +100,23 @@ __global__ __launch_bounds__(256) void topk_route_kernel(float* __restrict__ log
     topk_row(v, lane, k, idx + row * k, gate + row * k);
 }
 
+// rows of a launch: 64 threads each at the most, in the product too
+#define ROUTE_ROWS (1ll << 24)
+static_assert(ROUTE_ROWS * 64 <= MAX_GRID_THREADS, "one launch");
+
+int launch_router_logits(compact_ctx* ctx, const void* m, const void* w_router, int64_t rows, float* logits, hipStream_t s) {
+    const compact_layer_cfg& c = ctx->cfg;
+    for (int64_t r = 0; r < rows; r += ROUTE_ROWS) {
+        const int64_t n = std::min<int64_t>(rows - r, ROUTE_ROWS), o = r * c.d_model;
+        float* out = logits + r * c.n_experts;
+        const int rc = c.dtype == COMPACT_BF16
+                           ? launch_gemm_bf16(ctx, (const bf16*)m + o, (const bf16*)w_router, nullptr, false, (bf16*)out, n, c.n_experts, c.d_model, 2, nullptr, s)
+                           : launch_gemm_f32(ctx, (const float*)m + o, (const float*)w_router, nullptr, out, n, c.n_experts, c.d_model, 0, nullptr, s);
+        if (rc != COMPACT_OK) return rc;
+    }
+    return COMPACT_OK;
+}
+
 int launch_moe_route(compact_ctx* ctx, const void* m, const void* w_router, int64_t rows, int32_t* idx, float* gate,
                      float* logits, hipStream_t s, float* partials_ws) {
     if (rows == 0) return COMPACT_OK;
@@ -114,15 +131,14 @@ int launch_moe_route(compact_ctx* ctx, const void* m, const void* w_router, int6
         LAUNCH_CHECK(ctx);
         return COMPACT_OK;
     }
-    if (c.dtype == COMPACT_BF16)
-        rc = launch_gemm_bf16(ctx, (const bf16*)m, (const bf16*)w_router, nullptr, false, (bf16*)logits, rows,
-                              c.n_experts, c.d_model, 2, nullptr, s);
-    else
-        rc = launch_gemm_f32(ctx, (const float*)m, (const float*)w_router, nullptr, logits, rows, c.n_experts,
-                             c.d_model, 0, nullptr, s);
+    rc = launch_router_logits(ctx, m, w_router, rows, logits, s);
     if (rc != COMPACT_OK) return rc;
-    topk_route_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(logits, nullptr, 0, rows, c.n_experts, c.top_k, idx, gate);
-    LAUNCH_CHECK(ctx);
+    for (int64_t r = 0; r < rows; r += ROUTE_ROWS) {
+        const int64_t n = std::min<int64_t>(rows - r, ROUTE_ROWS);
+        topk_route_kernel<<<(unsigned)((n + 3) / 4), 256, 0, s>>>(logits + r * c.n_experts, nullptr, 0, n, c.n_experts, c.top_k, idx + r * c.top_k,
+                                                                  gate + r * c.top_k);
+        LAUNCH_CHECK(ctx);
+    }
     return COMPACT_OK;
 }
 
