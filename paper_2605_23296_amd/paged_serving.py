@@ -53,13 +53,13 @@ def int8_weights(lay, weights):
 class PagedServer:
     """One layer (weights as for binding.Layer; dense or routed) that serves up to n_slots requests at a time from n_pages pages
     of page_rows rows, max_rows rows a step, max_len rows a request.  int8: the projections run from codes made of the weights.  route (routed
-    layers): a binding.RouteRule in the place of the layer's own rule, route_bias fp32 [n_experts] its bias."""
+    layers): a binding.RouteRule in the place of the layer's own rule, route_bias fp32 [n_experts] its bias, or the own rule's."""
 
     def __init__(self, layer, weights, n_slots, n_pages, page_rows, max_rows, max_len, device="cuda", int8=False, route=None, route_bias=None):
         self.lay, self.cfg, self.device = B.Layer(layer, None if int8 else weights), layer, device
         self.route, self.route_bias, self.int8 = route, route_bias, int8
         self.w = int8_weights(self.lay, weights) if int8 else weights
-        if int8 and layer.n_experts and route is None:
+        if layer.n_experts and route is None and (int8 or route_bias is not None):
             self.route = B.RouteRule()      # (the layer's own: softmax over the chosen logits)
         self.slots, self.leaving, self.max_rows, self.max_len = [None] * n_slots, set(), max_rows, max_len
         self.kv = B.PagedKV.allocate(layer, n_slots, -(-max_len // page_rows), n_pages, page_rows, device)
