@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2605_23296_amd import binding as B
-from tests.test_gpu_int8 import by_products, codes, experts, gen, in_form, layer, product, routed, rows_of, scales
+from tests.test_gpu_int8 import RULES, by_products, check_route, codes, experts, gen, in_form, layer, product, routed, rows_of, scales
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +159,20 @@ def test_routing_of_more_rows_than_one_launch_has(rule):
     full = choose(slice(0, rows))
     for at in pieces(rows, 2 ** 24, 2 ** 25):
         assert all(torch.equal(f[at], small) for f, small in zip(full, choose(at)))
+
+
+HARD = {"coarse": lambda x: torch.round(x * 2) / 2, "alike": lambda x: torch.where(x > 1.0, 1.0, -1.0), "close": lambda x: 1 + x * 2.0 ** -21, "low": lambda x: x * 3 - 100,
+        "tiny": lambda x: x * 1e-30, "masked": lambda x: x.index_fill(1, torch.arange(0, x.shape[1], 3), -math.inf), "large": lambda x: x * 20}
+
+
+@pytest.mark.parametrize("kind", HARD)
+@pytest.mark.parametrize("E", [64, 256])
+@pytest.mark.parametrize("bias", [False, True])
+def test_routing_of_hard_rows_by_kind(kind, E, bias):
+    """Rows that 32 bits do not decide, kind by kind, so that how many of each rest on numbers closer than 2^-40 is known: of scores that differ from 1
+    by less than that (large) any number do, of close scores whose sums rank groups some half, of the other kinds hardly one."""
+    x = HARD[kind](torch.randn((400, E), generator=torch.Generator().manual_seed(3)))
+    b = torch.round(8 * torch.randn(E, generator=torch.Generator().manual_seed(4))) / 64 if bias else None
+    for rule in RULES[:6]:
+        sums = rule.get("group_top") == 2 and not bias
+        check_route(layer(E=E, k=8), rule, x.cuda(), None if b is None else b.cuda(), share=-1 if kind == "large" else 0.3 if kind == "close" and sums else 0.97)
