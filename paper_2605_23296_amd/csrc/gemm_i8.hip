@@ -305,6 +305,7 @@ __global__ __launch_bounds__(WM* WN * 64) void gemm_i8_tile_kernel(const GemmI8P
     }
     if (gridDim.y > 1) {
         i8_store_sums<GLU, TM, TN>(p, tp, acc, lane, wm * WTM, tp.n0 + wn * WOUT);
+        wait_all_memory();   // nor must they land in LDS that is another workgroup's by then
         return;
     }
     ring_barrier<0>();   // the repeated loads must not land in the slabs
