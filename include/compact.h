@@ -424,11 +424,12 @@ int compact_block_norm(compact_ctx* ctx, const void* d_x, const void* d_b, const
  * c is compared to 44 bits; without a bias, and where no sums of scores rank groups (no groups, or group_top 1), the logits themselves are compared,
  * of which scores are increasing functions.  An expert whose logit is -inf or NaN, or whose c is -inf or NaN, is chosen only where fewer than top_k
  * others are eligible (weight 0 for the logit's sake), does not count in its group, and a group of such experts is the last choice; a row without
- * a finite logit has weights 0.  Logits of +inf share the softmax among them.  Indices are always distinct and valid. */
+ * a finite logit has weights 0.  Logits of +inf share the softmax among them.  Scores are held in 64 bits: one below their range (a sigmoid's logit under -745) is 0, and so is its
+ * weight, renormalised or not.  Indices are always distinct and valid. */
 enum { COMPACT_SCORE_SOFTMAX = 0, COMPACT_SCORE_SIGMOID = 1 };
 typedef struct compact_route_rule {
     int32_t score;         /* COMPACT_SCORE_* */
-    int32_t n_groups;      /* divides n_experts; 1 = no groups; at most 64 */
+    int32_t n_groups;      /* divides n_experts; 1 = no groups; at most 64 (more than 16: some 30 times the time) */
     int32_t topk_groups;   /* 1 .. n_groups, with top_k experts at least in them */
     int32_t group_top;     /* 1 or 2 */
     int32_t renorm;
@@ -448,7 +449,8 @@ typedef struct compact_experts_i8 {
     const float* d_down_scale;      /* [E, d] */
 } compact_experts_i8;
 /* y = h + sum_k weight_k FFN_{idx_k}(m), rows m as codes (d_m int8 [rows, d], d_m_scale [rows]), routing given, as compact_moe_ffn; silu(gate) * up is
- * rounded to the storage type and then to codes, a row for each of its experts.  Indices outside 0 .. n_experts - 1 choose no
+ * rounded to the storage type and then to codes, a row for each of its experts; an expert's weighted row is rounded to the storage type before the k of them
+ * and h are added in fp32.  Indices outside 0 .. n_experts - 1 choose no
  * expert.  d_y may be d_h.  bf16 storage only; at most 2^26 / top_k rows.  (More rows than one launch covers, some ten million routed ones at F 2880, go in pieces, for
  * one of which the workspace is.) */
 int compact_moe_ffn_i8_workspace_bytes(const compact_ctx* ctx, int64_t rows, size_t* bytes);

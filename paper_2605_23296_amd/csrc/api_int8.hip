@@ -114,6 +114,9 @@ extern "C" int compact_route(compact_ctx* ctx, const compact_route_rule* rule, c
 // ---- the routed experts -----------------------------------------------------------------------------------------------
 struct MoeI8Bufs {
     MoePlan plan;
+    // out: an expert's rows wait in bf16 for their sum, as in compact_moe_ffn.  In fp32 16384 rows of 128 experts of 2880 x 2880, top-4, take 2362 us for 2218 (twice the bytes of
+    // what is written and read again; 16 rows 193.8 for 192.8); the error against 64 bits is 0.0020 of the output, 0.0017 with fp32: the output's own
+    // rounding and the codes of act make the most of it.  The choice may not go by the rows, or a row's bits would depend on the others.
     bf16 *act, *out;
     int8_t* act_q;
     float* act_scale;

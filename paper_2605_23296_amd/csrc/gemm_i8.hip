@@ -722,7 +722,8 @@ static int launch_form(compact_ctx* ctx, int form, int64_t n_full, GemmI8Params&
     return set_err(ctx, COMPACT_EINVAL, "unknown GEMM tile");
 }
 
-// Slices of K for products whose 64 x 64 tiles leave half of the chip idle and more: as many as fill its 256 compute units, of 8 k-tiles at least, and
+// (Both rules count in the 256 compute units of the whole chip, not in those of the device at hand: the workspace's size goes by them, and is asked for where there may be none.)
+// Slices of K for products whose 64 x 64 tiles leave half of the chip idle and more: as many as fill it, of 8 k-tiles at least, and
 // from K 5120 on (the second launch, which adds the slices up, costs 3 us, and the caller's thread 1 more).  Whole and in 2, 3, 4, 5 slices, us:
 //  * 64 rows: N 4096 K 4096 12.0, 11.9, 11.8, 11.1, 13.7 (N 2048 at 128 rows 10.1, 11.1, 10.6, 10.8); K 5120 15.6, 13.8, 12.6, 12.1; K 8192 20.7, 16.4, 14.4, 13.1,
 //    16.7; K 14336 36 whole, 19.2 in 4, 24 in 6;
@@ -746,6 +747,7 @@ static bool gemm_i8_streams(int64_t M, int N, int K, int epilogue) {
     const int64_t tiles = gemm_i8_small_tiles(M, N, epilogue);
     if (M > I8_STREAM_ROWS_MOST || tiles > 128) return false;
     if (K < 4096) return M <= 32 || tiles <= 64;
+    // bytes that a workgroup reads for a column tile, its weight rows and the activations that are staged: the other way's second launch pays from some 400 KB on
     return (int64_t)(16 + (M <= 32 ? 32 : 48)) * K <= 400000;
 }
 size_t gemm_i8_workspace(int64_t M, int N, int K, int epilogue) {

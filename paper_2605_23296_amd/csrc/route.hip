@@ -2,7 +2,7 @@
 //
 // Which expert is chosen, and in which order, is a matter of single comparisons: of 131072 rows of 256 sigmoid scores with a bias some ten have two that 32 bits do not
 // tell apart.  So the order is made of 64-bit values, but only of the few experts that 32 bits leave in question (a whole row in 64 bits: 527 us
-// for those rows).  Bound: the vector ALU, busy without a pause in the 60 us that 8 groups and top-8 of these rows take (2.4 TB/s of logits); 64 rows of 128 3.5 us.
+// for those rows).  Bound: the vector ALU, busy without a pause in the 63 us that 8 groups and top-8 of these rows take (2.3 TB/s of logits, indices and weights); 64 rows of 128 3.5 us.
 // What made it so: four rows a wavefront and candidates 527 -> 93, groups by whole lanes and candidates from a bit mask -> 80, straight loads of
 // full rows and maxima of whole numbers -> 60.
 #include "common.h"
